@@ -318,6 +318,120 @@ a2sf_status a2sf_similarity_mean(const float* cos, int32_t steps, int32_t G, int
 a2sf_status a2sf_decode_plan(int32_t G, int32_t capacity, int32_t d, int32_t* nsplit,
                              int32_t* rows_per_split, int32_t* wave_slots, int32_t* wave_heads);
 
+/* ---- What a decoder layer computes around the attention ----------------------------------------------------------------
+ * Root-mean-square norm, 8-bit rows and their products, rotary positions, sampling: the calls between one attention call
+ * and the next.  The conventions above hold (device pointers, one stream, no allocation, no synchronisation); further:
+ *  - Rows of a tensor lie `stride` elements apart, any stride >= their length (of a single row it is not looked at).
+ *    Pointers need the alignment of their elements only, so rows may be parts of wider ones; 8-bit rows and the workspace:
+ *    16 bytes.
+ *  - Where an input and an output are the same rows, every element is read before it is written.  Other overlaps are
+ *    not allowed.
+ *  - Sums, norms and products are formed in 32 bits or more whatever the type; results are rounded once. */
+typedef struct {
+  void* data;
+  int64_t stride; /* elements from row to row */
+} a2sf_rows;
+
+/* Rows of 8-bit floats (e4m3: largest value 448, no infinities) with a scale for each 128 columns (for weights: for each
+ * 128 x 128).  A scale is a power of two, held as its exponent plus 127 in a byte; 255 stands for "not a number".  The
+ * values stand for q * 2^(scale - 127).  The calls that make them take the smallest scale, no smaller than 2^-127, that brings the
+ * largest magnitude of its block to 448 or below, and round q to nearest, ties to even.  A block that holds an infinity
+ * or a NaN becomes all NaN (scale 255). */
+typedef struct {
+  void* data;           /* rows start at multiples of 16 bytes */
+  uint8_t* scales;      /* [rows (weights: ceil(rows / 128)), ceil(columns / 128)], rows start at multiples of 4 bytes */
+  int64_t stride;       /* bytes from row to row, a multiple of 16 */
+  int64_t scale_stride; /* bytes, a multiple of 4 */
+} a2sf_rows8;
+
+#define A2SF_MAX_ROW 65536 /* longest row of a2sf_rms_norm */
+
+/* h = x + residual;  total = h;  y = h / sqrt(mean(h^2) + eps) * weight, row by row.
+ *   x, residual  [rows, n] dtype; residual may be NULL (h = x).
+ *   weight       [n] dtype.
+ *   total        out [rows, n] dtype; may be NULL, and may be the rows of x or residual.  The norm is of h before its
+ *                rounding to dtype.
+ *   out, out8    out: y in dtype, y in 8 bits; either may be NULL, not both.
+ * n <= A2SF_MAX_ROW, eps >= 0 and finite. */
+a2sf_status a2sf_rms_norm(const a2sf_rows* x, const a2sf_rows* residual, const void* weight, float eps, int32_t rows,
+                          int32_t n, int32_t dtype, const a2sf_rows* total, const a2sf_rows* out,
+                          const a2sf_rows8* out8, void* hip_stream);
+
+/* Rows to 8 bits: y = x, or with a gate y = gate / (1 + exp(-gate)) * x.
+ *   x, gate    [rows, n] dtype; gate may be NULL.
+ *   out, out8  out: y in dtype, y in 8 bits; either may be NULL, not both. */
+a2sf_status a2sf_quantize(const a2sf_rows* x, const a2sf_rows* gate, int32_t rows, int32_t n, int32_t dtype,
+                          const a2sf_rows* out, const a2sf_rows8* out8, void* hip_stream);
+
+/* Weights [n, k] (n outputs of k inputs) to 8 bits with a scale for each 128 x 128; done once, when they are loaded. */
+a2sf_status a2sf_quantize_weight(const a2sf_rows* w, int32_t n, int32_t k, int32_t dtype, const a2sf_rows8* out8,
+                                 void* hip_stream);
+
+/* C = A B^T of 8-bit rows: C[i, j] = sum over blocks of 128 of k: scale of A's block * scale of B's block * sum a b.
+ *   a          [m, k] as a2sf_rms_norm and a2sf_quantize write them.
+ *   b          [n, k] as a2sf_quantize_weight writes them.
+ *   c          out [m, n], c_dtype (A2SF_F32 or A2SF_BF16).
+ *   workspace  may be NULL; with a2sf_matmul_workspace_bytes(m, n, k) bytes (0: none is of use) products that have too few
+ *              tiles for the whole chip split their sums over k.  The same sizes with the same choice give the same bits.
+ * Bytes of the rows past k are not used.  k <= 2^20. */
+size_t a2sf_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
+a2sf_status a2sf_matmul_scaled(const a2sf_rows8* a, const a2sf_rows8* b, int32_t m, int32_t n, int32_t k,
+                               const a2sf_rows* c, int32_t c_dtype, void* workspace, size_t workspace_bytes,
+                               void* hip_stream);
+
+/* Rotary positions.  Each part is the heads [batch, length, heads, d] of one tensor, read and written through strides, so that a
+ * QKV product [batch, length, (Hq + 2 Hkv) d] goes in one call to q [batch, Hq, length, d], k and v [batch, Hkv, length, d]
+ * as a2sf_prefill takes them (length = 1: as a2sf_decode_step does), or turns in place.
+ * Of a head's elements the first rotary_dims turn in pairs, the others are copied.  Pair i has the elements (i, i +
+ * rotary_dims / 2) (A2SF_ROTARY_HALVES) or (2i, 2i + 1) (A2SF_ROTARY_NEIGHBOURS) and becomes
+ * (x0 c - x1 s, x1 c + x0 s) with c, s of the token's position; inverse != 0: with -s, the rotation back, which is also
+ * the gradient's. */
+#define A2SF_MAX_ROTARY_PARTS 4
+typedef enum { A2SF_ROTARY_HALVES = 0, A2SF_ROTARY_NEIGHBOURS = 1 } a2sf_rotary_pairs;
+typedef struct {
+  const void* x;
+  void* y;             /* may be x with the same strides */
+  int64_t x_stride[3]; /* elements from sequence to sequence, token to token, head to head; a head's are contiguous */
+  int64_t y_stride[3];
+  int32_t heads;
+  int32_t rotate; /* 0: copied as they are (the heads of v) */
+} a2sf_rotary_part;
+/*   pos    [batch, length] int32, rows pos_stride apart.  A token whose position is not a row of the table gets NaN in
+ *          the rotated parts' rotary_dims.
+ *   table  [table_rows, rotary_dims] fp32: a position's cosines, then its sines (a2sf_rotary_table).
+ * 1 to A2SF_MAX_ROTARY_PARTS parts, d <= 512, rotary_dims even and <= d. */
+a2sf_status a2sf_rotary(const a2sf_rotary_part* parts, int32_t n_parts, int32_t batch, int32_t length, int32_t d,
+                        int32_t dtype, const int32_t* pos, int64_t pos_stride, const float* table, int32_t table_rows,
+                        int32_t rotary_dims, int32_t pairs, int32_t inverse, void* hip_stream);
+
+/* The table of a2sf_rotary: row p holds magnitude * cos(p f_i), then magnitude * sin(p f_i), f_i = base^(-2 i /
+ * rotary_dims) * (g + (1 - g) / factor), computed in 64 bits.
+ * g, the share of a frequency that a longer context leaves as it is, is 0 for original_length = 0 (all positions are
+ * divided by factor: linear scaling), else it grows from 0 to 1 where the turns that the pair makes over
+ * original_length positions go from low to high. factor = 1: no scaling. */
+a2sf_status a2sf_rotary_table(float* table, int32_t table_rows, int32_t rotary_dims, double base, double factor,
+                              int32_t original_length, double low, double high, double magnitude, void* hip_stream);
+
+/* One token of each row of logits.  The tokens of a row are ordered by logit, larger ones first, equal ones by index; the
+ * filters keep, one after the other, the top_k first; of these the shortest prefix whose probabilities (softmax of
+ * logit / temperature) reach top_p of their sum; of these the ones with at least min_p of the first one's probability.  The
+ * first always stays.  Of what is left the token with the largest probability / noise is taken (the lower index where
+ * equal): with exponential variates as noise, each with its probability.
+ *   logits       [rows, n] dtype.  A NaN counts as -infinity and is never taken; where some are +infinity only those
+ *                can be.  A row of -infinity: token -1, prob 0.
+ *   noise        [rows, n] fp32, positive; NULL: the first token is taken.
+ *   temperature  [rows] fp32, may be NULL (1); <= 0: the first token, whatever the filters.
+ *   top_k        [rows] int32, may be NULL; <= 0 or >= n: all.
+ *   top_p        [rows] fp32, may be NULL; >= 1: all.
+ *   min_p        [rows] fp32, may be NULL; <= 0: all.
+ *   token        out [rows] int32.
+ *   prob         out [rows] fp32, may be NULL: the token's probability among those that were left.
+ * n <= A2SF_MAX_VOCABULARY. */
+#define A2SF_MAX_VOCABULARY 4194304
+a2sf_status a2sf_sample(const a2sf_rows* logits, const a2sf_rows* noise, int32_t rows, int32_t n, int32_t dtype,
+                        const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                        int32_t* token, float* prob, void* hip_stream);
+
 const char* a2sf_status_string(int32_t status);
 
 #ifdef __cplusplus

@@ -24,12 +24,15 @@ A2SF_F32, A2SF_BF16 = 0, 1
 A2SF_EVICT_FAST, A2SF_EVICT_STABLE = 0, 1
 A2SF_MAX_CAPACITY = 36864
 A2SF_STATIC_WS_BYTES = 16 << 20
+A2SF_MAX_ROW, A2SF_MAX_VOCABULARY, A2SF_MAX_ROTARY_PARTS = 65536, 4194304, 4
 
 EXPORTS = ("a2sf_workspace_bytes", "a2sf_prefill", "a2sf_decode_step", "a2sf_select",
            "a2sf_compact", "a2sf_status_string", "a2sf_prefill_alpha_per_head",
            "a2sf_decode_step_alpha_per_head", "a2sf_ideal_similarity", "a2sf_decode_step_static_ws",
            "a2sf_similarity_mean", "a2sf_decode_plan", "a2sf_prefill_windowed",
-           "a2sf_prefill_chunk", "a2sf_prefill_gqa", "a2sf_decode_step_gqa", "a2sf_prefill_chunk_gqa")
+           "a2sf_prefill_chunk", "a2sf_prefill_gqa", "a2sf_decode_step_gqa", "a2sf_prefill_chunk_gqa",
+           "a2sf_rms_norm", "a2sf_quantize", "a2sf_quantize_weight", "a2sf_matmul_workspace_bytes", "a2sf_matmul_scaled",
+           "a2sf_rotary", "a2sf_rotary_table", "a2sf_sample")
 
 
 class Budget(ctypes.Structure):
@@ -40,6 +43,20 @@ class CacheStruct(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scores", ctypes.c_void_p),
                 ("pos", ctypes.c_void_p), ("len", ctypes.c_void_p), ("G", ctypes.c_int32),
                 ("capacity", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class Rows8(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("stride", ctypes.c_int64),
+                ("scale_stride", ctypes.c_int64)]
+
+
+class RotaryPart(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_stride", ctypes.c_int64 * 3),
+                ("y_stride", ctypes.c_int64 * 3), ("heads", ctypes.c_int32), ("rotate", ctypes.c_int32)]
 
 
 _lib = None
@@ -99,6 +116,24 @@ def lib() -> ctypes.CDLL:
         L.a2sf_decode_plan.restype = i32
         L.a2sf_decode_plan.argtypes = [i32, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32),
                                        ctypes.POINTER(i32), ctypes.POINTER(i32)]
+        f64, rows, rows8 = ctypes.c_double, ctypes.POINTER(Rows), ctypes.POINTER(Rows8)
+        L.a2sf_rms_norm.restype = i32
+        L.a2sf_rms_norm.argtypes = [rows, rows, vp, f32, i32, i32, i32, rows, rows, rows8, vp]
+        L.a2sf_quantize.restype = i32
+        L.a2sf_quantize.argtypes = [rows, rows, i32, i32, i32, rows, rows8, vp]
+        L.a2sf_quantize_weight.restype = i32
+        L.a2sf_quantize_weight.argtypes = [rows, i32, i32, i32, rows8, vp]
+        L.a2sf_matmul_workspace_bytes.restype = sz
+        L.a2sf_matmul_workspace_bytes.argtypes = [i32, i32, i32]
+        L.a2sf_matmul_scaled.restype = i32
+        L.a2sf_matmul_scaled.argtypes = [rows8, rows8, i32, i32, i32, rows, i32, vp, sz, vp]
+        L.a2sf_rotary.restype = i32
+        L.a2sf_rotary.argtypes = [ctypes.POINTER(RotaryPart), i32, i32, i32, i32, i32, vp, ctypes.c_int64, vp, i32, i32,
+                                  i32, i32, vp]
+        L.a2sf_rotary_table.restype = i32
+        L.a2sf_rotary_table.argtypes = [vp, i32, i32, f64, f64, i32, f64, f64, f64, vp]
+        L.a2sf_sample.restype = i32
+        L.a2sf_sample.argtypes = [rows, rows, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
         L.a2sf_status_string.restype = ctypes.c_char_p
         L.a2sf_status_string.argtypes = [i32]
         if _call is None:
@@ -115,7 +150,7 @@ class _NoExtension:
     def _leave(*args):
         return -1
 
-    decode_step = prefill = prefill_chunk = _leave
+    decode_step = prefill = prefill_chunk = rms_norm = quantize = matmul_scaled = rotary = sample = _leave
 
 
 def _load_extension():
@@ -376,3 +411,137 @@ def a2sf_compact(cache, keep_idx, keep_stride, n_keep, stream=None):
     cs = _cache_struct(cache)
     _check(lib().a2sf_compact(ctypes.byref(cs), _ptr(keep_idx), keep_stride, _ptr(n_keep),
                               _stream(stream)))
+
+
+# ---- the operators around the attention: rows are 2-D tensors whose sizes, strides and type the C arguments are taken from ----
+
+_EIGHT_BIT = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _need(ok, status=A2SF_ESHAPE):
+    if not ok:
+        raise A2SFError(status)
+
+
+def _rows(x, like, dtype=None):
+    """The C struct of [rows, n] (None of None); `like`: the tensor whose sizes (and type, unless one is named) it has to have."""
+    if x is None:
+        return None
+    _need(x.dim() == 2 and x.shape == like.shape and (x.stride(1) == 1 or x.shape[1] == 1))
+    _need(x.dtype == (dtype or like.dtype), A2SF_EDTYPE)
+    return Rows(x.data_ptr(), x.stride(0))
+
+
+def _rows8(q, scales, rows, n, scale_rows=None):
+    """... of 8-bit rows [rows, n] (torch.float8_e4m3fn, or uint8 for their bytes) and scales [scale_rows, ceil(n / 128)] uint8."""
+    if q is None and scales is None:
+        return None
+    _need(q is not None and scales is not None, A2SF_EINVAL)
+    _need(q.dtype in _EIGHT_BIT and scales.dtype == torch.uint8, A2SF_EDTYPE)
+    _need(tuple(q.shape) == (rows, n) and (q.stride(1) == 1 or n == 1))
+    _need(tuple(scales.shape) == (scale_rows or rows, -(-n // 128)) and (scales.stride(1) == 1 or n <= 128))
+    return Rows8(q.data_ptr(), scales.data_ptr(), q.stride(0), scales.stride(0))
+
+
+def _column(x, rows, dtype):
+    """The address of [rows] (None of None)."""
+    if x is None:
+        return None
+    _need(x.dim() == 1 and x.shape[0] == rows and (x.stride(0) == 1 or rows == 1))
+    _need(x.dtype == dtype, A2SF_EDTYPE)
+    return x.data_ptr()
+
+
+def a2sf_rms_norm(x, weight, eps, residual=None, total=None, out=None, q=None, scales=None, stream=None):
+    at = _entry("a2sf_rms_norm")
+    status = _call.rms_norm(at, x, weight, eps, residual, total, out, q, scales, stream)
+    if status >= 0:
+        return _check(status)
+    _need(x.dim() == 2)
+    rows, n = x.shape
+    _check(lib().a2sf_rms_norm(_rows(x, x), _rows(residual, x), _column(weight, n, x.dtype), eps, rows, n, dtype_code(x.dtype),
+                               _rows(total, x), _rows(out, x), _rows8(q, scales, rows, n), _stream(stream)))
+
+
+def a2sf_quantize(x, q, scales, gate=None, out=None, stream=None):
+    at = _entry("a2sf_quantize")
+    status = _call.quantize(at, x, q, scales, gate, out, stream)
+    if status >= 0:
+        return _check(status)
+    _need(x.dim() == 2)
+    rows, n = x.shape
+    _check(lib().a2sf_quantize(_rows(x, x), _rows(gate, x), rows, n, dtype_code(x.dtype), _rows(out, x),
+                               _rows8(q, scales, rows, n), _stream(stream)))
+
+
+def a2sf_quantize_weight(w, q, scales, stream=None):
+    _need(w.dim() == 2)
+    n, k = w.shape
+    _check(lib().a2sf_quantize_weight(_rows(w, w), n, k, dtype_code(w.dtype), _rows8(q, scales, n, k, -(-n // 128)),
+                                      _stream(stream)))
+
+
+def a2sf_matmul_workspace_bytes(m, n, k) -> int:
+    return int(lib().a2sf_matmul_workspace_bytes(m, n, k))
+
+
+def a2sf_matmul_scaled(a, a_scales, b, b_scales, c, workspace=None, workspace_bytes=None, stream=None):
+    at = _entry("a2sf_matmul_scaled")
+    status = _call.matmul_scaled(at, a, a_scales, b, b_scales, c, workspace, workspace_bytes, stream)
+    if status >= 0:
+        return _check(status)
+    _need(a.dim() == 2 and b.dim() == 2 and c.dim() == 2)
+    m, k = a.shape
+    n = b.shape[0]
+    _need(tuple(c.shape) == (m, n))
+    if workspace_bytes is None:
+        workspace_bytes = workspace.nbytes if workspace is not None else 0
+    _check(lib().a2sf_matmul_scaled(_rows8(a, a_scales, m, k), _rows8(b, b_scales, n, k, -(-n // 128)), m, n, k, _rows(c, c),
+                                    dtype_code(c.dtype), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def a2sf_rotary(parts, pos, table, interleaved=False, inverse=False, stream=None):
+    """parts: (x, y) or (x, y, rotate), each [batch, length, heads, d] with a head's elements next to each other;
+    pos [batch, length] int32; table [rows, rotary_dims] fp32.  interleaved: A2SF_ROTARY_NEIGHBOURS, else A2SF_ROTARY_HALVES."""
+    at = _entry("a2sf_rotary")
+    status = _call.rotary(at, parts, pos, table, interleaved, inverse, stream)
+    if status >= 0:
+        return _check(status)
+    _need(1 <= len(parts) <= A2SF_MAX_ROTARY_PARTS, A2SF_EINVAL)
+    first = parts[0][0]
+    _need(first.dim() == 4)
+    batch, length, _, d = first.shape
+    made = (RotaryPart * len(parts))()
+    for to, (x, y, *rotate) in zip(made, parts):
+        _need(x.dim() == 4 and x.shape == y.shape and x.shape[:2] == (batch, length) and x.shape[3] == d)
+        _need((x.stride(3) == 1 and y.stride(3) == 1) or d == 1)
+        _need(x.dtype == first.dtype and y.dtype == first.dtype, A2SF_EDTYPE)
+        to.x, to.y, to.heads, to.rotate = x.data_ptr(), y.data_ptr(), x.shape[2], int(rotate[0]) if rotate else 1
+        to.x_stride[:], to.y_stride[:] = x.stride()[:3], y.stride()[:3]
+    _need(tuple(pos.shape) == (batch, length) and (pos.stride(1) == 1 or length == 1))
+    _need(table.dim() == 2 and table.is_contiguous())
+    _need(pos.dtype == torch.int32 and table.dtype == torch.float32, A2SF_EDTYPE)
+    _check(lib().a2sf_rotary(made, len(parts), batch, length, d, dtype_code(first.dtype), pos.data_ptr(), pos.stride(0),
+                             table.data_ptr(), table.shape[0], table.shape[1], int(bool(interleaved)), int(bool(inverse)),
+                             _stream(stream)))
+
+
+def a2sf_rotary_table(table, base=10000.0, factor=1.0, original_length=0, low=0.0, high=0.0, magnitude=1.0, stream=None):
+    _need(table.dim() == 2 and table.is_contiguous())
+    _need(table.dtype == torch.float32, A2SF_EDTYPE)
+    _check(lib().a2sf_rotary_table(table.data_ptr(), table.shape[0], table.shape[1], base, factor, original_length, low,
+                                   high, magnitude, _stream(stream)))
+
+
+def a2sf_sample(logits, noise, token, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, stream=None):
+    at = _entry("a2sf_sample")
+    status = _call.sample(at, logits, noise, token, temperature, top_k, top_p, min_p, prob, stream)
+    if status >= 0:
+        return _check(status)
+    _need(logits.dim() == 2)
+    rows, n = logits.shape
+    f = torch.float32
+    _check(lib().a2sf_sample(_rows(logits, logits), _rows(noise, logits, f), rows, n, dtype_code(logits.dtype),
+                             _column(temperature, rows, f), _column(top_k, rows, torch.int32), _column(top_p, rows, f),
+                             _column(min_p, rows, f), _column(token, rows, torch.int32), _column(prob, rows, f),
+                             _stream(stream)))

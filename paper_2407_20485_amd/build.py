@@ -9,6 +9,7 @@ import os
 import subprocess
 import sys
 import sysconfig
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -16,7 +17,8 @@ LIB = os.path.join(HERE, "liba2sf.so")
 CALL = os.path.join(HERE, "_call.so")
 CEILINGS = os.path.join(HERE, "ceilings")
 SOURCES = ["a2sf_api.hip", "decode.hip", "select_compact.hip", "prefill_f32.hip", "prefill_bf16.hip",
-           "similarity.hip", "chunk.hip"]
+           "similarity.hip", "chunk.hip", "layer_api.hip", "rows.hip", "matmul.hip", "rotary.hip", "sample.hip"]
+OBJECTS = os.path.join(HERE, "_build")
 # -packed-fp32-ops is switched off: packed fp32 forms have produced wrong results on the
 # target machines; the host pass does not know the feature and says so (harmless).
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17",
@@ -60,9 +62,17 @@ def build_call(verbose: bool = False) -> str:
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     generate()
-    _compile([hipcc, *FLAGS, *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB], verbose)
-    build_call(verbose)
-    _compile([hipcc, *COMMON, os.path.join(CSRC, "ceilings.hip"), "-o", CEILINGS], verbose)
+    os.makedirs(OBJECTS, exist_ok=True)
+    objects = {s: os.path.join(OBJECTS, s.replace(".hip", ".o")) for s in SOURCES}
+    # the sources are independent of each other: an object each, several at a time
+    with ThreadPoolExecutor(max(1, min(8, os.cpu_count() or 1))) as pool:
+        jobs = [pool.submit(_compile, [hipcc, *COMMON, "-fPIC", "-c", os.path.join(CSRC, s), "-o", o], verbose)
+                for s, o in objects.items()]
+        jobs.append(pool.submit(build_call, verbose))
+        jobs.append(pool.submit(_compile, [hipcc, *COMMON, os.path.join(CSRC, "ceilings.hip"), "-o", CEILINGS], verbose))
+        for j in jobs:
+            j.result()
+    _compile([hipcc, *FLAGS, *objects.values(), "-o", LIB], verbose)
     return LIB
 
 

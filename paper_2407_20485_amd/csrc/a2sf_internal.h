@@ -139,4 +139,73 @@ void launch_scores_bf16(const void* q, const void* k, const float* lse2, int G, 
 // Also returns log2(alpha) as used in the exponent (0 for alpha == 0, whose only row is n-1).
 int first_contributing_row(int n, float alpha, float* log2_alpha);
 
+// ---- the operators around the attention ------------------------------------------------------------------------------------
+// rows.hip.  Strides in elements (8-bit rows and scales: bytes); absent tensors are null.
+struct NormArgs {
+  const void *x, *residual, *weight;
+  void *total, *out;
+  uint8_t *q, *scales;
+  long long x_stride, residual_stride, total_stride, out_stride, q_stride, scale_stride;
+  float eps;
+  int rows, n;
+};
+void launch_rms_norm(const NormArgs& a, int dtype, hipStream_t st);
+struct QuantArgs {
+  const void *x, *gate;
+  void* out;
+  uint8_t *q, *scales;
+  long long x_stride, gate_stride, out_stride, q_stride, scale_stride;
+  int rows, n, blocks_per_row;
+};
+void launch_quantize(const QuantArgs& a, int dtype, hipStream_t st);
+void launch_quantize_weight(const QuantArgs& a, int dtype, hipStream_t st);
+
+// matmul.hip: C[m, n] = A[m, k] B[n, k]^T
+struct MatmulArgs {
+  const uint8_t *a, *a_scales, *b, *b_scales;
+  void* c;
+  long long a_stride, a_scale_stride, b_stride, b_scale_stride, c_stride;
+  int m, n, k;
+};
+size_t matmul_workspace(int m, int n, int k);
+void launch_matmul(const MatmulArgs& a, int dtype, void* workspace, size_t workspace_bytes, hipStream_t st);
+
+// rotary.hip
+struct RotaryPart {
+  const void* x;
+  void* y;
+  long long x_stride[3], y_stride[3];  // batch, position, head
+  int rotate, in_place;
+};
+struct RotaryArgs {
+  RotaryPart part[A2SF_MAX_ROTARY_PARTS];
+  int first_head[A2SF_MAX_ROTARY_PARTS + 1];  // heads of all parts in a row; the unused end repeats the total
+  int heads, batch, length, d, rot, inverse;
+  const int32_t* pos;
+  long long pos_stride;
+  const float* table;
+  int table_rows;
+  int items, lanes, tokens_per_block;  // set by the launcher
+};
+void launch_rotary(RotaryArgs a, int dtype, bool neighbours, hipStream_t st);
+struct RotaryTableArgs {
+  float* table;
+  int rows, rot, original_length;
+  double base, factor, low, high, magnitude;
+};
+void launch_rotary_table(const RotaryTableArgs& a, hipStream_t st);
+
+// sample.hip
+struct SampleArgs {
+  const void* logits;
+  const float* noise;
+  const float *temperature, *top_p, *min_p;
+  const int32_t* top_k;
+  int32_t* token;
+  float* prob;
+  long long stride, noise_stride;
+  int rows, n;
+};
+void launch_sample(const SampleArgs& a, int dtype, hipStream_t st);
+
 }  // namespace a2sf

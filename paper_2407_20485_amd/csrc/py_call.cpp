@@ -183,6 +183,196 @@ PyObject* prefill_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the operators around the attention: [rows, n] tensors, whose sizes, strides and types the C arguments come from.  What
+// does not fit together (or is no plain tensor) is left to binding.py, which names the error.
+bool type_of(const at::Tensor& t, int32_t* dtype) {
+  const auto k = t.scalar_type();
+  *dtype = k == at::kFloat ? A2SF_F32 : A2SF_BF16;
+  return k == at::kFloat || k == at::kBFloat16;
+}
+bool matrix(const at::Tensor& t, int64_t rows, int64_t n) {
+  return t.dim() == 2 && t.size(0) == rows && t.size(1) == n && (n == 1 || t.stride(1) == 1);
+}
+// `to` is null after an absent tensor
+bool rows_like(PyObject* x, const at::Tensor& like, at::ScalarType type, a2sf_rows* s, const a2sf_rows** to) {
+  const at::Tensor* t;
+  *to = nullptr;
+  if (x == Py_None) return true;
+  if (!tensor(x, &t) || t->scalar_type() != type || !matrix(*t, like.size(0), like.size(1))) return false;
+  *s = {t->data_ptr(), t->stride(0)};
+  *to = s;
+  return true;
+}
+bool rows8(PyObject* q, PyObject* scales, int64_t rows, int64_t scale_rows, int64_t n, a2sf_rows8* s, const a2sf_rows8** to) {
+  const at::Tensor *t, *u;
+  *to = nullptr;
+  if (q == Py_None && scales == Py_None) return true;
+  if (!tensor(q, &t) || !tensor(scales, &u) || u->scalar_type() != at::kByte) return false;
+  if (t->scalar_type() != at::kFloat8_e4m3fn && t->scalar_type() != at::kByte) return false;
+  const int64_t nb = n / 128 + (n % 128 != 0);
+  if (!matrix(*t, rows, n) || !matrix(*u, scale_rows, nb)) return false;
+  *s = {t->data_ptr(), (uint8_t*)u->data_ptr(), t->stride(0), u->stride(0)};
+  *to = s;
+  return true;
+}
+bool column(PyObject* x, int64_t rows, at::ScalarType type, const void** p) {
+  const at::Tensor* t;
+  *p = nullptr;
+  if (x == Py_None) return true;
+  if (!tensor(x, &t) || t->scalar_type() != type || t->dim() != 1 || t->size(0) != rows || (rows != 1 && t->stride(0) != 1))
+    return false;
+  *p = t->data_ptr();
+  return true;
+}
+bool first(PyObject* x, const at::Tensor** t, int32_t* dtype) {  // the tensor that gives a call its sizes
+  return tensor(x, t) && (*t)->dim() == 2 && type_of(**t, dtype) && (*t)->size(0) <= INT32_MAX && (*t)->size(1) <= INT32_MAX;
+}
+
+// (entry point, x, weight, eps, residual, total, out, q, scales, stream)
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!expects(n, 10)) return nullptr;
+  return guarded([&] {
+    void *st, *fn = PyLong_AsVoidPtr(a[0]);
+    const at::Tensor* x;
+    const void* w;
+    a2sf_rows s[4];
+    a2sf_rows8 s8;
+    const a2sf_rows *rx, *residual, *total, *out;
+    const a2sf_rows8* out8;
+    int32_t dtype;
+    float eps;
+    if (!(fn && first(a[1], &x, &dtype) && rows_like(a[1], *x, x->scalar_type(), s, &rx) &&
+          column(a[2], x->size(1), x->scalar_type(), &w) && number(a[3], &eps) &&
+          rows_like(a[4], *x, x->scalar_type(), s + 1, &residual) && rows_like(a[5], *x, x->scalar_type(), s + 2, &total) &&
+          rows_like(a[6], *x, x->scalar_type(), s + 3, &out) && rows8(a[7], a[8], x->size(0), x->size(0), x->size(1), &s8, &out8) &&
+          stream(a[9], a[1], &st)))
+      return -1;
+    return without_gil([&]() -> int {
+      return ((decltype(&a2sf_rms_norm))fn)(rx, residual, w, eps, (int32_t)x->size(0), (int32_t)x->size(1), dtype, total, out,
+                                            out8, st);
+    });
+  });
+}
+
+// (entry point, x, q, scales, gate, out, stream)
+PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!expects(n, 7)) return nullptr;
+  return guarded([&] {
+    void *st, *fn = PyLong_AsVoidPtr(a[0]);
+    const at::Tensor* x;
+    a2sf_rows s[3];
+    a2sf_rows8 s8;
+    const a2sf_rows *rx, *gate, *out;
+    const a2sf_rows8* out8;
+    int32_t dtype;
+    if (!(fn && first(a[1], &x, &dtype) && rows_like(a[1], *x, x->scalar_type(), s, &rx) &&
+          rows8(a[2], a[3], x->size(0), x->size(0), x->size(1), &s8, &out8) &&
+          rows_like(a[4], *x, x->scalar_type(), s + 1, &gate) && rows_like(a[5], *x, x->scalar_type(), s + 2, &out) &&
+          stream(a[6], a[1], &st)))
+      return -1;
+    return without_gil([&]() -> int {
+      return ((decltype(&a2sf_quantize))fn)(rx, gate, (int32_t)x->size(0), (int32_t)x->size(1), dtype, out, out8, st);
+    });
+  });
+}
+
+// (entry point, a, a_scales, b, b_scales, c, workspace, workspace_bytes, stream)
+PyObject* matmul_scaled(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!expects(n, 9)) return nullptr;
+  return guarded([&] {
+    void *ws, *st, *fn = PyLong_AsVoidPtr(a[0]);
+    const at::Tensor *c, *b;
+    a2sf_rows s;
+    a2sf_rows8 s8[2];
+    const a2sf_rows* rc;
+    const a2sf_rows8 *ra, *rb;
+    const at::Tensor* ta;
+    size_t bytes;
+    int32_t dtype;
+    if (!(fn && first(a[5], &c, &dtype) && rows_like(a[5], *c, c->scalar_type(), &s, &rc) && tensor(a[1], &ta) && ta->dim() == 2 &&
+          tensor(a[3], &b) && ta->size(1) <= INT32_MAX &&
+          rows8(a[1], a[2], c->size(0), c->size(0), ta->size(1), s8, &ra) &&
+          rows8(a[3], a[4], c->size(1), c->size(1) / 128 + (c->size(1) % 128 != 0), ta->size(1), s8 + 1, &rb) &&
+          workspace(a[6], a[7], &ws, &bytes) && stream(a[8], a[1], &st)))
+      return -1;
+    return without_gil([&]() -> int {
+      return ((decltype(&a2sf_matmul_scaled))fn)(ra, rb, (int32_t)c->size(0), (int32_t)c->size(1), (int32_t)ta->size(1), rc, dtype,
+                                                 ws, bytes, st);
+    });
+  });
+}
+
+// (entry point, list of (x, y[, rotate]), pos, table, interleaved, inverse, stream)
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!expects(n, 7)) return nullptr;
+  return guarded([&] {
+    void *st, *fn = PyLong_AsVoidPtr(a[0]);
+    const at::Tensor *x, *y, *head = nullptr, *pos, *table;
+    a2sf_rotary_part parts[A2SF_MAX_ROTARY_PARTS];
+    int32_t dtype = 0;
+    if (!fn || !PyList_CheckExact(a[1]) || PyList_GET_SIZE(a[1]) < 1 || PyList_GET_SIZE(a[1]) > A2SF_MAX_ROTARY_PARTS) return -1;
+    const int count = (int)PyList_GET_SIZE(a[1]);
+    for (int i = 0; i < count; ++i) {
+      PyObject* p = PyList_GET_ITEM(a[1], i);
+      if (!PyTuple_CheckExact(p) || PyTuple_GET_SIZE(p) < 2 || PyTuple_GET_SIZE(p) > 3) return -1;
+      if (!tensor(PyTuple_GET_ITEM(p, 0), &x) || !tensor(PyTuple_GET_ITEM(p, 1), &y) || x->dim() != 4 || x->sizes() != y->sizes()) return -1;
+      PyObject* turn = PyTuple_GET_SIZE(p) == 3 ? PyTuple_GET_ITEM(p, 2) : Py_True;
+      if (!PyBool_Check(turn)) return -1;
+      if (i == 0) {
+        head = x;
+        if (!type_of(*x, &dtype)) return -1;
+        for (int j = 0; j < 4; ++j)
+          if (x->size(j) > INT32_MAX) return -1;
+      }
+      if (x->size(0) != head->size(0) || x->size(1) != head->size(1) || x->size(3) != head->size(3) || x->size(2) > INT32_MAX ||
+          x->scalar_type() != head->scalar_type() || y->scalar_type() != head->scalar_type() ||
+          (x->size(3) != 1 && (x->stride(3) != 1 || y->stride(3) != 1)))
+        return -1;
+      parts[i].x = x->data_ptr();
+      parts[i].y = y->data_ptr();
+      for (int j = 0; j < 3; ++j) {
+        parts[i].x_stride[j] = x->stride(j);
+        parts[i].y_stride[j] = y->stride(j);
+      }
+      parts[i].heads = (int32_t)x->size(2);
+      parts[i].rotate = turn == Py_True;
+    }
+    if (!tensor(a[2], &pos) || pos->scalar_type() != at::kInt || !matrix(*pos, head->size(0), head->size(1)) || !tensor(a[3], &table) ||
+        table->scalar_type() != at::kFloat || table->dim() != 2 || !table->is_contiguous() || table->size(0) > INT32_MAX ||
+        table->size(1) > INT32_MAX || !PyBool_Check(a[4]) || !PyBool_Check(a[5]) || !stream(a[6], a[2], &st))
+      return -1;
+    return without_gil([&]() -> int {
+      return ((decltype(&a2sf_rotary))fn)(parts, count, (int32_t)head->size(0), (int32_t)head->size(1), (int32_t)head->size(3), dtype,
+                                          (const int32_t*)pos->data_ptr(), pos->stride(0), (const float*)table->data_ptr(),
+                                          (int32_t)table->size(0), (int32_t)table->size(1), a[4] == Py_True, a[5] == Py_True, st);
+    });
+  });
+}
+
+// (entry point, logits, noise, token, temperature, top_k, top_p, min_p, prob, stream)
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!expects(n, 10)) return nullptr;
+  return guarded([&] {
+    void *st, *fn = PyLong_AsVoidPtr(a[0]);
+    const at::Tensor* x;
+    a2sf_rows s[2];
+    const a2sf_rows *logits, *noise;
+    const void *token, *temperature, *top_k, *top_p, *min_p, *prob;
+    int32_t dtype;
+    if (!(fn && first(a[1], &x, &dtype) && rows_like(a[1], *x, x->scalar_type(), s, &logits) &&
+          rows_like(a[2], *x, at::kFloat, s + 1, &noise) && column(a[3], x->size(0), at::kInt, &token) &&
+          column(a[4], x->size(0), at::kFloat, &temperature) && column(a[5], x->size(0), at::kInt, &top_k) &&
+          column(a[6], x->size(0), at::kFloat, &top_p) && column(a[7], x->size(0), at::kFloat, &min_p) &&
+          column(a[8], x->size(0), at::kFloat, &prob) && stream(a[9], a[1], &st)))
+      return -1;
+    return without_gil([&]() -> int {
+      return ((decltype(&a2sf_sample))fn)(logits, noise, (int32_t)x->size(0), (int32_t)x->size(1), dtype, (const float*)temperature,
+                                          (const int32_t*)top_k, (const float*)top_p, (const float*)min_p, (int32_t*)token,
+                                          (float*)prob, st);
+    });
+  });
+}
+
 // (binding.Cache, torch.float32, torch.bfloat16, function device -> current raw stream or None, function -> current device)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!expects(n, 5)) return nullptr;
@@ -199,6 +389,11 @@ PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)())init, METH_FASTCALL, 
                          {"decode_step", (PyCFunction)(void (*)())decode_step, METH_FASTCALL, nullptr},
                          {"prefill", (PyCFunction)(void (*)())prefill, METH_FASTCALL, nullptr},
                          {"prefill_chunk", (PyCFunction)(void (*)())prefill_chunk, METH_FASTCALL, nullptr},
+                         {"rms_norm", (PyCFunction)(void (*)())rms_norm, METH_FASTCALL, nullptr},
+                         {"quantize", (PyCFunction)(void (*)())quantize, METH_FASTCALL, nullptr},
+                         {"matmul_scaled", (PyCFunction)(void (*)())matmul_scaled, METH_FASTCALL, nullptr},
+                         {"rotary", (PyCFunction)(void (*)())rotary, METH_FASTCALL, nullptr},
+                         {"sample", (PyCFunction)(void (*)())sample, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,188 @@
+// Row operators of a decoder layer: residual sum with root-mean-square norm, and conversion to 8-bit rows (of rows, of
+// silu(gate) * rows, of weights).  All read and write each element once and are bound by memory.
+#include "a2sf_internal.h"
+#include "rows_dev.h"
+
+namespace a2sf {
+namespace {
+
+// ---- y = h / sqrt(mean(h^2) + eps) * w,  h = x + residual ----------------------------------------------------------------
+// A row stays in registers between the sum of its squares and its scaling: V units of eight elements per lane, unit
+// i * THREADS + t in lane t, so that 16 neighbouring lanes hold the 128 columns of a scale and the wave's accesses are
+// contiguous.  h is formed, squared, summed and scaled in fp32; only the stored sum is rounded to the rows' type (the norm is
+// of the sum before that rounding, which costs nothing here and is nearer to the definition).
+// THREADS = 64: a wave per row, four rows per workgroup, no barrier.
+template <typename T, int THREADS, int V>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel(NormArgs a) {
+  constexpr int kRows = THREADS == 64 ? 4 : 1;
+  const int t = threadIdx.x % THREADS;
+  const long long row = (long long)blockIdx.x * kRows + threadIdx.x / THREADS;
+  if (kRows > 1 && row >= a.rows) return;  // whole waves: nothing below waits for them
+  const T* x = (const T*)a.x + row * a.x_stride;
+  const T* r = a.residual ? (const T*)a.residual + row * a.residual_stride : nullptr;
+  float h[V][kUnit];
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < V; ++i) load_unit(x + (i * THREADS + t) * kUnit, a.n - (i * THREADS + t) * kUnit, h[i]);
+  if (r) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      float g[kUnit];
+      load_unit(r + (i * THREADS + t) * kUnit, a.n - (i * THREADS + t) * kUnit, g);
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) h[i][j] += g[j];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) sum = fmaf(h[i][j], h[i][j], sum);
+  sum = wave_sum(sum);
+  if constexpr (THREADS > 64) {
+    __shared__ float part[THREADS / 64];
+    if ((t & 63) == 0) part[t >> 6] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) sum += part[w];
+  }
+  const float scale = 1.0f / sqrtf(sum / (float)a.n + a.eps);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int c = (i * THREADS + t) * kUnit;
+    const int have = a.n - c;
+    // the 16 lanes of a block that ends inside it stay together: the exchange below reads all of them
+    if ((c & ~(kBlock - 1)) >= a.n) break;
+    if (a.total && have > 0) store_unit((T*)a.total + row * a.total_stride + c, have, h[i]);
+    float w[kUnit];
+    load_unit((const T*)a.weight + c, have, w);
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) h[i][j] = h[i][j] * scale * w[j];
+    if (have < kUnit) {
+      // columns past the end are 0 also where the row's scale is not a number
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) h[i][j] = j < have ? h[i][j] : 0.f;
+    }
+    if (a.out && have > 0) store_unit((T*)a.out + row * a.out_stride + c, have, h[i]);
+    if (a.q) {
+      const uint32_t b = scale_byte(block_top(unit_top(h[i])));
+      if (have > 0) store_eight_bits(a.q + row * a.q_stride + c, have, to_eight_bits(h[i], b));
+      if ((t & 15) == 0) a.scales[row * a.scale_stride + c / kBlock] = (uint8_t)b;
+    }
+  }
+}
+
+template <typename T, int THREADS, int V>
+void norm(const NormArgs& a, hipStream_t st) {
+  constexpr int kRows = THREADS == 64 ? 4 : 1;
+  rms_norm_kernel<T, THREADS, V><<<dim3((a.rows + kRows - 1) / kRows), dim3(THREADS == 64 ? 256 : THREADS), 0, st>>>(a);
+}
+template <typename T, int THREADS>
+void norm_units(const NormArgs& a, hipStream_t st) {
+  const int v = (a.n + THREADS * kUnit - 1) / (THREADS * kUnit);
+  if (v <= 1) return norm<T, THREADS, 1>(a, st);
+  if (v <= 2) return norm<T, THREADS, 2>(a, st);
+  if constexpr (THREADS > 64) {
+    if (v <= 3) return norm<T, THREADS, 3>(a, st);
+    if (v <= 4) return norm<T, THREADS, 4>(a, st);
+    if constexpr (THREADS == 256) {
+      if (v <= 6) return norm<T, THREADS, 6>(a, st);
+    }
+    return norm<T, THREADS, 8>(a, st);
+  }
+}
+template <typename T>
+void norm_type(const NormArgs& a, hipStream_t st) {
+  if (a.n <= 2 * 64 * kUnit) return norm_units<T, 64>(a, st);
+  if (a.rows < 512 && a.n > 256 * kUnit) {
+    // few rows: the time is a chain of round trips, the more lanes the shorter
+    if (a.n <= 512 * kUnit) return norm<T, 512, 1>(a, st);
+    return norm_units<T, 1024>(a, st);
+  }
+  if (a.n <= 8 * 256 * kUnit) return norm_units<T, 256>(a, st);
+  return norm_units<T, 1024>(a, st);
+}
+
+// ---- rows or silu(gate) * rows, to the rows' type and / or to 8 bits -------------------------------------------------------
+// 16 lanes take a block of 128 columns.
+template <typename T, bool GATE>
+__global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
+  const uint32_t block = blockIdx.x * 16u + threadIdx.x / 16;
+  const uint32_t row = block / (uint32_t)a.blocks_per_row;
+  if (row >= (uint32_t)a.rows) return;  // all 16 lanes of a block
+  const int c = (int)(block - row * (uint32_t)a.blocks_per_row) * kBlock + (threadIdx.x & 15) * kUnit;
+  const int have = a.n - c;
+  float f[kUnit];
+  load_unit((const T*)a.x + (long long)row * a.x_stride + c, have, f);
+  if constexpr (GATE) {
+    float g[kUnit];
+    load_unit((const T*)a.gate + (long long)row * a.gate_stride + c, have, g);
+    // g / (1 + e^-g) * x: v_exp_f32 and v_rcp_f32 are good to the last bit or two of fp32; e^-g = inf gives 0
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j)
+      f[j] = g[j] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g[j] * -1.44269504088896340736f)) * f[j];
+  }
+  if (a.out && have > 0) store_unit((T*)a.out + (long long)row * a.out_stride + c, have, f);
+  if (a.q) {
+    const uint32_t b = scale_byte(block_top(unit_top(f)));
+    if (have > 0) store_eight_bits(a.q + (long long)row * a.q_stride + c, have, to_eight_bits(f, b));
+    if ((threadIdx.x & 15) == 0) a.scales[(long long)row * a.scale_stride + c / kBlock] = (uint8_t)b;
+  }
+}
+
+// ---- weights: a scale per 128 x 128 ------------------------------------------------------------------------------------------
+// A workgroup per tile, 16 rows of it per step; the tile stays in registers (64 values per lane).
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_weight_kernel(QuantArgs a) {
+  const int r0 = (int)(blockIdx.x / (uint32_t)a.blocks_per_row) * kBlock;
+  const int c = (int)(blockIdx.x % (uint32_t)a.blocks_per_row) * kBlock + (threadIdx.x & 15) * kUnit;
+  const int have = a.n - c;
+  float f[kBlock / 16][kUnit];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < kBlock / 16; ++i) {
+    const int row = r0 + i * 16 + threadIdx.x / 16;
+    load_unit((const T*)a.x + (long long)row * a.x_stride + c, row < a.rows ? have : 0, f[i]);
+    top = max(top, unit_top(f[i]));
+  }
+  top = block_top(top);
+  __shared__ uint32_t part[16];
+  if ((threadIdx.x & 15) == 0) part[threadIdx.x / 16] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, part[i]);
+  const uint32_t b = scale_byte(top);
+#pragma unroll
+  for (int i = 0; i < kBlock / 16; ++i) {
+    const int row = r0 + i * 16 + threadIdx.x / 16;
+    if (row < a.rows && have > 0)
+      store_eight_bits(a.q + (long long)row * a.q_stride + c, have, to_eight_bits(f[i], b));
+  }
+  if (threadIdx.x == 0) a.scales[(long long)(r0 / kBlock) * a.scale_stride + c / kBlock] = (uint8_t)b;
+}
+
+}  // namespace
+
+void launch_rms_norm(const NormArgs& a, int dtype, hipStream_t st) {
+  if (dtype == A2SF_F32) norm_type<float>(a, st);
+  else norm_type<bf16_t>(a, st);
+}
+
+void launch_quantize(const QuantArgs& a, int dtype, hipStream_t st) {
+  const dim3 grid((uint32_t)(((long long)a.rows * a.blocks_per_row + 15) / 16));
+  if (dtype == A2SF_F32) {
+    if (a.gate) quantize_kernel<float, true><<<grid, 256, 0, st>>>(a);
+    else quantize_kernel<float, false><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (a.gate) quantize_kernel<bf16_t, true><<<grid, 256, 0, st>>>(a);
+    else quantize_kernel<bf16_t, false><<<grid, 256, 0, st>>>(a);
+  }
+}
+
+void launch_quantize_weight(const QuantArgs& a, int dtype, hipStream_t st) {
+  const dim3 grid((uint32_t)((a.rows + kBlock - 1) / kBlock) * (uint32_t)a.blocks_per_row);
+  if (dtype == A2SF_F32) quantize_weight_kernel<float><<<grid, 256, 0, st>>>(a);
+  else quantize_weight_kernel<bf16_t><<<grid, 256, 0, st>>>(a);
+}
+
+}  // namespace a2sf

@@ -1,0 +1,585 @@
+"""The operators around the attention on the GPU against the float64 oracle.
+
+Tolerances, from the arithmetic (u = 2^-24 is fp32's unit of rounding):
+  * a sum of n squares by fused multiply-adds, at most 64 + 16 of them one after the other, is off by at most 80 u, its root by 40 u;
+    with the additions, divisions and products around it a norm is within 48 u = 3e-6 of its value, plus 2^-8 where it is
+    rounded to bf16;
+  * silu: two instructions of about one u each, the exponent's argument off by |g| u with |g| <= 88: 100 u = 6e-6;
+  * 8-bit values: half a step of three bits, 2^-4 of the value, or half a step of the smallest, 2^-10 of the scale;
+    without arithmetic before it (plain rows) the conversion is exact to the bit;
+  * a product of k terms in fp32: k u times the sum of the magnitudes; for a bf16 result the matrix instruction cuts each of eight
+    products under 2^-13 of the largest of them: 8 * 2^-13 of that sum; of small whole numbers it is exact.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_oracle as L
+from paper_2407_20485_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+BF16 = 2.0 ** -8  # half of the distance 2^-7 between neighbours of seven bits behind the point, of the smallest value that has it
+
+
+def up(x, m):
+    return -(-x // m) * m
+
+
+def rng(*key):
+    return np.random.default_rng([7, *key])
+
+
+def on_gpu(a, dtype, stride=None, offset=0):
+    """A tensor of a's values whose rows lie `stride` elements apart and start `offset` elements into an allocation."""
+    a = torch.from_numpy(np.ascontiguousarray(a)).float()
+    rows, n = a.shape
+    stride = stride or n
+    store = torch.full((offset + rows * stride + 16,), 7.0, dtype=dtype, device="cuda")
+    t = torch.as_strided(store, (rows, n), (stride, 1), offset)
+    t.copy_(a)
+    return t
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def eight(rows, n, scale_rows=None, extra=0):
+    """8-bit buffers filled with marks, so that what is written past a row's end shows."""
+    q = torch.full((rows, up(n, 16) + extra), 0x55, dtype=torch.uint8, device="cuda")
+    s = torch.full((scale_rows or rows, up(-(-n // 128), 4)), 0x55, dtype=torch.uint8, device="cuda")
+    return q[:, :n], s[:, : -(-n // 128)]
+
+
+def check_marks(q, s):
+    n, nb = q.shape[1], s.shape[1]
+    assert bool((q._base[:, n:] == 0x55).all()) and bool((s._base[:, nb:] == 0x55).all())
+
+
+def check_eight(q, s, y, rel, rows_per_scale=1):
+    """q, s stand for y (float64) as the format says, y being known to `rel`."""
+    q, s = q.cpu().numpy(), s.cpu().numpy()
+    for i in range(s.shape[0]):
+        for j in range(s.shape[1]):
+            at = slice(i * rows_per_scale, (i + 1) * rows_per_scale), slice(j * 128, (j + 1) * 128)
+            block = y[at]
+            if not np.isfinite(block).all():
+                assert s[i, j] == 255 and (q[at] == 0x7F).all()
+                continue
+            top, unit = np.abs(block).max(), 2.0 ** (float(s[i, j]) - 127)
+            assert top <= 448 * unit * (1 + rel)
+            assert s[i, j] == 0 or top > 224 * unit * (1 - rel)
+            off = np.abs(L.E4M3[q[at]] * unit - block)
+            assert (off <= np.maximum(2.0 ** -4 * np.abs(block), 2.0 ** -10 * unit) + rel * np.abs(block)).all()
+
+
+# ---- norm -----------------------------------------------------------------------------------------------------------------
+
+NORM = [(1, 1), (3, 7), (2, 64), (5, 127), (4, 128), (3, 129), (9, 512), (6, 1000), (5, 1024), (2, 1025), (7, 2048), (3, 2500), (1, 4096),
+        (600, 4096), (2, 5120), (520, 5125), (2, 8192), (515, 9000), (3, 12000), (514, 16384), (2, 20001), (1, 40000), (2, 65536)]
+
+
+@pytest.mark.parametrize("rows,n", NORM)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rms_norm(rows, n, dtype):
+    g = rng(rows, n)
+    dt = DT[dtype]
+    x = on_gpu(g.normal(size=(rows, n)) * g.choice([0.01, 1.0, 30.0], size=(rows, 1)), dt)
+    r = on_gpu(g.normal(size=(rows, n)), dt, stride=n + 3, offset=5)
+    w = on_gpu(1 + 0.1 * g.normal(size=(1, n)), dt)[0]
+    total, out = (on_gpu(np.zeros((rows, n)), dt, stride=n + s) for s in (0, 8))
+    q, s = eight(rows, n)
+    B.a2sf_rms_norm(x, w, 1e-5, residual=r, total=total, out=out, q=q, scales=s)
+    few = slice(0, rows, max(1, rows // 8))
+    h, y = L.rms_norm(host(x[few]), host(r[few]), host(w), 1e-5)
+    half = BF16 if dtype == "bf16" else 0.0
+    assert (np.abs(host(total[few]) - h) <= (half + 2.0 ** -24) * np.abs(h)).all()
+    # a sum that nearly cancels keeps the error of its rounding, relative to the terms
+    slack = 3e-6 * np.abs(y) + 2.0 ** -24 * np.abs(y / np.where(h == 0, 1, h)) * (np.abs(host(x[few])) + np.abs(host(r[few])))
+    assert (np.abs(host(out[few]) - y) <= half * np.abs(y) + slack).all()
+    check_eight(q[few], s[few], y, 5e-6 if dtype == "f32" else 5e-6)
+    check_marks(q, s)
+    # the same without the residual, 8 bits alone, and again: the same bits
+    q2, s2 = eight(rows, n)
+    B.a2sf_rms_norm(x, w, 1e-5, q=q2, scales=s2)
+    check_eight(q2[few], s2[few], L.rms_norm(host(x[few]), None, host(w), 1e-5)[1], 5e-6)
+    q3, s3 = eight(rows, n)
+    B.a2sf_rms_norm(x, w, 1e-5, q=q3, scales=s3)
+    assert torch.equal(q2, q3) and torch.equal(s2, s3)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rms_norm_in_place(dtype):
+    g = rng(1)
+    x, r = (g.normal(size=(70, 777)) for _ in range(2))
+    w = on_gpu(g.normal(size=(1, 777)), DT[dtype])[0]
+    tx, tr = on_gpu(x, DT[dtype]), on_gpu(r, DT[dtype])
+    total, out = torch.empty_like(tx), torch.empty_like(tx)
+    B.a2sf_rms_norm(tx, w, 1e-6, residual=tr, total=total, out=out)
+    B.a2sf_rms_norm(tx, w, 1e-6, residual=tr, total=tr, out=tx)
+    assert torch.equal(tr, total) and torch.equal(tx, out)
+
+
+def test_rms_norm_rows_that_are_not_numbers():
+    x = torch.randn(6, 300, device="cuda")
+    x[1, 5], x[2, 299] = math.nan, math.inf
+    x[3] = 0.0
+    x[4] = 1e-30  # squares vanish beside eps
+    w = torch.ones(300, device="cuda")
+    out = torch.empty_like(x)
+    q, s = eight(6, 300)
+    B.a2sf_rms_norm(x, w, 1e-5, out=out, q=q, scales=s)
+    assert bool(torch.isnan(out[1]).all()) and bool((s[1] == 255).all()) and bool((q[1] == 0x7F).all())
+    assert bool(torch.isnan(out[2, 299])) and bool((out[2, :299] == 0).all())     # divided by infinity
+    assert s[2].tolist() == [0, 0, 255]
+    assert bool((out[3] == 0).all()) and s[3].tolist() == [0, 0, 0] and bool((q[3] == 0).all())
+    _, y = L.rms_norm(host(x[4:]), None, np.ones(300), 1e-5)
+    check_eight(q[4:], s[4:], y, 5e-6)
+    check_marks(q, s)
+
+
+# ---- rows to 8 bits ---------------------------------------------------------------------------------------------------------
+
+QUANT = [(1, 1), (1, 15), (3, 128), (2, 130), (17, 257), (5, 1001), (64, 4096), (3, 11008), (2, 70001)]
+
+
+@pytest.mark.parametrize("rows,n", QUANT)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quantize_is_exact(rows, n, dtype):
+    g = rng(2, rows, n)
+    v = g.normal(size=(rows, n)) * 2.0 ** g.integers(-12, 12, size=(rows, n))
+    v[:, :: 37] = 0.0
+    x = on_gpu(v, DT[dtype], stride=n + 1, offset=3)
+    q, s = eight(rows, n, extra=16)
+    B.a2sf_quantize(x, q, s)
+    wq, ws = L.quantize(host(x))
+    assert np.array_equal(s.cpu().numpy(), ws) and np.array_equal(q.cpu().numpy(), wq)
+    check_marks(q, s)
+
+
+def test_quantize_at_the_edges_of_the_scale():
+    """Blocks whose largest value is 448 times a power of two, or a little more; ties; values too small to be seen; ends of the range."""
+    v = np.zeros((7, 128))
+    v[0, :4] = 448.0, -1.0, 18.0, 19.0          # 18, 19: steps of 2; 19 and 17 are ties
+    v[1, :4] = 448.1, 17.0, 1.0, 2.0 ** -9
+    v[2, :4] = 1e-45, 3e-45, -1e-45, 0.0        # subnormal numbers
+    v[3, :4] = 3.3e38, 1.0, -3.3e38, 1e30
+    v[4, :4] = 448.0, 2.0 ** -10, 1.5 * 2.0 ** -9, 2.0 ** -9
+    v[5, 0], v[5, 1] = math.inf, 1.0
+    v[6, 100] = math.nan
+    x = torch.from_numpy(v).float().cuda()
+    q, s = eight(7, 128)
+    B.a2sf_quantize(x, q, s)
+    wq, ws = L.quantize(host(x))
+    assert s[:, 0].tolist() == ws[:, 0].tolist() and np.array_equal(q.cpu().numpy(), wq)
+
+
+@pytest.mark.parametrize("rows,n", QUANT)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gated_rows(rows, n, dtype):
+    g = rng(3, rows, n)
+    both = on_gpu(g.normal(size=(rows, 2 * n)) * 4, DT[dtype])   # gate and up: two halves of one product
+    gate, x = both[:, :n], both[:, n:]
+    out = on_gpu(np.zeros((rows, n)), DT[dtype], stride=n + 5)
+    q, s = eight(rows, n)
+    B.a2sf_quantize(x, q, s, gate=gate, out=out)
+    y = L.gated(host(x), host(gate))
+    half = BF16 if dtype == "bf16" else 0.0
+    assert (np.abs(host(out) - y) <= (half + 6e-6) * np.abs(y)).all()
+    check_eight(q, s, y, 6e-6)
+    check_marks(q, s)
+    only = torch.empty(rows, n, dtype=DT[dtype], device="cuda")
+    B.a2sf_quantize(x, None, None, gate=gate, out=only)
+    assert torch.equal(only, out)
+
+
+def test_gate_far_from_zero():
+    g = torch.tensor([[-1e4, -200.0, -88.0, 88.0, 200.0, 1e4, 0.0, -0.0]], device="cuda")
+    out = torch.empty_like(g)
+    B.a2sf_quantize(torch.ones_like(g), None, None, gate=g, out=out)
+    assert np.allclose(host(out), L.gated(np.ones((1, 8)), host(g)), rtol=1e-5, atol=1e-30)
+
+
+@pytest.mark.parametrize("n,k", [(1, 1), (128, 128), (129, 127), (300, 513), (77, 4100)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quantize_weight_is_exact(n, k, dtype):
+    g = rng(4, n, k)
+    w = on_gpu(g.normal(size=(n, k)) * 2.0 ** g.integers(-8, 3, size=(n, 1)), DT[dtype], stride=k + 2)
+    q, s = eight(n, k, scale_rows=-(-n // 128))
+    B.a2sf_quantize_weight(w, q, s)
+    wq, ws = L.quantize(host(w), 128)
+    assert np.array_equal(s.cpu().numpy(), ws) and np.array_equal(q.cpu().numpy(), wq)
+    check_marks(q, s)
+
+
+# ---- products ---------------------------------------------------------------------------------------------------------------
+
+def filled(rows, cols, codes, scales, pad):
+    """8-bit rows of these bytes; the bytes behind them are NaN."""
+    q = torch.full((rows, up(cols, 16) + pad), 0x7F, dtype=torch.uint8, device="cuda")
+    q[:, :cols] = torch.from_numpy(codes).cuda()
+    s = torch.full((scales.shape[0], up(scales.shape[1], 4)), 0xFF, dtype=torch.uint8, device="cuda")
+    s[:, : scales.shape[1]] = torch.from_numpy(scales).cuda()
+    return q[:, :cols], s[:, : scales.shape[1]]
+
+
+def operands(g, m, n, k, whole):
+    """Bytes and scales of A and B.  whole: small whole numbers and scales that leave every sum exact in 32 bits."""
+    nb = -(-k // 128)
+    if whole:
+        codes = np.array([L.to_e4m3(np.array([float(v)]))[0] for v in range(-4, 5)], np.uint8)
+        draw = lambda r: codes[g.integers(0, 9, size=(r, k))]
+        scale = lambda r: g.integers(126, 129, size=(r, nb)).astype(np.uint8)
+    else:
+        def draw(r):
+            c = g.integers(0, 256, size=(r, k)).astype(np.uint8)
+            c[(c & 0x7F) == 0x7F] = 0
+            return c
+        scale = lambda r: g.integers(112, 132, size=(r, nb)).astype(np.uint8)
+    return (draw(m), scale(m)), (draw(n), scale(-(-n // 128)))
+
+
+MATMUL = [(1, 1, 1), (1, 16, 128), (1, 257, 384), (1, 4096, 1024), (2, 100, 15), (3, 65, 200), (5, 1000, 1000), (16, 129, 129), (17, 31, 4096),
+          (31, 500, 640), (33, 64, 16), (48, 4100, 512), (64, 256, 2048), (65, 640, 130), (96, 33, 5000), (100, 2000, 300), (127, 127, 127),
+          (128, 128, 128), (129, 257, 256), (200, 1030, 900), (256, 512, 2304), (257, 300, 384), (300, 3001, 129), (512, 768, 1024),
+          (700, 513, 77), (1000, 1111, 640), (2049, 130, 260), (4100, 300, 96), (2100, 5000, 384)]
+
+
+@pytest.mark.parametrize("m,n,k", MATMUL)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("workspace", [True, False])
+def test_matmul_of_whole_numbers_is_exact(m, n, k, dtype, workspace):
+    g = rng(5, m, n, k)
+    (a, sa), (b, sb) = operands(g, m, n, k, True)
+    ta, tsa = filled(m, k, a, sa, 0)
+    tb, tsb = filled(n, k, b, sb, 32)
+    c = on_gpu(np.zeros((m, n)), DT[dtype], stride=n + 3, offset=1)
+    c._base.fill_(99.0)
+    ws = torch.full((B.a2sf_matmul_workspace_bytes(m, n, k),), 0xFF, dtype=torch.uint8, device="cuda") if workspace else None
+    B.a2sf_matmul_scaled(ta, tsa, tb, tsb, c, workspace=ws)
+    # sums of quarters below 2^22: exact in 64 bits as in 32
+    want = torch.from_numpy(L.values(a, sa)).cuda() @ torch.from_numpy(L.values(b, sb, 128)).cuda().t()
+    assert float(want.abs().max()) < 2 ** 21
+    assert torch.equal(c, want.to(DT[dtype])), (c.double() - want).abs().max()
+    assert bool((torch.as_strided(c._base, (m, 3), (n + 3, 1), 1 + n) == 99).all()) and float(c._base[0]) == 99
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 300, 1000), (7, 777, 4096), (40, 200, 333), (150, 700, 2000), (300, 300, 8000), (1030, 600, 500)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_matmul(m, n, k, dtype):
+    g = rng(6, m, n, k)
+    (a, sa), (b, sb) = operands(g, m, n, k, False)
+    ta, tsa = filled(m, k, a, sa, 16)
+    tb, tsb = filled(n, k, b, sb, 0)
+    c = torch.empty(m, n, dtype=DT[dtype], device="cuda")
+    ws = torch.empty(B.a2sf_matmul_workspace_bytes(m, n, k), dtype=torch.uint8, device="cuda")
+    B.a2sf_matmul_scaled(ta, tsa, tb, tsb, c, workspace=ws)
+    va, vb = torch.from_numpy(L.values(a, sa)).cuda(), torch.from_numpy(L.values(b, sb, 128)).cuda().t()
+    want = va @ vb
+    bound = (max(k, 16) * 2.0 ** -24 + (8 * 2.0 ** -13 if dtype == "bf16" else 0)) * (va.abs() @ vb.abs())
+    bound += BF16 * want.abs() if dtype == "bf16" else 0
+    assert bool(((c.double() - want).abs() <= bound).all())
+    again = torch.empty_like(c)
+    B.a2sf_matmul_scaled(ta, tsa, tb, tsb, again, workspace=ws)
+    assert torch.equal(c, again)
+
+
+@pytest.mark.parametrize("m", [1, 20, 200, 600])
+def test_matmul_scales_that_are_no_numbers_reach_their_rows_only(m):
+    g = rng(7, m)
+    n, k = 300, 640
+    (a, sa), (b, sb) = operands(g, m, n, k, True)
+    sa[m // 2, 2] = 255
+    a[m // 3, 100] = 0x7F
+    sb[1, 4] = 255
+    c = torch.empty(m, n, device="cuda")
+    B.a2sf_matmul_scaled(*filled(m, k, a, sa, 0), *filled(n, k, b, sb, 0), c)
+    want = np.zeros((m, n), bool)
+    want[[m // 2, m // 3]] = True
+    want[:, 128:256] = True
+    assert np.array_equal(torch.isnan(c).cpu().numpy(), want)
+
+
+def test_matmul_of_what_the_norm_and_the_weights_give():
+    g = rng(8)
+    m, n, k = 50, 384, 1000
+    x, w = on_gpu(g.normal(size=(m, k)), torch.bfloat16), on_gpu(g.normal(size=(n, k)) * 0.05, torch.bfloat16)
+    a, b = eight(m, k), eight(n, k, scale_rows=3)
+    B.a2sf_rms_norm(x, torch.ones(k, dtype=torch.bfloat16, device="cuda"), 1e-5, q=a[0], scales=a[1])
+    B.a2sf_quantize_weight(w, *b)
+    c = torch.empty(m, n, device="cuda")
+    B.a2sf_matmul_scaled(*a, *b, c)
+    y = L.rms_norm(host(x), None, np.ones(k), 1e-5)[1]
+    # a value keeps 2^-4 at worst, 2^-5.2 on the average of squares; a thousand independent errors
+    want = y @ host(w).T
+    assert np.linalg.norm(host(c) - want) < 0.05 * np.linalg.norm(want)
+
+
+# ---- rotary -------------------------------------------------------------------------------------------------------------------
+
+ROTARY = [(1, 1, 1, 1, 64, 64), (2, 1, 32, 8, 128, 128), (1, 7, 3, 1, 128, 32), (3, 5, 4, 2, 64, 24), (2, 9, 2, 1, 96, 96), (1, 300, 5, 5, 128, 128),
+          (4, 3, 40, 40, 128, 64), (2, 4, 2, 2, 10, 6), (1, 5, 1, 1, 7, 2), (1, 2, 2, 1, 512, 512), (2, 3, 3, 1, 511, 510), (70, 1, 2, 2, 64, 64)]
+
+
+@pytest.mark.parametrize("batch,length,heads,kv,d,rot", ROTARY)
+@pytest.mark.parametrize("neighbours", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rotary_splits_a_product(batch, length, heads, kv, d, rot, neighbours, dtype):
+    g = rng(9, batch, length, heads, d, rot)
+    dt = DT[dtype]
+    all_heads = heads + 2 * kv
+    x = on_gpu(g.normal(size=(batch * length, all_heads * d)), dt, stride=all_heads * d + 6)
+    x = x.unflatten(0, (batch, length)).unflatten(2, (all_heads, d))
+    pos = torch.from_numpy(g.integers(0, 500, size=(batch, length)).astype(np.int32)).cuda()
+    table = torch.empty(500, rot, device="cuda")
+    B.a2sf_rotary_table(table)
+    parts = x.split([heads, kv, kv], 2)
+    outs = [torch.full((batch, h, length, d), 3.0, dtype=dt, device="cuda") for h in (heads, kv, kv)]
+    call = [(p, o.transpose(1, 2), i < 2) for i, (p, o) in enumerate(zip(parts, outs))]
+    t = host(table)[pos.cpu().numpy()][:, :, None]
+    for inverse in (False, True):
+        B.a2sf_rotary(call, pos, table, interleaved=neighbours, inverse=inverse)
+        for i, (p, o) in enumerate(zip(parts, outs)):
+            v = host(p)
+            want = L.rotate(v, t[..., : rot // 2], t[..., rot // 2:], rot, neighbours, inverse) if i < 2 else v
+            # a pair's sum of two products: 3 u of the pair's size
+            a, b = (slice(0, rot, 2), slice(1, rot, 2)) if neighbours else (slice(0, rot // 2), slice(rot // 2, rot))
+            size = np.zeros(v.shape)
+            if i < 2:
+                size[..., a] = size[..., b] = np.abs(v[..., a]) + np.abs(v[..., b])
+            bound = 3 * 2.0 ** -24 * size + (BF16 * np.abs(want) if dtype == "bf16" else 0)
+            assert (np.abs(host(o.transpose(1, 2)) - want) <= bound).all()
+    # in place: the same bits
+    before = [o.clone() for o in outs]
+    y = x.clone()
+    ys = y.split([heads, kv, kv], 2)
+    B.a2sf_rotary([(p, p, i < 2) for i, p in enumerate(ys)], pos, table, interleaved=neighbours, inverse=True)
+    for p, o in zip(ys, before):
+        assert torch.equal(p, o.transpose(1, 2))
+
+
+def test_rotary_there_and_back():
+    x = torch.randn(2, 50, 3, 128, device="cuda")
+    pos = torch.arange(100, dtype=torch.int32, device="cuda").view(2, 50) * 1000
+    table = torch.empty(100000, 128, device="cuda")
+    B.a2sf_rotary_table(table)
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    B.a2sf_rotary([(x, y)], pos, table)
+    B.a2sf_rotary([(y, z)], pos, table, inverse=True)
+    # the table's cosine and sine are rounded: their squares add up to 1 within 2 u; the two turns add 6 u of a pair's size
+    assert float((z - x).abs().max()) <= 10 * 2.0 ** -24 * 2 * float(x.abs().max())
+
+
+def test_rotary_is_its_gradient_by_differences():
+    """d (g . turn(x)) / dx = turn back (g): the turn is linear, so the difference quotient is exact up to rounding."""
+    g = rng(10)
+    x, d = (torch.from_numpy(g.normal(size=(1, 6, 2, 64))).float().cuda() for _ in range(2))
+    up_ = torch.from_numpy(g.normal(size=(1, 6, 2, 64))).float().cuda()
+    pos = torch.arange(6, dtype=torch.int32, device="cuda")[None]
+    table = torch.empty(6, 64, device="cuda")
+    B.a2sf_rotary_table(table)
+    turn = lambda v, inverse=False: (lambda y: (B.a2sf_rotary([(v, y)], pos, table, inverse=inverse), y)[1])(torch.empty_like(v))
+    quotient = (up_.double() * (turn(x + d).double() - turn(x).double())).sum()
+    gradient = (turn(up_, True).double() * d.double()).sum()
+    scale = float((up_.abs().double() * (x.abs() + d.abs()).double()).sum())
+    assert abs(float(quotient - gradient)) <= 12 * 2.0 ** -24 * scale
+
+
+def test_rotary_positions_outside_the_table_are_not_numbers():
+    x = torch.randn(1, 4, 2, 64, device="cuda")
+    pos = torch.tensor([[0, 9, -1, 10]], dtype=torch.int32, device="cuda")
+    table = torch.empty(10, 32, device="cuda")
+    B.a2sf_rotary_table(table)
+    y, v = torch.empty_like(x), torch.empty_like(x)
+    B.a2sf_rotary([(x, y), (x, v, False)], pos, table)
+    bad = torch.isnan(y)
+    assert bool(bad[0, 2:, :, :32].all()) and not bool(bad[0, :2].any()) and torch.equal(y[..., 32:], x[..., 32:])
+    assert torch.equal(v, x)
+
+
+@pytest.mark.parametrize("args", [dict(), dict(base=500000.0, factor=8.0, original_length=8192, low=1.0, high=4.0),
+                                  dict(factor=4.0, magnitude=1.1386), dict(factor=2.0, original_length=2048, low=1.0, high=32.0)])
+def test_rotary_table(args):
+    table = torch.empty(200000, 96, device="cuda")
+    B.a2sf_rotary_table(table, **args)
+    at = np.array([0, 1, 2, 77, 4096, 65535, 131071, 199999])
+    m = args.get("magnitude", 1.0)
+    f = L.frequencies(96, args.get("base", 10000.0), args.get("factor", 1.0), args.get("original_length", 0), args.get("low", 0.0),
+                      args.get("high", 0.0))
+    angle = at[:, None] * f
+    got = host(table)[at]
+    # one rounding of values up to m; the angle in 64 bits is off by 2e5 * 2^-52 at most
+    assert np.abs(got - m * np.concatenate([np.cos(angle), np.sin(angle)], 1)).max() <= m * 2.0 ** -24 * 1.01
+
+
+# ---- sampling ------------------------------------------------------------------------------------------------------------------
+
+def draw_tokens(logits, noise, **filters):
+    rows, n = logits.shape
+    token = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+    prob = torch.full((rows,), -7.0, device="cuda")
+    on = {k: (None if v is None else torch.from_numpy(np.asarray(v)).cuda().to(torch.int32 if k == "top_k" else torch.float32))
+          for k, v in filters.items()}
+    B.a2sf_sample(logits, noise, token, prob=prob, **on)
+    return token.cpu().numpy(), prob.double().cpu().numpy()
+
+
+def check_tokens(logits, noise, **filters):
+    got = draw_tokens(logits, noise, **filters)
+    l, e = host(logits), host(noise) if noise is not None else None
+    for r in range(l.shape[0]):
+        one = {k: float(np.float32(v[r])) if k != "top_k" else int(v[r]) for k, v in filters.items() if v is not None}
+        token, prob = L.sample(l[r], e[r] if e is not None else None, **one)
+        assert got[0][r] == token, (r, one)
+        # the weights' exponents are off by 2 u of their size (under 150 octaves), the sum by its chains of additions
+        assert abs(got[1][r] - prob) <= 3e-5 * prob, (r, one)
+
+
+VOCABULARY = [1, 2, 63, 200, 1024, 5000, 8192, 8193, 20001, 32000, 50272, 65536, 70001, 128256]
+
+
+@pytest.mark.parametrize("n", VOCABULARY)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("filters", ["", "t", "k", "p", "m", "tkpm", "kp"])
+def test_sample(n, dtype, filters):
+    rows = 5
+    g = rng(11, n, len(filters))
+    l = 2 * g.normal(size=(rows, n)) + (g.random((rows, n)) < 30 / n) * (5 + 3 * g.random((rows, n)))
+    logits = on_gpu(l, DT[dtype], stride=n + 3, offset=1)
+    noise = on_gpu(g.exponential(size=(rows, n)) + 1e-9, torch.float32, stride=n + 1)
+    f = {}
+    if "t" in filters:
+        f["temperature"] = [0.3, 0.0, 1.0, 1.7, 0.01]
+    if "k" in filters:
+        f["top_k"] = [1, 40, 0, 100000, 700]
+    if "p" in filters:
+        f["top_p"] = [0.9, 0.5, 1.0, 0.0, 0.999]
+    if "m" in filters:
+        f["min_p"] = [0.05, 0.0, 2.0, 0.3, 1e-4]
+    check_tokens(logits, noise, **f)
+
+
+@pytest.mark.parametrize("n", [300, 5000, 70001])
+def test_sample_equal_logits_go_by_index(n):
+    """All tokens in one bin, more of them than are ranked at once, or a few values with many ties."""
+    g = rng(12, n)
+    flat = torch.zeros(4, n, device="cuda")
+    noise = on_gpu(g.exponential(size=(4, n)) + 1e-9, torch.float32)
+    check_tokens(flat, noise, top_k=[1, 7, n // 2, n - 1])
+    check_tokens(flat, noise, top_p=[0.1, 0.5, 0.9, 0.01])
+    steps = on_gpu(np.round(2 * g.normal(size=(4, n))) / 2, torch.bfloat16)
+    check_tokens(steps, noise, top_k=[3, 100, 150, n // 3], top_p=[0.5, 0.9, 1.0, 0.7], temperature=[1.0, 0.5, 2.0, 1.0])
+
+
+def test_sample_values_close_together():
+    """Thousands of different logits in one bin of the first histogram: it is split by their bits."""
+    g = rng(13)
+    logits = on_gpu(1.0 + g.random((3, 9000)) * 1e-3, torch.float32)
+    noise = on_gpu(g.exponential(size=(3, 9000)) + 1e-9, torch.float32)
+    check_tokens(logits, noise, top_k=[4000, 8999, 1500])
+    check_tokens(logits, noise, top_p=[0.3, 0.77, 0.5], top_k=[0, 5000, 2])
+
+
+def test_sample_infinities_and_nan():
+    inf, nan = math.inf, math.nan
+    rows = [[-inf, nan, -inf, nan], [inf, 1.0, inf, 2.0], [nan, -inf, 3.0, -inf], [-inf, 0.0, 1.0, nan], [nan, inf, nan, -1.0],
+            [-3e38, 3e38, 3e38, -3e38]]
+    logits = torch.tensor(rows, device="cuda")
+    noise = torch.tensor([[1.0, 2.0, 0.5, 3.0]] * 6, device="cuda")
+    for f in ({}, {"top_k": [3] * 6}, {"top_p": [0.99] * 6}, {"top_k": [3] * 6, "top_p": [0.5] * 6, "min_p": [0.2] * 6},
+              {"temperature": [0.0] * 6}, {"temperature": [1e-38] * 6}):
+        check_tokens(logits, noise, **f)
+    check_tokens(logits, None, top_k=[2] * 6)
+
+
+def test_sample_without_prob_and_with_numbers_that_are_zero():
+    logits = torch.zeros(1, 10, device="cuda")
+    noise = torch.ones(1, 10, device="cuda")
+    noise[0, 6] = 0.0
+    token = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.a2sf_sample(logits, noise, token)
+    assert token.tolist() == [6]
+
+
+def test_sample_frequencies():
+    """20 000 draws of one distribution: each token about as often as it is likely (five standard deviations)."""
+    g = rng(14)
+    n, draws = 37, 20000
+    l = g.normal(size=n)
+    logits = torch.from_numpy(np.repeat(l[None], draws, 0)).float().cuda()
+    noise = torch.empty(draws, n, device="cuda").exponential_(generator=torch.Generator("cuda").manual_seed(3))
+    token = torch.empty(draws, dtype=torch.int32, device="cuda")
+    B.a2sf_sample(logits, noise, token)
+    p = np.exp(l) / np.exp(l).sum()
+    share = np.bincount(token.cpu().numpy(), minlength=n) / draws
+    assert (np.abs(share - p) <= 5 * np.sqrt(p * (1 - p) / draws)).all()
+
+
+# ---- streams, graphs, host paths ---------------------------------------------------------------------------------------------
+
+def layer_calls(m=6, k=640, n=384):
+    """One of each call on small data; returns (function that makes them, the tensors they write)."""
+    g = rng(15)
+    x, w = on_gpu(g.normal(size=(m, k)), torch.bfloat16), on_gpu(1 + 0.1 * g.normal(size=(1, k)), torch.bfloat16)[0]
+    weight = on_gpu(g.normal(size=(n, k)) * 0.1, torch.bfloat16)
+    a, b, h = eight(m, k), eight(n, k, scale_rows=3), eight(m, n)
+    c = torch.zeros(m, n, dtype=torch.bfloat16, device="cuda")
+    table, pos = torch.empty(64, 64, device="cuda"), torch.arange(m, dtype=torch.int32, device="cuda")[None]
+    y = torch.zeros(1, 6, m, 64, dtype=torch.bfloat16, device="cuda")
+    logits = on_gpu(3 * g.normal(size=(m, 2000)), torch.float32)
+    noise = on_gpu(g.exponential(size=(m, 2000)) + 1e-9, torch.float32)
+    token, prob = torch.zeros(m, dtype=torch.int32, device="cuda"), torch.zeros(m, device="cuda")
+    p = torch.full((m,), 0.9, device="cuda")
+    B.a2sf_rotary_table(table)
+    B.a2sf_quantize_weight(weight, *b)
+    ws = torch.empty(max(1, B.a2sf_matmul_workspace_bytes(m, n, k)), dtype=torch.uint8, device="cuda")
+
+    def calls(stream=None):
+        B.a2sf_rms_norm(x, w, 1e-5, q=a[0], scales=a[1], stream=stream)
+        B.a2sf_matmul_scaled(*a, *b, c, workspace=ws, stream=stream)
+        B.a2sf_rotary([(c.view(1, m, 6, 64), y.transpose(1, 2))], pos, table, stream=stream)
+        B.a2sf_quantize(c, *h, gate=c, stream=stream)
+        B.a2sf_sample(logits, noise, token, top_p=p, prob=prob, stream=stream)
+
+    return calls, [*a, c, y, *h, token, prob]
+
+
+def test_calls_replay_from_a_hip_graph():
+    calls, outs = layer_calls()
+    calls()
+    torch.cuda.synchronize()
+    eager = [t.clone() for t in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(4):
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, e) for t, e in zip(outs, eager))
+
+
+def test_calls_on_another_stream_and_through_ctypes(monkeypatch):
+    calls, outs = layer_calls()
+    calls()
+    torch.cuda.synchronize()
+    eager = [t.clone() for t in outs]
+    side = torch.cuda.Stream()
+    for way in ("current", "named", "ctypes"):
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        if way == "current":
+            with torch.cuda.stream(side):
+                calls()
+        elif way == "named":
+            calls(side.cuda_stream)
+        else:
+            monkeypatch.setattr(B, "_call", B._NoExtension)
+            calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, e) for t, e in zip(outs, eager)), way

@@ -1,0 +1,182 @@
+"""Refusals of the operators around the attention: found on the host, before any launch."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2407_20485_amd import binding as B
+
+FAKE = 0x10000  # never dereferenced on these paths
+ref = ctypes.byref
+
+
+def rows(data=FAKE, stride=256):
+    return ref(B.Rows(data, stride))
+
+
+def rows8(data=FAKE, scales=FAKE, stride=256, scale_stride=4):
+    return ref(B.Rows8(data, scales, stride, scale_stride))
+
+
+def norm(x=None, residual=None, weight=FAKE, eps=1e-5, m=4, n=200, dtype=B.A2SF_BF16, total=None, out=None, out8=None):
+    return B.lib().a2sf_rms_norm(x or rows(), residual, weight, eps, m, n, dtype, total, out, out8, None)
+
+
+def test_rms_norm_refusals():
+    assert norm() == B.A2SF_EINVAL                                        # no output
+    assert norm(out=rows(None)) == B.A2SF_EINVAL
+    assert norm(out=rows(FAKE + 1)) == B.A2SF_EINVAL                      # not even an element's alignment
+    assert norm(x=rows(FAKE + 2), out=rows(), dtype=B.A2SF_F32) == B.A2SF_EINVAL
+    assert norm(out=rows(), dtype=7) == B.A2SF_EDTYPE
+    assert norm(out=rows(), n=0) == B.A2SF_ESHAPE
+    assert norm(out=rows(), m=0) == B.A2SF_ESHAPE
+    assert norm(out=rows(), n=B.A2SF_MAX_ROW + 1, m=1) == B.A2SF_ESHAPE
+    assert norm(out=rows(stride=199)) == B.A2SF_ESHAPE                    # rows overlap
+    assert norm(out=rows(), weight=None) == B.A2SF_EINVAL
+    assert norm(out=rows(), residual=rows(None)) == B.A2SF_EINVAL
+    for eps in (-1e-5, float("nan"), float("inf")):
+        assert norm(out=rows(), eps=eps) == B.A2SF_EINVAL
+    assert norm(out8=rows8(scales=None)) == B.A2SF_EINVAL
+    assert norm(out8=rows8(FAKE + 8)) == B.A2SF_EINVAL
+    assert norm(out8=rows8(stride=200)) == B.A2SF_ESHAPE                  # 8-bit rows start at multiples of 16
+    assert norm(out8=rows8(scale_stride=2)) == B.A2SF_ESHAPE
+    assert norm(out8=rows8(scale_stride=1)) == B.A2SF_ESHAPE
+
+
+def test_quantize_refusals():
+    f = B.lib().a2sf_quantize
+    assert f(rows(), None, 4, 200, B.A2SF_BF16, None, None, None) == B.A2SF_EINVAL
+    assert f(None, None, 4, 200, B.A2SF_BF16, None, rows8(), None) == B.A2SF_EINVAL
+    assert f(rows(), rows(stride=10), 4, 200, B.A2SF_BF16, None, rows8(), None) == B.A2SF_ESHAPE
+    assert f(rows(), None, 4, 200, 2, None, rows8(), None) == B.A2SF_EDTYPE
+    assert f(rows(), None, 2 ** 31 - 1, 200, B.A2SF_BF16, None, rows8(), None) == B.A2SF_ESHAPE
+    w = B.lib().a2sf_quantize_weight
+    assert w(rows(), 4, 200, B.A2SF_BF16, None, None) == B.A2SF_EINVAL
+    assert w(rows(), 0, 200, B.A2SF_BF16, rows8(), None) == B.A2SF_ESHAPE
+    assert w(rows(), 200, 200, B.A2SF_BF16, rows8(scale_stride=3), None) == B.A2SF_ESHAPE
+
+
+def test_matmul_refusals():
+    def f(a=None, b=None, c=None, m=4, n=200, k=200, dtype=B.A2SF_BF16, ws=None, nbytes=0):
+        return B.lib().a2sf_matmul_scaled(a or rows8(), b or rows8(), m, n, k, c or rows(), dtype, ws, nbytes, None)
+
+    assert f(a=rows8(None)) == B.A2SF_EINVAL
+    assert f(b=rows8(FAKE + 4)) == B.A2SF_EINVAL
+    assert f(a=rows8(scales=FAKE + 1)) == B.A2SF_EINVAL
+    assert f(a=rows8(stride=200)) == B.A2SF_ESHAPE
+    assert f(b=rows8(stride=208), k=209) == B.A2SF_ESHAPE
+    assert f(c=rows(stride=199)) == B.A2SF_ESHAPE
+    assert f(c=rows(FAKE + 1)) == B.A2SF_EINVAL
+    assert f(k=0) == B.A2SF_ESHAPE
+    assert f(m=0) == B.A2SF_ESHAPE
+    assert f(dtype=9) == B.A2SF_EDTYPE
+    assert f(k=(1 << 20) + 1, a=rows8(stride=1 << 21), b=rows8(stride=1 << 21)) == B.A2SF_ESHAPE
+    assert f(a=rows8(stride=1 << 24)) == B.A2SF_ESHAPE
+    assert f(ws=FAKE + 8, nbytes=1 << 20) == B.A2SF_EWORKSPACE
+    assert B.a2sf_matmul_workspace_bytes(0, 5, 5) == 0
+    assert B.a2sf_matmul_workspace_bytes(8192, 8192, 4096) == 0          # tiles enough
+    assert B.a2sf_matmul_workspace_bytes(64, 4096, 16384) <= 32 << 20
+
+
+def part(x=FAKE, y=FAKE + 4096, xs=(4096, 512, 64), ys=(4096, 512, 64), heads=8, rotate=1):
+    return B.RotaryPart(x, y, (ctypes.c_int64 * 3)(*xs), (ctypes.c_int64 * 3)(*ys), heads, rotate)
+
+
+def test_rotary_refusals():
+    def f(*parts, n=None, batch=2, length=8, d=64, dtype=B.A2SF_BF16, pos=FAKE, pos_stride=8, table=FAKE, table_rows=32, rot=64, pairs=0):
+        made = (B.RotaryPart * max(1, len(parts)))(*parts)
+        return B.lib().a2sf_rotary(made, len(parts) if n is None else n, batch, length, d, dtype, pos, pos_stride, table,
+                                   table_rows, rot, pairs, 0, None)
+
+    assert f() == B.A2SF_EINVAL
+    assert f(part(), n=5) == B.A2SF_EINVAL
+    assert f(part(), dtype=3) == B.A2SF_EDTYPE
+    assert f(part(), pairs=2) == B.A2SF_EINVAL
+    assert f(part(), rot=63) == B.A2SF_ESHAPE
+    assert f(part(), rot=66) == B.A2SF_ESHAPE
+    assert f(part(), d=513) == B.A2SF_ESHAPE
+    assert f(part(), pos=None) == B.A2SF_EINVAL
+    assert f(part(), pos_stride=7) == B.A2SF_ESHAPE
+    assert f(part(), table_rows=0) == B.A2SF_ESHAPE
+    assert f(part(heads=0)) == B.A2SF_ESHAPE
+    assert f(part(x=FAKE + 1)) == B.A2SF_EINVAL
+    assert f(part(xs=(4096, -512, 64))) == B.A2SF_ESHAPE
+    assert f(part(y=FAKE, ys=(4096, 64, 512))) == B.A2SF_EINVAL           # in place with another layout
+    t = B.lib().a2sf_rotary_table
+    assert t(None, 8, 64, 1e4, 1.0, 0, 0.0, 0.0, 1.0, None) == B.A2SF_EINVAL
+    assert t(FAKE, 8, 63, 1e4, 1.0, 0, 0.0, 0.0, 1.0, None) == B.A2SF_ESHAPE
+    assert t(FAKE, 8, 64, 0.0, 1.0, 0, 0.0, 0.0, 1.0, None) == B.A2SF_EINVAL
+    assert t(FAKE, 8, 64, 1e4, 0.0, 0, 0.0, 0.0, 1.0, None) == B.A2SF_EINVAL
+    assert t(FAKE, 8, 64, 1e4, 2.0, 100, 4.0, 1.0, 1.0, None) == B.A2SF_EINVAL
+    assert t(FAKE, 8, 64, 1e4, 2.0, -1, 1.0, 4.0, 1.0, None) == B.A2SF_EINVAL
+
+
+def test_sample_refusals():
+    def f(logits=None, noise=None, m=4, n=200, dtype=B.A2SF_F32, token=FAKE, temperature=None, prob=None):
+        return B.lib().a2sf_sample(logits or rows(), noise, m, n, dtype, temperature, None, None, None, token, prob, None)
+
+    assert f(token=None) == B.A2SF_EINVAL
+    assert f(token=FAKE + 2) == B.A2SF_EINVAL
+    assert f(prob=FAKE + 2) == B.A2SF_EINVAL
+    assert f(temperature=FAKE + 1) == B.A2SF_EINVAL
+    assert f(noise=rows(FAKE + 2)) == B.A2SF_EINVAL
+    assert f(noise=rows(stride=100)) == B.A2SF_ESHAPE
+    assert f(logits=rows(FAKE + 2)) == B.A2SF_EINVAL
+    assert f(n=0) == B.A2SF_ESHAPE
+    assert f(m=1, n=B.A2SF_MAX_VOCABULARY + 1) == B.A2SF_ESHAPE
+    assert f(dtype=4) == B.A2SF_EDTYPE
+
+
+def test_python_calls_refuse_what_does_not_fit_together():
+    """Tensors on the host: the extension leaves them to the ctypes form, which names the error before anything is called."""
+    x = torch.zeros(4, 200, dtype=torch.bfloat16)
+    q, s = torch.zeros(4, 208, dtype=torch.float8_e4m3fn)[:, :200], torch.zeros(4, 4, dtype=torch.uint8)[:, :2]
+
+    def status(call):
+        with pytest.raises(B.A2SFError) as e:
+            call()
+        return e.value.status
+
+    w = torch.ones(200, dtype=torch.bfloat16)
+    assert status(lambda: B.a2sf_rms_norm(x, w[:100], 1e-5, q=q, scales=s)) == B.A2SF_ESHAPE
+    assert status(lambda: B.a2sf_rms_norm(x, w.float(), 1e-5, q=q, scales=s)) == B.A2SF_EDTYPE
+    assert status(lambda: B.a2sf_rms_norm(x, w, 1e-5, residual=x[:3], q=q, scales=s)) == B.A2SF_ESHAPE
+    assert status(lambda: B.a2sf_rms_norm(x, w, 1e-5, q=q)) == B.A2SF_EINVAL
+    assert status(lambda: B.a2sf_rms_norm(x, w, 1e-5)) == B.A2SF_EINVAL
+    assert status(lambda: B.a2sf_rms_norm(x.t(), w[:4], 1e-5, out=x.t())) == B.A2SF_ESHAPE
+    assert status(lambda: B.a2sf_rms_norm(x.half(), w.half(), 1e-5, out=x.half())) == B.A2SF_EDTYPE
+    assert status(lambda: B.a2sf_quantize(x, q, s[:, :1])) == B.A2SF_ESHAPE
+    assert status(lambda: B.a2sf_quantize(x, q.view(torch.float8_e5m2), s)) == B.A2SF_EDTYPE
+    assert status(lambda: B.a2sf_quantize(x, q, s, gate=x.float())) == B.A2SF_EDTYPE
+    b, bs = torch.zeros(9, 208, dtype=torch.uint8)[:, :200], torch.zeros(1, 4, dtype=torch.uint8)[:, :2]
+    assert status(lambda: B.a2sf_matmul_scaled(q, s, b, bs, torch.zeros(4, 8))) == B.A2SF_ESHAPE
+    assert status(lambda: B.a2sf_matmul_scaled(q, s, b[:, :150], bs, torch.zeros(4, 9))) == B.A2SF_ESHAPE
+    assert status(lambda: B.a2sf_matmul_scaled(q, s, b, bs, torch.zeros(4, 9).half())) == B.A2SF_EDTYPE
+    h, pos, table = torch.zeros(2, 3, 4, 64), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(9, 64)
+    assert status(lambda: B.a2sf_rotary([], pos, table)) == B.A2SF_EINVAL
+    assert status(lambda: B.a2sf_rotary([(h, h[:1])], pos, table)) == B.A2SF_ESHAPE
+    assert status(lambda: B.a2sf_rotary([(h, h)], pos[:1], table)) == B.A2SF_ESHAPE
+    assert status(lambda: B.a2sf_rotary([(h, h)], pos.long(), table)) == B.A2SF_EDTYPE
+    assert status(lambda: B.a2sf_rotary([(h, h.bfloat16())], pos, table)) == B.A2SF_EDTYPE
+    assert status(lambda: B.a2sf_rotary([(h, h)], pos, torch.zeros(9, 66))) == B.A2SF_ESHAPE
+    logits, token = torch.zeros(4, 50), torch.zeros(4, dtype=torch.int32)
+    assert status(lambda: B.a2sf_sample(logits, logits[:, :49], token)) == B.A2SF_ESHAPE
+    assert status(lambda: B.a2sf_sample(logits, logits.bfloat16(), token)) == B.A2SF_EDTYPE
+    assert status(lambda: B.a2sf_sample(logits, logits, token.long())) == B.A2SF_EDTYPE
+    assert status(lambda: B.a2sf_sample(logits, logits, token, top_k=torch.ones(4))) == B.A2SF_EDTYPE
+    assert status(lambda: B.a2sf_sample(logits, logits, token[:3])) == B.A2SF_ESHAPE
+
+
+def test_extension_leaves_unusual_arguments_to_ctypes():
+    B.lib()
+    x = torch.zeros(4, 200)
+    t = torch.zeros(4, dtype=torch.int32)
+    assert B._call.rms_norm(B._entry("a2sf_rms_norm"), x, x[0], 1e-5, None, None, x, None, None, None) == -1  # not on a GPU
+    assert B._call.rms_norm(B._entry("a2sf_rms_norm"), x, x[0], 1, None, None, x, None, None, None) == -1     # eps no float
+    assert B._call.sample(B._entry("a2sf_sample"), x, None, t, None, None, None, None, None, 5) == -1
+    assert B._call.rotary(B._entry("a2sf_rotary"), ((x, x),), t, x, False, False, None) == -1                 # no list
+    assert B._call.rotary(B._entry("a2sf_rotary"), [(x, x)], t, x, False, False, None) == -1
+    assert B._call.quantize(B._entry("a2sf_quantize"), 5, None, None, None, None, None) == -1
+    assert B._call.matmul_scaled(B._entry("a2sf_matmul_scaled"), x, x, x, x, x, None, None, None) == -1
+    with pytest.raises(TypeError):
+        B._call.sample(x)
