@@ -4,11 +4,21 @@
 // independent exponential clocks to ring is each with the probability of its rate).
 //
 // Every filter keeps a prefix of the order "larger logit first, equal ones by index", so what they leave is described by its
-// last token: a cut (logit, index).  It is found without sorting: a histogram of how far the logits lie below the largest
-// says in which bin the cut falls, and only that bin's tokens are ranked against each other.
+// last token: a cut (logit, index).  It is found without sorting, in a list of candidates that is certain to hold it:
+//  * top_k <= 512: the largest logit of each of 64, 256 or 512 groups of lanes is looked at; the smallest of these has so many
+//    tokens at or above it, and only a few times as many on the average: these are the list;
+//  * else: a rough histogram of the row (32 bins per octave of probability) says between which bins the cut lies; what lies above
+//    them is counted exactly, what lies in them is the list.
+// In the list a histogram finds the bin of the cut and the tokens of that bin are ranked against each other.  A list that
+// overflows or misses the cut (rows of few different values) is replaced by the row itself, whose bins are split until one
+// can be ranked, or holds one value only.
 //
-// Masses are whole numbers of 2^-40 of the largest token's weight in 64 bits: their sums do not depend on the order in which
-// the lanes add, so the same inputs give the same cut, and a bin's mass is exactly the sum of its tokens'.
+// Masses are whole numbers of 2^-31 of the largest token's weight, summed in 64 bits: their sums do not depend on the order in which
+// the lanes add, so the same inputs give the same cut, whichever way it was found.
+//
+// A workgroup of 1024 lanes takes a row.  Few rows are a chain of passes and barriers whose instructions are mostly fetched for the first
+// time: what counts is little code, so passes are loops that read the row again (from the caches) instead of unrolled ones over
+// registers (32 000 logits in fp32: 17 us, 24 with the row in registers), and one function serves counts and masses.
 #include "a2sf_internal.h"
 #include "rows_dev.h"
 
@@ -17,216 +27,288 @@ namespace {
 
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleWaves = kSampleThreads / 64;
-constexpr int kBins = 2 * kSampleThreads;
-constexpr int kList = kSampleThreads;  // tokens ranked against each other at once
-constexpr float kBinsPerOctave = 64.f;
-constexpr float kMassOne = 1099511627776.f;  // 2^40
+constexpr int kBins = kSampleThreads;
+constexpr int kRanked = kSampleThreads;  // tokens ranked against each other at once
+constexpr int kListed = 512;             // tokens that a wave lists
+constexpr float kBinsPerOctave = 32.f;
 constexpr float kInf = __builtin_huge_valf();
 
 struct SampleShared {
   unsigned long long mass[kBins];
   uint32_t count[kBins];
-  uint32_t list_key[kList];
-  int list_index[kList];
-  unsigned long long wave64[kSampleWaves];
+  float list[kSampleWaves][kListed];
+  int list_index[kSampleWaves][kListed];
+  float rank[kRanked];
+  int rank_index[kRanked];
+  uint32_t rank_mass[kRanked];
+  unsigned long long wave64[kSampleWaves], wave64b[kSampleWaves];
   uint32_t wave32[kSampleWaves], wave32b[kSampleWaves];
-  float wavef[kSampleWaves];
+  float wavef[kSampleWaves], wavef2[kSampleWaves];
   // what the scan found
-  unsigned long long before_mass, total_mass, kept_mass;
-  uint32_t before_count, in_bin, listed;
-  int bin;
-  uint32_t cut_key;
+  unsigned long long before_mass, kept_mass;
+  uint32_t before_count, in_bin, ranked;
+  int bin, overflow;
+  float cut;
   int cut_index;
 };
+constexpr int kSampleLds = (int)sizeof(SampleShared);
 
-__device__ __forceinline__ unsigned long long shfl_up64(unsigned long long v, int by) {
-  const uint32_t lo = __shfl_up((uint32_t)v, by), hi = __shfl_up((uint32_t)(v >> 32), by);
-  return ((unsigned long long)hi << 32) | lo;
+// Sums of this lane and all before it in the wave: shifts inside rows of 16, then the rows' totals.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_zero(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
 }
-__device__ __forceinline__ unsigned long long wave_max64(unsigned long long v) {
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void scan_step(uint32_t& c, unsigned long long& m) {
+  const uint32_t lo = dpp_or_zero<CTRL, ROWS>((uint32_t)m), hi = dpp_or_zero<CTRL, ROWS>((uint32_t)(m >> 32));
+  c += dpp_or_zero<CTRL, ROWS>(c);
+  m += ((unsigned long long)hi << 32) | lo;
+}
+__device__ __forceinline__ void wave_scan(uint32_t& c, unsigned long long& m) {
+  scan_step<0x111, 0xF>(c, m);  // row_shr 1, 2, 4, 8
+  scan_step<0x112, 0xF>(c, m);
+  scan_step<0x114, 0xF>(c, m);
+  scan_step<0x118, 0xF>(c, m);
+  scan_step<0x142, 0xA>(c, m);  // the last lane of a row to the row after it
+  scan_step<0x143, 0xC>(c, m);  // the last lane of the lower half to the upper
+}
+
+// Eight logits as they are in memory; -infinity past the end of the row.  A NaN comes as it is: maxima pass it over and it is
+// not >= anything.
+template <typename T> struct RawUnit;
+template <> struct RawUnit<float> {
+  float v[kUnit];
+  __device__ __forceinline__ void load(const float* p, int have) {
+    if (have >= kUnit) load_unit(p, v);
+    else
 #pragma unroll
-  for (int by = 1; by < 64; by *= 2) {
-    const uint32_t lo = __shfl_xor((uint32_t)v, by), hi = __shfl_xor((uint32_t)(v >> 32), by);
-    const unsigned long long o = ((unsigned long long)hi << 32) | lo;
-    v = o > v ? o : v;
+      for (int j = 0; j < kUnit; ++j) v[j] = j < have ? p[j] : -kInf;
   }
-  return v;
-}
-
-// One row of logits as a workgroup sees it: in registers (V units of eight per lane; unit i * threads + t), or read again for
-// every pass where a row is longer than the registers are (V = 0).
-template <typename T, int V>
+  __device__ __forceinline__ float at(int j) const { return v[j]; }
+};
+template <> struct RawUnit<bf16_t> {
+  u32x4_t v;
+  __device__ __forceinline__ void load(const bf16_t* p, int have) {
+    if (have >= kUnit) v = *(const u32x4_at2_t*)p;
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = 2 * j < have ? p[2 * j] : 0xFF80u, hi = 2 * j + 1 < have ? p[2 * j + 1] : 0xFF80u;
+        v[j] = lo | hi << 16;
+      }
+  }
+  __device__ __forceinline__ float at(int j) const {
+    return __uint_as_float(j & 1 ? v[j / 2] & 0xFFFF0000u : v[j / 2] << 16);
+  }
+};
+// A row of logits.  TOP_IS_INF: the largest is +infinity; then such tokens count as 0 and all others as -infinity.
+template <typename T, bool TOP_IS_INF>
 struct Row {
   const T* p;
   int n;
-  float at[V > 0 ? V : 1][kUnit];
-
-  static __device__ __forceinline__ float clean(float l) { return l != l ? -kInf : l; }  // a NaN is never taken
-  __device__ __forceinline__ void load() {
-    if constexpr (V > 0) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int first = (i * kSampleThreads + (int)threadIdx.x) * kUnit;
-        load_unit(p + first, n - first, at[i]);
-#pragma unroll
-        for (int j = 0; j < kUnit; ++j) at[i][j] = first + j < n ? clean(at[i][j]) : -kInf;
-      }
+  static __device__ __forceinline__ float logit(float l) { return TOP_IS_INF ? (l == kInf ? 0.f : -kInf) : l; }
+  // f(unit, index of its first element) for this lane's units, the next one on its way; whole waves go through the same ones
+  template <typename F>
+  __device__ __forceinline__ void each_unit(F f) const {
+    int first = (int)threadIdx.x * kUnit;
+    RawUnit<T> u;
+    u.load(p + first, n - first);
+    for (;;) {
+      const int next = first + kSampleThreads * kUnit;
+      const bool more = next - (int)(threadIdx.x & 63) * kUnit < n;
+      RawUnit<T> v;
+      if (more) v.load(p + next, n - next);
+      f(u, first);
+      if (!more) break;
+      u = v;
+      first = next;
     }
   }
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
-    if constexpr (V > 0) {
+    each_unit([&](const RawUnit<T>& u, int first) {
 #pragma unroll
-      for (int i = 0; i < V; ++i)
+      for (int j = 0; j < kUnit; ++j) f(logit(u.at(j)), first + j);
+    });
+  }
+};
+// The candidates in a row's place: each wave goes through what it has listed itself.
+struct List {
+  SampleShared& s;
+  int n;
+  int count = 0;  // of this wave
+  // a unit's tokens that `which` has a bit for, one of each lane at a time: most units have none, few lanes have two
+  template <typename U, typename L>
+  __device__ __forceinline__ void add(uint32_t which, const U& u, int first, L logit) {
+    unsigned long long who;
+    while ((who = __ballot(which != 0)) != 0) {
+      const int to = count + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+      const int j = __builtin_ctz(which | 256u);
+      float l = u.at(0);
 #pragma unroll
-        for (int j = 0; j < kUnit; ++j) f(at[i][j], (i * kSampleThreads + (int)threadIdx.x) * kUnit + j);
-    } else {
-      for (int first = (int)threadIdx.x * kUnit; first < n; first += kSampleThreads * kUnit) {
-        float v[kUnit];
-        load_unit(p + first, n - first, v);
-#pragma unroll
-        for (int j = 0; j < kUnit; ++j) f(first + j < n ? clean(v[j]) : -kInf, first + j);
+      for (int i = 1; i < kUnit; ++i) l = j == i ? u.at(i) : l;
+      if (which && to < kListed) {
+        s.list[threadIdx.x >> 6][to] = logit(l);
+        s.list_index[threadIdx.x >> 6][to] = first + j;
       }
+      which &= which - 1;
+      count += __popcll(who);
     }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    for (int i = threadIdx.x & 63; i < count; i += 64) f(s.list[threadIdx.x >> 6][i], s.list_index[threadIdx.x >> 6][i]);
+  }
+  // after the last add: whether all waves had room
+  __device__ __forceinline__ bool complete() {
+    if (count > kListed) s.overflow = 1;
+    __syncthreads();
+    return !s.overflow;
   }
 };
 
-__device__ __forceinline__ float block_max(float v, SampleShared& s) {
-  v = wave_max(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s.wavef[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = s.wavef[0];
-#pragma unroll
-  for (int w = 1; w < kSampleWaves; ++w) v = fmaxf(v, s.wavef[w]);
-  return v;
+// Every wave has left a value: the sixteen of them in the sixteen lanes of a row, then across the row.
+template <typename T, typename Op>
+__device__ __forceinline__ T of_waves(const T* left, Op op) {
+  T v = left[threadIdx.x & 15];
+  const auto bits = [](T x) { return __builtin_bit_cast(uint32_t, x); };
+  const auto back = [](uint32_t x) { return __builtin_bit_cast(T, x); };
+  v = op(v, back(dpp_move_u32<0xB1>(bits(v))));
+  v = op(v, back(dpp_move_u32<0x4E>(bits(v))));
+  v = op(v, back(dpp_move_u32<0x141>(bits(v))));
+  return op(v, back(dpp_move_u32<0x140>(bits(v))));
 }
-__device__ __forceinline__ float block_sum(float v, SampleShared& s) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s.wavef[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.f;
-#pragma unroll
-  for (int w = 0; w < kSampleWaves; ++w) v += s.wavef[w];
-  return v;
+struct OpSumI { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a + b; } };
+struct OpMaxI { __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); } };
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, dpp_move_u32<0xB1>(v));
+  v = max(v, dpp_move_u32<0x4E>(v));
+  v = max(v, dpp_move_u32<0x141>(v));
+  v = max(v, dpp_move_u32<0x140>(v));
+  u32x2_t r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(r[0], r[1]);
+  r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(r[0], r[1]);
 }
-__device__ __forceinline__ int block_sum_i(int v, SampleShared& s) {
-  v = wave_sum_i(v);
+// (their sums are whole numbers, or taken in one fixed order)
+__device__ __forceinline__ uint32_t block_sum_u32(uint32_t v, uint32_t* left) {
+  v = (uint32_t)wave_sum_i((int)v);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) s.wave32[threadIdx.x >> 6] = (uint32_t)v;
+  if ((threadIdx.x & 63) == 0) left[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = 0;
-#pragma unroll
-  for (int w = 0; w < kSampleWaves; ++w) v += (int)s.wave32[w];
-  return v;
+  return of_waves(left, OpSumI());
 }
 
 // The distance below the largest logit in octaves of probability, its weight, its bin
 struct Scale {
   float top, per;  // largest logit; octaves per unit of logit (log2(e) / temperature)
-  bool at_infinity;  // the largest is +inf: such tokens share the mass, nothing else has any
-  __device__ __forceinline__ float below(float l) const {
-    if (at_infinity) return l == kInf ? 0.f : kInf;
-    return (top - l) * per;
-  }
+  __device__ __forceinline__ float below(float l) const { return (top - l) * per; }
 };
 __device__ __forceinline__ float weight(float below) { return __builtin_amdgcn_exp2f(-below); }
-__device__ __forceinline__ unsigned long long mass_of(float below) {
-  // rintf: half a unit more than the product's own rounding; below 41 octaves nothing is left
-  return below < 42.f ? (unsigned long long)rintf(weight(below) * kMassOne) : 0ull;
-}
+__device__ __forceinline__ uint32_t mass_of(float below) { return (uint32_t)rintf(weight(below) * 2147483648.f); }
+// (of -infinity and NaN: 0, and the last bin)
 __device__ __forceinline__ int bin_of(float below) { return (int)fminf(below * kBinsPerOctave, (float)(kBins - 1)); }
-__device__ __forceinline__ float logit_of(uint32_t key) {
-  return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key);
-}
+
+// What is looked for: the token at which the count (by_mass: the mass) reaches a number
+struct Target {
+  bool by_mass;
+  uint32_t tokens;
+  unsigned long long mass;
+};
 
 __device__ __forceinline__ void clear_bins(SampleShared& s) {
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    s.mass[threadIdx.x + i * kSampleThreads] = 0;
-    s.count[threadIdx.x + i * kSampleThreads] = 0;
-  }
+  s.mass[threadIdx.x] = 0;
+  s.count[threadIdx.x] = 0;
   __syncthreads();
 }
 
-// The bin in which the running count reaches `tokens` (MASS: the running mass reaches `mass`), and what lies before it.
-template <bool MASS>
-__device__ void scan_bins(SampleShared& s, uint32_t tokens, unsigned long long mass, uint32_t count0, unsigned long long mass0) {
+// The bin in which the target is reached and what lies before it; s.bin = -1 if there is none.  Returns the total mass.  Four waves
+// do it, a lane four bins: with all sixteen at it the vector units would be four times as long busy with the same few bins.
+__device__ __forceinline__ unsigned long long scan_bins(SampleShared& s, Target to, uint32_t count0, unsigned long long mass0) {
+  if (threadIdx.x == 0) s.bin = -1;
   __syncthreads();
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
-  const uint32_t c0 = s.count[2 * t], c1 = s.count[2 * t + 1];
-  const unsigned long long m0 = s.mass[2 * t], m1 = s.mass[2 * t + 1];
-  uint32_t c = c0 + c1;
-  unsigned long long m = m0 + m1;
+  const int t = threadIdx.x, wave = t >> 6;
+  uint32_t c = 0, own_c[4];
+  unsigned long long m = 0, own_m[4];
+  if (t < kBins / 4) {
 #pragma unroll
-  for (int by = 1; by < 64; by *= 2) {
-    const uint32_t pc = __shfl_up(c, by);
-    const unsigned long long pm = shfl_up64(m, by);
-    if (lane >= by) { c += pc; m += pm; }
-  }
-  if (lane == 63) { s.wave32b[wave] = c; s.wave64[wave] = m; }
-  __syncthreads();
-  c += count0;
-  m += mass0;
-  for (int w = 0; w < wave; ++w) { c += s.wave32b[w]; m += s.wave64[w]; }
-  if (t == kSampleThreads - 1) s.total_mass = m;
-  c -= c0 + c1;
-  m -= m0 + m1;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t ci = i ? c1 : c0;
-    const unsigned long long mi = i ? m1 : m0;
-    const bool here = MASS ? (m < mass && m + mi >= mass) : (c < tokens && c + ci >= tokens);
-    if (here) {
-      s.bin = 2 * t + i;
-      s.before_count = c;
-      s.before_mass = m;
-      s.in_bin = ci;
+    for (int i = 0; i < 4; ++i) {
+      own_c[i] = s.count[4 * t + i];
+      own_m[i] = s.mass[4 * t + i];
+      c += own_c[i];
+      m += own_m[i];
     }
-    c += ci;
-    m += mi;
+    wave_scan(c, m);
+    if ((t & 63) == 63) { s.wave32b[wave] = c; s.wave64[wave] = m; }
   }
   __syncthreads();
+  unsigned long long total = mass0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) total += s.wave64[w];
+  if (t < kBins / 4) {
+    c += count0;
+    m += mass0;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) {
+      c += w < wave ? s.wave32b[w] : 0u;
+      m += w < wave ? s.wave64[w] : 0ull;
+    }
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {  // back from the sum up to the lane's last bin
+      const uint32_t c1 = c - own_c[i];
+      const unsigned long long m1 = m - own_m[i];
+      if (to.by_mass ? (m1 < to.mass && m >= to.mass) : (c1 < to.tokens && c >= to.tokens)) {
+        s.bin = 4 * t + i;
+        s.before_count = c1;
+        s.before_mass = m1;
+        s.in_bin = own_c[i];
+      }
+      c = c1;
+      m = m1;
+    }
+  }
+  __syncthreads();
+  return total;
 }
 
-// Fills the bins of the whole row.
+// Fills the bins of a row or of the list.
 template <typename R>
-__device__ void fill_bins(const R& row, const Scale& sc, SampleShared& s) {
+__device__ __forceinline__ void fill_bins(const R& row, const Scale& sc, SampleShared& s) {
   clear_bins(s);
-  // the last bin takes the far tail, most of a row: summed in registers, not by everybody at one address
-  uint32_t tail_count = 0;
-  unsigned long long tail_mass = 0;
+  // (the last bin, where most of a row may lie, in registers first)
+  uint32_t far_count = 0;
+  unsigned long long far_mass = 0;
   row.each([&](float l, int) {
     const float below = sc.below(l);
     const int bin = bin_of(below);
+    const uint32_t m = mass_of(below);
     if (bin < kBins - 1) {
       atomicAdd(&s.count[bin], 1u);
-      atomicAdd(&s.mass[bin], mass_of(below));
-    } else {
-      tail_count += l > -kInf;
-      tail_mass += mass_of(below);
+      atomicAdd(&s.mass[bin], (unsigned long long)m);
+    } else if (l > -kInf) {
+      ++far_count;
+      far_mass += m;
     }
   });
-  if (tail_count) {
-    atomicAdd(&s.count[kBins - 1], tail_count);
-    atomicAdd(&s.mass[kBins - 1], tail_mass);
+  if (far_count) {
+    atomicAdd(&s.count[kBins - 1], far_count);
+    atomicAdd(&s.mass[kBins - 1], far_mass);
   }
 }
 
-// The cut inside the bin that the scan found: the token at which the count reaches `tokens` (the mass `mass`).  Leaves it in
-// s.cut_key / s.cut_index and the mass up to and with it in s.kept_mass.  Returns whether the bins were overwritten.
-template <bool MASS, typename R>
-__device__ bool cut_in_bin(const R& row, const Scale& sc, SampleShared& s, uint32_t tokens, unsigned long long mass) {
+// The cut inside the bin that the scan found, left in s.cut / s.cut_index, with the mass up to and with it in s.kept_mass.  Returns
+// whether the bins were overwritten.
+template <typename R>
+__device__ __forceinline__ bool cut_in_bin(const R& row, const Scale& sc, SampleShared& s, Target to) {
   const int t = threadIdx.x;
   const int bin = s.bin;
   uint32_t before_count = s.before_count, members = s.in_bin;
   unsigned long long before_mass = s.before_mass;
-  bool overwritten = false;
   uint32_t low = 1, high = 0;  // keys of the members; low > high: those of the bin
-  if (members > kList) {
-    // Too many: split the range of their keys again, 11 bits at a time
+  bool split = false;
+  if (members > kRanked) {
+    // Too many: split the range of their keys, 10 bits at a time
     uint32_t lo = 0xFFFFFFFFu, hi = 0;
     row.each([&](float l, int) {
       if (l > -kInf && bin_of(sc.below(l)) == bin) {
@@ -235,27 +317,26 @@ __device__ bool cut_in_bin(const R& row, const Scale& sc, SampleShared& s, uint3
         hi = max(hi, key);
       }
     });
-    const unsigned long long hi64 = wave_max64(hi), lo64 = wave_max64(~lo);
+    hi = wave_max_u32(hi);
+    lo = wave_max_u32(~lo);
     __syncthreads();
-    if ((t & 63) == 0) { s.wave32[t >> 6] = (uint32_t)hi64; s.wave32b[t >> 6] = (uint32_t)lo64; }
+    if ((t & 63) == 0) { s.wave32[t >> 6] = hi; s.wave32b[t >> 6] = lo; }
     __syncthreads();
-    hi = lo = 0;
-    for (int w = 0; w < kSampleWaves; ++w) { hi = max(hi, s.wave32[w]); lo = max(lo, s.wave32b[w]); }
-    high = hi;
-    low = ~lo;
-    overwritten = true;
-    while (members > kList && low < high) {
+    high = of_waves(s.wave32, OpMaxI());
+    low = ~of_waves(s.wave32b, OpMaxI());
+    split = true;
+    while (members > kRanked && low < high) {
       const int bits = 32 - __clz(high - low);
-      const int shift = bits > 11 ? bits - 11 : 0;
+      const int shift = bits > 10 ? bits - 10 : 0;
       clear_bins(s);
       row.each([&](float l, int) {
         const uint32_t key = ordered_key(l);
         if (l > -kInf && key >= low && key <= high) {
           atomicAdd(&s.count[(high - key) >> shift], 1u);
-          atomicAdd(&s.mass[(high - key) >> shift], mass_of(sc.below(l)));
+          atomicAdd(&s.mass[(high - key) >> shift], (unsigned long long)mass_of(sc.below(l)));
         }
       });
-      scan_bins<MASS>(s, tokens, mass, before_count, before_mass);
+      scan_bins(s, to, before_count, before_mass);
       before_count = s.before_count;
       before_mass = s.before_mass;
       members = s.in_bin;
@@ -263,168 +344,403 @@ __device__ bool cut_in_bin(const R& row, const Scale& sc, SampleShared& s, uint3
       const uint32_t span = (1u << shift) - 1u;
       low = high - low > span ? high - span : low;
     }
-  }
-  if (members > kList) {
-    // all of one value: the cut is the r-th of them by index, found by halving the range of indices
-    const unsigned long long each = mass_of(sc.below(logit_of(high)));
-    uint32_t r = tokens - before_count;
-    if (MASS) r = each ? (uint32_t)((mass - before_mass + each - 1) / each) : members;
-    int lo = 0, hi = row.n - 1;
-    while (lo < hi) {
-      const int mid = lo + (hi - lo) / 2;
-      int c = 0;
-      row.each([&](float l, int at) { c += l > -kInf && ordered_key(l) == high && at <= mid; });
-      if ((uint32_t)block_sum_i(c, s) >= r) hi = mid;
-      else lo = mid + 1;
+    if (members > kRanked) {
+      // all of one value: the cut is the r-th of them by index, found by halving the range of indices
+      const float value = __uint_as_float((high & 0x80000000u) ? high ^ 0x80000000u : ~high);
+      const uint32_t each = mass_of(sc.below(value));
+      uint32_t r = to.tokens - before_count;
+      if (to.by_mass) r = each ? (uint32_t)((to.mass - before_mass + each - 1) / each) : members;
+      int first = 0, last = row.n - 1;
+      while (first < last) {
+        const int mid = first + (last - first) / 2;
+        int c = 0;
+        row.each([&](float l, int at) { c += l == value && at <= mid; });
+        if (block_sum_u32((uint32_t)c, s.wave32) >= r) last = mid;
+        else first = mid + 1;
+      }
+      __syncthreads();
+      if (t == 0) {
+        s.cut = value;
+        s.cut_index = first;
+        s.kept_mass = before_mass + (unsigned long long)r * each;
+      }
+      __syncthreads();
+      return split;
     }
-    __syncthreads();
-    if (t == 0) {
-      s.cut_key = high;
-      s.cut_index = lo;
-      s.kept_mass = before_mass + r * each;
-    }
-    __syncthreads();
-    return overwritten;
   }
-  __syncthreads();
-  if (t == 0) s.listed = 0;
+  if (t == 0) s.ranked = 0;
   __syncthreads();
   row.each([&](float l, int at) {
-    if (!(l > -kInf)) return;
+    const float below = sc.below(l);
     const uint32_t key = ordered_key(l);
-    if (low > high ? bin_of(sc.below(l)) == bin : (key >= low && key <= high)) {
-      const uint32_t to = atomicAdd(&s.listed, 1u);  // in any order: the ranks below do not depend on it
-      s.list_key[to] = key;
-      s.list_index[to] = at;
+    if (l > -kInf && (low > high ? bin_of(below) == bin : key >= low && key <= high)) {
+      const uint32_t slot = atomicAdd(&s.ranked, 1u);  // in any order: the ranks below do not depend on it
+      s.rank[slot] = l;
+      s.rank_index[slot] = at;
+      s.rank_mass[slot] = mass_of(below);
     }
   });
   __syncthreads();
-  if (t < (int)members) {
-    const uint32_t key = s.list_key[t];
-    const int at = s.list_index[t];
-    uint32_t c = before_count;
-    unsigned long long m = before_mass;
-    for (int j = 0; j < (int)members; ++j) {
-      const uint32_t k = s.list_key[j];
-      if (k > key || (k == key && s.list_index[j] < at)) {
+  // `share` lanes (of one wave) to a token, each comparing it with a part of the others
+  int shift = 6;
+  while (shift > 0 && ((int)members << shift) > kSampleThreads) --shift;
+  const int share = 1 << shift, mine = t >> shift;
+  uint32_t c = 0;
+  unsigned long long m = 0;
+  if (mine < (int)members) {
+    const float l = s.rank[mine];
+    const int at = s.rank_index[mine];
+#pragma unroll 2
+    for (int j = t & (share - 1); j < (int)members; j += share) {
+      const float o = s.rank[j];
+      if (o > l || (o == l && s.rank_index[j] < at)) {
         ++c;
-        m += mass_of(sc.below(logit_of(k)));
+        m += s.rank_mass[j];
       }
     }
-    const unsigned long long own = mass_of(sc.below(logit_of(key)));
-    if (MASS ? (m < mass && m + own >= mass) : c + 1 == tokens) {
-      s.cut_key = key;
-      s.cut_index = at;
+  }
+  for (int by = 1; by < share; by *= 2) {
+    c += __shfl_xor(c, by);
+    const uint32_t lo = __shfl_xor((uint32_t)m, by), hi = __shfl_xor((uint32_t)(m >> 32), by);
+    m += ((unsigned long long)hi << 32) | lo;
+  }
+  if (mine < (int)members && (t & (share - 1)) == 0) {
+    c += before_count;
+    m += before_mass;
+    const uint32_t own = s.rank_mass[mine];
+    if (to.by_mass ? (m < to.mass && m + own >= to.mass) : c + 1 == to.tokens) {
+      s.cut = s.rank[mine];
+      s.cut_index = s.rank_index[mine];
       s.kept_mass = m + own;
     }
   }
   __syncthreads();
-  return overwritten;
+  return split;
 }
 
-template <typename T, int V>
-__global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
-  __shared__ SampleShared s;
+struct Filters {
+  int k;          // tokens, 0: all
+  float p, min_p; // p >= 1: all
+};
+__device__ __forceinline__ unsigned long long mass_for(float p, unsigned long long inside) {
+  const unsigned long long mass = p > 0.f ? (unsigned long long)ceil((double)p * (double)inside) : 1ull;
+  return mass < 1 ? 1 : mass > inside ? inside : mass;
+}
+
+// Top-k and top-p on a row, or on a list that holds the first k tokens.
+template <typename R>
+__device__ __forceinline__ void find_cut(const R& row, const Scale& sc, const Filters& f, SampleShared& s) {
+  Target to{false, f.k ? (uint32_t)f.k : 0xFFFFFFFFu, 0};
+  bool filled = false;
+#pragma unroll 1
+  for (int by_mass = 0; by_mass < 2; ++by_mass) {
+    if (!filled) fill_bins(row, sc, s);
+    filled = true;
+    unsigned long long inside = scan_bins(s, to, 0, 0);
+    if (s.bin >= 0) {  // (fewer than k tokens above -inf: all of them stay)
+      filled = !cut_in_bin(row, sc, s, to);
+      inside = s.kept_mass;
+    }
+    if (!(f.p < 1.f)) break;
+    to = {true, 0, mass_for(f.p, inside)};
+  }
+}
+
+// The cut by mass (or by more tokens than lists are made for) in a whole row: a rough histogram, then the bins around the cut
+// exactly.  inside: the mass that p is a share of, 0: the row's.  s_above: tokens above the zone.  Returns false where that does not do.
+template <typename R>
+__device__ __forceinline__ bool find_zone_cut(const R& row, const Scale& sc, const Filters& f, bool by_mass, unsigned long long inside,
+                                              SampleShared& s, uint32_t& s_above) {
+  clear_bins(s);
+  // a bin's masses in units of its own size, 13 bits of each token.  (Rows of more than 2^18 tokens may overflow 32 bits: then the bins
+  // are wrong, and the exact count below finds it out.)  The last bin stays empty: most of a row may lie there, and everybody would add at one
+  // address; a target that no bin reaches is there.
+  const float per = sc.per * kBinsPerOctave, top = sc.top * per;
+  if (by_mass) {
+    row.each([&](float l, int) {
+      const float below = fminf(fmaf(-l, per, top), (float)(kBins - 1));
+      const int bin = (int)fmaxf(below, 0.f);
+      const float m = __builtin_amdgcn_exp2f(fmaf((float)bin - below, 1.f / kBinsPerOctave, 13.f));
+      if (bin < kBins - 1) atomicAdd(&s.count[bin], (uint32_t)m);
+    });
+  } else {
+    row.each([&](float l, int) {
+      const int bin = bin_of(sc.below(l));
+      if (bin < kBins - 1) atomicAdd(&s.count[bin], 1u);
+    });
+  }
+  __syncthreads();
+  // (a token of 1 is 2^41 here)
+  s.mass[threadIdx.x] = (unsigned long long)((float)s.count[threadIdx.x] * __builtin_amdgcn_exp2f(28.f - (float)threadIdx.x * (1.f / kBinsPerOctave)));
+  Target to{by_mass, (uint32_t)f.k, ~0ull};
+  if (by_mass) {
+    unsigned long long rough = scan_bins(s, to, 0, 0);
+    if (inside) rough = inside << 10;
+    to.mass = mass_for(f.p, rough);
+  }
+  // The bins between which the cut lies for certain, and one more on either side, in logits (whose edges need not be exact).  The masses
+  // are good to 2^-13; the logits of one bin may all be the same, with nothing in the bins around it.
+  to.mass -= to.mass >> 11;
+  scan_bins(s, to, 0, 0);
+  const int from = s.bin < 0 ? kBins - 1 : s.bin;
+  int upto = from;
+  if (by_mass) {
+    to.mass += to.mass >> 10;
+    scan_bins(s, to, 0, 0);
+    upto = s.bin < 0 ? kBins - 1 : s.bin;
+  }
+  const float high = from < 2 ? kInf : sc.top - (float)(from - 1) / (kBinsPerOctave * sc.per);
+  const float low = upto > kBins - 3 ? -3.4e38f : sc.top - (float)(upto + 2) / (kBinsPerOctave * sc.per);
+  if (threadIdx.x == 0) s.overflow = 0;
+  List list{s, row.n};
+  unsigned long long above = 0, all = 0;
+  uint32_t count = 0;
+  row.each_unit([&](const auto& u, int first) {
+    uint32_t zone = 0;
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) {
+      const float l = u.at(j);
+      const uint32_t m = mass_of(sc.below(l));
+      const bool over = l > high;
+      all += m;
+      above += over ? m : 0u;
+      count += over;
+      zone |= l >= low && !over ? 1u << j : 0u;
+    }
+    list.add(zone, u, first, [](float l) { return l; });
+  });
+  uint32_t c = count, none = 0;
+  wave_scan(c, above);
+  wave_scan(none, all);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) {
+    s.wave32[threadIdx.x >> 6] = c;
+    s.wave64[threadIdx.x >> 6] = above;
+    s.wave64b[threadIdx.x >> 6] = all;
+  }
+  if (!list.complete()) return false;
+  c = of_waves(s.wave32, OpSumI());
+  above = s.wave64[threadIdx.x & 15];
+  all = s.wave64b[threadIdx.x & 15];
+  none = 0;
+  scan_step<0x111, 0xF>(none, above);
+  scan_step<0x112, 0xF>(none, above);
+  scan_step<0x114, 0xF>(none, above);
+  scan_step<0x118, 0xF>(none, above);
+  scan_step<0x111, 0xF>(none, all);
+  scan_step<0x112, 0xF>(none, all);
+  scan_step<0x114, 0xF>(none, all);
+  scan_step<0x118, 0xF>(none, all);
+  const auto last_of_row = [](unsigned long long v) {
+    return ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 15) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, 15);
+  };
+  above = last_of_row(above);
+  all = last_of_row(all);
+  s_above = c;
+  to = {by_mass, (uint32_t)f.k, by_mass ? mass_for(f.p, inside ? inside : all) : 0};
+  fill_bins(list, sc, s);
+  scan_bins(s, to, c, above);
+  if (s.bin < 0) return !by_mass && c < to.tokens && low < -3e38f ? (s.cut = -kInf, s.kept_mass = all, true) : false;
+  cut_in_bin(list, sc, s, to);
+  return true;
+}
+
+// What a token brings to the race.  A lane meets its tokens by index: the first of equal ones stays.
+struct Runner {
+  float z = 0.f, best = -kInf;
+  int at = -1;
+  __device__ __forceinline__ void enter(bool in, float below, float log_noise, int index) {
+    const float ring = -below - log_noise;  // (base 2; not a number: never taken)
+    z += in ? weight(below) : 0.f;
+    const bool ahead = in && ring > best;
+    best = ahead ? ring : best;
+    at = ahead ? index : at;
+  }
+};
+
+template <typename T, bool TOP_IS_INF>
+__device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP_IS_INF>& row, float top, float low, Filters f, bool greedy,
+                                           float temperature, SampleShared& s) {
   const int t = threadIdx.x;
   const long long r = blockIdx.x;
-  Row<T, V> row;
-  row.p = (const T*)a.logits + r * a.stride;
-  row.n = a.n;
-  row.load();
-  const float temperature = a.temperature ? a.temperature[r] : 1.f;
-  const int k = a.top_k ? a.top_k[r] : 0;
-  const float p = a.top_p ? a.top_p[r] : 1.f;
-  const float min_p = a.min_p ? a.min_p[r] : 0.f;
-
   Scale sc;
-  float top = -kInf;
-  row.each([&](float l, int) { top = fmaxf(top, l); });
-  sc.top = block_max(top, s);
-  if (sc.top == -kInf) {
+  sc.top = TOP_IS_INF ? 0.f : top;
+  sc.per = greedy ? 1.f : fminf(1.44269504088896340736f / temperature, 1e30f);  // (0 times it stays 0)
+  const float* noise = a.noise && !greedy ? a.noise + r * a.noise_stride : nullptr;
+  const float min_p = f.min_p;
+  const auto in_share = [&](float l, float below) { return weight(below) >= min_p || l == sc.top; };  // the first always stays
+  Runner run;
+  List list{s, a.n};
+  bool listed = false;
+  if (!TOP_IS_INF && f.k > 0 && f.k <= 512) {
+    row.each_unit([&](const RawUnit<T>& u, int first) {
+      uint32_t which = 0;
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) which |= u.at(j) >= low && u.at(j) > -kInf ? 1u << j : 0u;
+      list.add(which, u, first, [](float l) { return l; });
+    });
+    listed = list.complete();
+  }
+  if (listed) {
+    find_cut(list, sc, f, s);
+    const float cut = s.cut;
+    const int cut_index = s.cut_index;
+    list.each([&](float l, int at) {
+      const float below = sc.below(l);
+      const bool in = (l > cut || (l == cut && at <= cut_index)) && below < kInf && in_share(l, below);
+      if (in) run.enter(true, below, noise ? __builtin_amdgcn_logf(noise[at]) : 0.f, at);
+    });
+  } else {
+    // Where many tokens are left their random numbers are fetched for every unit, one unit ahead; else where one of the wave's
+    // is still in.
+    bool ahead = !(min_p > 0.f);
+    if (f.k > 0 || f.p < 1.f) {
+      bool found = !TOP_IS_INF;
+      unsigned long long inside = 0;
+      uint32_t above = 0;
+#pragma unroll 1
+      for (int by_mass = f.k > 0 ? 0 : 1; found && by_mass < (f.p < 1.f ? 2 : 1); ++by_mass) {
+        found = find_zone_cut(row, sc, f, by_mass, inside, s, above);
+        inside = s.kept_mass;
+      }
+      if (!found) {
+        __syncthreads();
+        if (t == 0) s.cut = -kInf;
+        find_cut(row, sc, f, s);
+      }
+      ahead = found && above >= (uint32_t)a.n / 64 && !(min_p > 0.f);
+    }
+    __syncthreads();
+    const float cut = s.cut;
+    const int cut_index = s.cut_index;
+    ahead = ahead && noise;
+    float next[kUnit];
+    const auto fetch = [&](int first) {
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) next[j] = 1.f;
+      if (first + kUnit <= a.n) load_unit(noise + first, next);
+      else if (first < a.n) load_unit(noise + first, a.n - first, next);
+    };
+    if (ahead) fetch(t * kUnit);
+    row.each_unit([&](const RawUnit<T>& u, int first) {
+      float e[kUnit];
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) e[j] = ahead ? next[j] : 1.f;
+      if (ahead) fetch(first + kSampleThreads * kUnit);
+      uint32_t in = 0;
+      if (greedy) {
+#pragma unroll
+        for (int j = 0; j < kUnit; ++j) in |= row.logit(u.at(j)) == sc.top ? 1u << j : 0u;
+      } else {
+#pragma unroll
+        for (int j = 0; j < kUnit; ++j) {
+          const float l = row.logit(u.at(j));
+          in |= l > cut || (l == cut && first + j <= cut_index && l > -kInf) ? 1u << j : 0u;
+        }
+        if (min_p > 0.f)
+#pragma unroll
+          for (int j = 0; j < kUnit; ++j) {
+            const float l = row.logit(u.at(j));
+            in &= in_share(l, sc.below(l)) ? ~0u : ~(1u << j);
+          }
+      }
+      if (!__any(in != 0)) return;
+      if (!ahead && noise && in) load_unit(noise + first, a.n - first, e);
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j)
+        run.enter(in >> j & 1, sc.below(row.logit(u.at(j))), __builtin_amdgcn_logf(e[j]), first + j);
+    });
+  }
+  // the furthest runner; of equal ones the lowest index
+  const float wave_z = wave_sum(run.z);
+  const uint32_t ring = run.at < 0 ? 0u : ordered_key(run.best);
+  const uint32_t wave_ring = wave_max_u32(ring);
+  const uint32_t wave_at = wave_max_u32(ring == wave_ring ? ~(uint32_t)run.at : 0u);
+  __syncthreads();
+  if ((t & 63) == 0) {
+    s.wavef[t >> 6] = wave_z;
+    s.wave32[t >> 6] = wave_ring;
+    s.wave32b[t >> 6] = wave_at;
+  }
+  if (t == 0) s.cut_index = a.n;
+  __syncthreads();
+  const float z = of_waves(s.wavef, OpAdd());
+  const uint32_t best = of_waves(s.wave32, OpMaxI());
+  const uint32_t own = s.wave32[t & 15] == best ? s.wave32b[t & 15] : 0u;
+  uint32_t at = max(own, dpp_move_u32<0xB1>(own));
+  at = max(at, dpp_move_u32<0x4E>(at));
+  at = max(at, dpp_move_u32<0x141>(at));
+  at = max(at, dpp_move_u32<0x140>(at));
+  int token = (int)~at;
+  if (best == 0) {  // no random number of the tokens that are left is one: the first token
+    row.each([&](float l, int at) {
+      if (l == sc.top) atomicMin(&s.cut_index, at);
+    });
+    __syncthreads();
+    token = s.cut_index;
+  }
+  if (t == 0) {
+    a.token[r] = token;
+    if (a.prob) a.prob[r] = greedy ? 1.f : weight(sc.below(row.logit(load_one(row.p + token)))) / z;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  SampleShared& s = *(SampleShared*)lds;
+  const int t = threadIdx.x;
+  const long long r = blockIdx.x;
+  const Row<T, false> row{(const T*)a.logits + r * a.stride, a.n};
+  const float temperature = a.temperature ? a.temperature[r] : 1.f;
+  const bool greedy = !(temperature > 0.f);
+  Filters f;
+  f.k = a.top_k ? a.top_k[r] : 0;
+  f.k = f.k > 0 && f.k < a.n ? f.k : 0;
+  f.p = a.top_p ? a.top_p[r] : 1.f;
+  f.min_p = a.min_p ? a.min_p[r] : 0.f;
+  if (greedy) f = {0, 1.f, 0.f};
+
+  // The largest logit; and the smallest of the largest ones of `groups` groups of lanes: so many tokens at least are not below
+  // it, and about groups * ln(groups) are.  Groups of 2, 4, 8, 16 lanes for up to 512, 256, 128, 64 tokens.
+  float high = -kInf;
+  row.each([&](float l, int) { high = fmaxf(high, l); });
+  float low = fmaxf(high, dpp_move<0xB1>(high));
+  if (f.k <= 256) low = fmaxf(low, dpp_move<0x4E>(low));
+  if (f.k <= 128) low = fmaxf(low, dpp_move<0x141>(low));
+  if (f.k <= 64) low = fmaxf(low, dpp_move<0x140>(low));
+  high = wave_max(high);
+  low = wave_max(-low);
+  if ((t & 63) == 0) {
+    s.wavef[t >> 6] = high;
+    s.wavef2[t >> 6] = low;
+  }
+  if (t == 0) {
+    s.overflow = 0;
+    s.cut = -kInf;
+    s.cut_index = 0x7FFFFFFF;
+  }
+  __syncthreads();
+  high = of_waves(s.wavef, OpMax());
+  low = -of_waves(s.wavef2, OpMax());
+  if (high == -kInf) {
     if (t == 0) {
       a.token[r] = -1;
       if (a.prob) a.prob[r] = 0.f;
     }
-    return;
-  }
-  const bool greedy = !(temperature > 0.f);
-  sc.at_infinity = sc.top == kInf;
-  sc.per = greedy ? 1.f : fminf(1.44269504088896340736f / temperature, 1e30f);  // (0 times it stays 0)
-
-  uint32_t cut_key = 0;  // below every key
-  int cut_index = 0x7FFFFFFF;
-  if (!greedy) {
-    const bool by_count = k > 0 && k < a.n, by_mass = p < 1.f;
-    if (by_count || by_mass) {
-      bool filled = false;
-      unsigned long long inside = 0;  // mass of the first k
-      bool cut_by_count = false;
-      fill_bins(row, sc, s);
-      filled = true;
-      if (t == 0) s.bin = -1;
-      scan_bins<false>(s, by_count ? (uint32_t)k : 0xFFFFFFFFu, 0, 0, 0);
-      inside = s.total_mass;
-      cut_by_count = by_count && s.bin >= 0;  // fewer than k tokens have a logit above -inf: all of them stay
-      if (cut_by_count) {
-        filled = !cut_in_bin<false>(row, sc, s, (uint32_t)k, 0);
-        cut_key = s.cut_key;
-        cut_index = s.cut_index;
-        inside = s.kept_mass;
-      }
-      if (by_mass) {
-        const double share = p > 0.f ? ceil((double)p * (double)inside) : 1.0;
-        unsigned long long mass = (unsigned long long)share;
-        mass = mass < 1 ? 1 : mass > inside ? inside : mass;
-        if (!filled) fill_bins(row, sc, s);
-        scan_bins<true>(s, 0, mass, 0, 0);
-        cut_in_bin<true>(row, sc, s, 0, mass);
-        cut_key = s.cut_key;
-        cut_index = s.cut_index;
-      }
-    }
-  }
-
-  // The race among what is left.  The first token of the order always takes part, whatever the filters say.
-  float z = 0.f;
-  unsigned long long best = 0;
-  const float* noise = a.noise ? a.noise + r * a.noise_stride : nullptr;
-  row.each([&](float l, int at) {
-    const float below = sc.below(l);
-    const float w = weight(below);
-    const uint32_t key = ordered_key(l);
-    bool kept = l > -kInf && below < kInf && (key > cut_key || (key == cut_key && at <= cut_index));
-    kept = greedy ? l == sc.top : kept && (w >= min_p || l == sc.top);
-    if (kept) {
-      z += w;
-      float ring = greedy || !noise ? -below : -below - __builtin_amdgcn_logf(noise[at]);  // (base 2)
-      ring = ring == ring ? ring : -kInf;  // a number that is none loses
-      const unsigned long long mine = ((unsigned long long)ordered_key(ring) << 32) | (uint32_t)~at;
-      best = mine > best ? mine : best;
-    }
-  });
-  z = block_sum(z, s);
-  best = wave_max64(best);
-  if ((t & 63) == 0) s.wave64[t >> 6] = best;
-  __syncthreads();
-  if (t == 0) {
-    for (int w = 1; w < kSampleWaves; ++w) best = s.wave64[w] > best ? s.wave64[w] : best;
-    const int token = (int)~(uint32_t)best;
-    a.token[r] = token;
-    if (a.prob) {
-      const float l = Row<T, V>::clean(load_one(row.p + token));
-      a.prob[r] = greedy ? 1.f : weight(sc.below(l)) / z;
-    }
+  } else if (high < kInf) {
+    sample_row(a, row, high, low, f, greedy, temperature, s);
+  } else {
+    sample_row(a, Row<T, true>{row.p, row.n}, high, low, f, greedy, temperature, s);
   }
 }
 
 template <typename T>
 void sample(const SampleArgs& a, hipStream_t st) {
-  const int units = (a.n + kSampleThreads * kUnit - 1) / (kSampleThreads * kUnit);
-  if (units <= 1) sample_kernel<T, 1><<<a.rows, kSampleThreads, 0, st>>>(a);
-  else if (units <= 2) sample_kernel<T, 2><<<a.rows, kSampleThreads, 0, st>>>(a);
-  else if (units <= 4) sample_kernel<T, 4><<<a.rows, kSampleThreads, 0, st>>>(a);
-  else if (units <= 8) sample_kernel<T, 8><<<a.rows, kSampleThreads, 0, st>>>(a);
-  else sample_kernel<T, 0><<<a.rows, kSampleThreads, 0, st>>>(a);
+  static const hipError_t raised =
+      hipFuncSetAttribute((const void*)sample_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, kSampleLds);
+  (void)raised;
+  sample_kernel<T><<<a.rows, kSampleThreads, kSampleLds, st>>>(a);
 }
 
 }  // namespace
