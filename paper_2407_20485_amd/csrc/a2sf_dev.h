@@ -376,6 +376,13 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t lane_off, uint3
   asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0"
                : "=&s"(copy) : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(lane_off), "s"(base) : "memory");
 }
+// ... AHEAD bytes further on in memory (not in LDS: the instruction's offset moves both addresses, so lds_addr is at least AHEAD).  For a
+// base that scalar instructions have formed: it is read as it is.
+template <int AHEAD>
+__device__ __forceinline__ void dma16_ahead(const void* base, uint32_t lane_off, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3"
+               :: "s"(__builtin_amdgcn_readfirstlane(lds_addr - AHEAD)), "v"(lane_off), "s"(base), "n"(AHEAD) : "memory");
+}
 // ... from an address per lane
 __device__ __forceinline__ void dma16_at(const void* p, uint32_t lds_addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"

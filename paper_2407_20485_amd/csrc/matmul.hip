@@ -12,7 +12,11 @@
 // In both the instruction's first operand is B, its second A: its result then has, per lane, four neighbouring columns of C of the
 // row lane % 16.  An operand fragment is 16 rows x 128 bytes, 32 bytes per lane, of row lane % 16; which of the 128 they are is the same
 // for both operands, and that is all that matters.
+#include <math.h>
+
+#include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "a2sf_internal.h"
 #include "rows_dev.h"
@@ -23,9 +27,11 @@ namespace {
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int kStep = 128;  // bytes of k per step: a scale block
+constexpr int kComputeUnits = 256;
 constexpr int kGroup = 4;   // steps whose scales are loaded together: four bytes
 
 struct Scaled {  // the 8-bit instruction
@@ -33,6 +39,15 @@ struct Scaled {  // the 8-bit instruction
   static __device__ __forceinline__ Fragment make(i32x8_t v, uint32_t) { return v; }
   static __device__ __forceinline__ f32x4_t mul(const Fragment& b, const Fragment& a, f32x4_t c, uint32_t b_scale, uint32_t a_scale) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, 0, (int)b_scale, 0, (int)a_scale);
+  }
+  static __device__ __forceinline__ f32x16_t mul(const Fragment& b, const Fragment& a, f32x16_t c, uint32_t b_scale, uint32_t a_scale, int block) {
+    // (which byte of the scale operands is part of the instruction)
+    switch (block) {
+      case 0: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, 0, 0, 0, (int)b_scale, 0, (int)a_scale);
+      case 1: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, 0, 0, 1, (int)b_scale, 1, (int)a_scale);
+      case 2: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, 0, 0, 2, (int)b_scale, 2, (int)a_scale);
+      default: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, 0, 0, 3, (int)b_scale, 3, (int)a_scale);
+    }
   }
 };
 struct Exact {  // by way of bf16, the scales applied on the way
@@ -55,6 +70,11 @@ struct Exact {  // by way of bf16, the scales applied on the way
   static __device__ __forceinline__ f32x4_t mul(const Fragment& b, const Fragment& a, f32x4_t c, uint32_t, uint32_t) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.part[i], a.part[i], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ f32x16_t mul(const Fragment& b, const Fragment& a, f32x16_t c, uint32_t, uint32_t, int) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.part[i], a.part[i], c, 0, 0, 0);
     return c;
   }
 };
@@ -106,63 +126,92 @@ __device__ __forceinline__ void store_columns<float>(float* p, int have, f32x4_t
     if (i < have) p[i] = v[i];
 }
 
+// sixteen bytes of neighbouring columns, as far as there are
+template <typename T>
+__device__ __forceinline__ void store_bytes(T* p, int have, u32x4_t v) {
+  constexpr int kHere = 16 / (int)sizeof(T);
+  if (have >= kHere) {
+    *(u32x4_at2_t*)p = v;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kHere; ++i)
+    if (i < have) {
+      if constexpr (sizeof(T) == 4) p[i] = __uint_as_float(v[i]);
+      else p[i] = (T)(v[i / 2] >> (16 * (i & 1)));
+    }
+}
+
 // ---- a few rows of A: B is streamed once, straight into registers ------------------------------------------------------------
 // A workgroup takes 16 columns of C and all rows (MT tiles of 16), its waves share k in groups of four steps and add their parts
-// in LDS in a fixed order.  Bound by the stream of B; A comes from the caches.
+// in LDS in a fixed order.  Bound by the stream of B; A comes from the caches.  The next group's part of B is on its way while the
+// present one is multiplied, and A is a step ahead.
 template <typename T, int MT>
-__global__ __launch_bounds__(1024) void matmul_rows_kernel(MatmulArgs g) {
+__global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs g) {
   typedef typename Way<T>::type W;
   extern __shared__ f32x4_t part[];  // [waves][MT][64]
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63, waves = blockDim.x >> 6;
   const int n0 = blockIdx.x * 16;
-  const int steps = (g.k + kStep - 1) / kStep;
-  const uint8_t* b = g.b + (long long)min(n0 + (lane & 15), g.n - 1) * g.b_stride;
+  const int steps = (g.k + kStep - 1) / kStep, groups = (steps + kGroup - 1) / kGroup;
+  const int kl = (lane >> 4) * 16;  // and 64 on: an access takes 64 bytes of each of 16 rows
+  const uint8_t* b = g.b + (long long)min(n0 + (lane & 15), g.n - 1) * g.b_stride + kl;
   const uint8_t* bs = g.b_scales + (long long)(n0 / 128) * g.b_scale_stride;
-  const uint8_t* a[MT];
-  const uint8_t* as[MT];
+  uint32_t a_at[MT], as_at[MT];  // byte offsets of this lane's rows (at most 64 of them)
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
-    const int row = min(i * 16 + (lane & 15), g.m - 1);
-    a[i] = g.a + (long long)row * g.a_stride;
-    as[i] = g.a_scales + (long long)row * g.a_scale_stride;
+    const uint32_t row = (uint32_t)min(i * 16 + (lane & 15), g.m - 1);
+    a_at[i] = row * (uint32_t)g.a_stride + kl;
+    as_at[i] = row * (uint32_t)g.a_scale_stride;
   }
   f32x4_t acc[MT] = {};
-  const int kl = (lane >> 4) * 32;
-  for (int s0 = wave * kGroup; s0 < steps; s0 += waves * kGroup) {
+  const auto whole = [&](int group) { return (group + 1) * kGroup * kStep <= g.k; };
+  i32x8_t bv[kGroup], bn[kGroup];
+  const auto load_b = [&](i32x8_t* to, int group) {
+    const uint8_t* p = b + (long long)group * kGroup * kStep;
+    if (whole(group)) {
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) to[j] = join(*(const i32x4_t*)(p + j * kStep), *(const i32x4_t*)(p + j * kStep + 64));
+    } else {
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) {
+        const int k0 = (group * kGroup + j) * kStep;
+        to[j] = join(load_chunk(b, k0, g.k - kl), load_chunk(b, k0 + 64, g.k - kl));
+      }
+    }
+  };
+  const auto load_a = [&](i32x8_t* to, int s) {
+    if ((s + 1) * kStep <= g.k) {
+      const uint8_t* p = g.a + (long long)s * kStep;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) to[i] = join(*(const i32x4_t*)(p + a_at[i]), *(const i32x4_t*)(p + a_at[i] + 64));
+    } else {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) to[i] = join(load_chunk(g.a + a_at[i], s * kStep, g.k - kl), load_chunk(g.a + a_at[i], s * kStep + 64, g.k - kl));
+    }
+  };
+  if (wave < groups) load_b(bv, wave);
+  for (int group = wave; group < groups; group += waves) {
+    const int s0 = group * kGroup;
     const uint32_t b4 = *(const uint32_t*)(bs + s0);
     uint32_t a4[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) a4[i] = *(const uint32_t*)(as[i] + s0);
-    if ((s0 + kGroup) * kStep <= g.k) {
-      i32x8_t bv[kGroup];
+    for (int i = 0; i < MT; ++i) a4[i] = *(const uint32_t*)(g.a_scales + as_at[i] + s0);
+    i32x8_t av[2][MT];
+    load_a(av[0], s0);
+    if (group + waves < groups) load_b(bn, group + waves);
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) {
-        const int k0 = (s0 + j) * kStep + kl;
-        bv[j] = join(*(const i32x4_t*)(b + k0), *(const i32x4_t*)(b + k0 + 16));
-      }
+    for (int j = 0; j < kGroup; ++j) {
+      if (j + 1 < kGroup) load_a(av[(j + 1) & 1], s0 + j + 1);  // (past the end of k: zeros)
+      const uint32_t sb = s0 + j < steps ? b4 >> (8 * j) & 255 : 0;
+      const auto fb = W::make(bv[j], sb);
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) {
-        const int k0 = (s0 + j) * kStep + kl;
-        const uint32_t sb = b4 >> (8 * j) & 255;
-        const auto fb = W::make(bv[j], sb);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const uint32_t sa = a4[i] >> (8 * j) & 255;
-          acc[i] = W::mul(fb, W::make(join(*(const i32x4_t*)(a[i] + k0), *(const i32x4_t*)(a[i] + k0 + 16)), sa), acc[i], sb, sa);
-        }
-      }
-    } else {
-      for (int j = 0; j < kGroup && s0 + j < steps; ++j) {
-        const int k0 = (s0 + j) * kStep + kl;
-        const uint32_t sb = b4 >> (8 * j) & 255;
-        const auto fb = W::make(join(load_chunk(b, k0, g.k), load_chunk(b, k0 + 16, g.k)), sb);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const uint32_t sa = a4[i] >> (8 * j) & 255;
-          acc[i] = W::mul(fb, W::make(join(load_chunk(a[i], k0, g.k), load_chunk(a[i], k0 + 16, g.k)), sa), acc[i], sb, sa);
-        }
+      for (int i = 0; i < MT; ++i) {
+        const uint32_t sa = s0 + j < steps ? a4[i] >> (8 * j) & 255 : 0;  // (there may be anything past the last scale)
+        acc[i] = W::mul(fb, W::make(av[j & 1][i], sa), acc[i], sb, sa);
       }
     }
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) bv[j] = bn[j];
   }
 #pragma unroll
   for (int i = 0; i < MT; ++i) part[(wave * MT + i) * 64 + lane] = acc[i];
@@ -176,133 +225,331 @@ __global__ __launch_bounds__(1024) void matmul_rows_kernel(MatmulArgs g) {
 }
 
 // ---- tiles of C ----------------------------------------------------------------------------------------------------------------
-// BM x BN of C per workgroup of WM x WN waves.  The tiles of A and B of a step go from memory straight into LDS, one step
-// ahead of the products, into the half that the step before has left.  A row of a step is 128 bytes, eight chunks of 16; chunk c of
-// row r lies at c ^ (r / 2 % 8): 16 lanes that read the same chunk of 16 rows then meet all 64 banks once.
-template <int BM, int BN>
-constexpr int tile_bytes() { return 2 * (BM + BN) * kStep; }
+// BM x BN of C per workgroup of WM x WN waves, by the 32 x 32 instructions.  k goes by half blocks of 64 bytes: a ring of STAGES
+// stages in LDS holds a half block of the tile's rows each, filled by loads that go from memory straight into LDS, STAGES - 1
+// half blocks ahead.  Persistent: a workgroup goes from tile to tile and the stream of half blocks runs on across them.
+//
+// Eight waves: the two of a SIMD are half an iteration apart, with a barrier at each half: while one has the matrix pipe, the other
+// reads the fragments of its next half block and fetches.  (8192 x 8192 x 8192, all waves in step 490 us, so 461; the matrix pipe is busy
+// 58 % of the cycles and the chip at its power limit, 1.95 GHz.)  Four waves: two or more workgroups share a compute unit instead.
+//
+// A row of a stage is 64 bytes, four chunks of 16; chunk c of row r lies at c ^ (r / 4 % 4): 16 lanes that read the same chunk of 16
+// rows then meet all 64 banks once.  The scales of four blocks of the tile's rows come the same way, a group ahead.  Results go through
+// LDS on their way out, so that they leave as 64 neighbouring bytes of a row (as a lane's own 8 bytes: 8192 x 22016 x 4096 707 us, so 675).
+constexpr int kHalf = 64;
+
+template <int BM, int BN, int STAGES>
+struct TileLds {
+  static constexpr int kStage = (BM + BN) * kHalf, kScales = (BM + 64) * 4;
+  static constexpr int kRing = 2 * kScales;  // (not at 0: a load's LDS address is formed from one up to 448 bytes lower)
+  static constexpr int kOut = kRing + STAGES * kStage;
+  static constexpr int kBytes = kOut;  // and 2 KB per wave, through which results leave
+};
 
 struct TilePlan {
   int tiles_m, tiles_n;
   int group_m;  // tiles are taken in strips of so many rows of tiles, columns inside a strip first
-  int splits;   // parts of k, each a workgroup of its own
-  int groups;   // groups of steps per part
+  int splits;   // parts of k, each a tile of its own
+  int groups;   // groups of four blocks per part
   float* partial;  // splits > 1: [splits][m][n]
 };
 
-template <typename T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(WM* WN * 64) void matmul_tile_kernel(MatmulArgs g, TilePlan plan) {
+template <int N, typename F, int... U>
+__device__ __forceinline__ void with_each(F f, std::integer_sequence<int, U...>) { (f(std::integral_constant<int, U>()), ...); }
+template <int N, typename F>
+__device__ __forceinline__ void with_each(F f) { with_each<N>(f, std::make_integer_sequence<int, N>()); }
+
+template <typename T, int BM, int BN, int WM, int WN, int STAGES>
+__global__ __launch_bounds__(WM* WN * 64, 2) void matmul_tile_kernel(MatmulArgs g, TilePlan plan) {
   typedef typename Way<T>::type W;
-  constexpr int kWavesHere = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
-  constexpr int kUnits = (BM + BN) / 8 / kWavesHere, kUnitsA = BM / 8 / kWavesHere;  // a unit: 8 rows, 1 KB, a load of a wave
-  static_assert(BM % (8 * kWavesHere) == 0 && BN % (8 * kWavesHere) == 0 && 128 % TN == 0, "");
+  typedef TileLds<BM, BN, STAGES> L;
+  constexpr int kWavesHere = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 32, NT = TN / 32;
+  constexpr int kUnits = (BM + BN) / 16 / kWavesHere, kUnitsA = BM / 16 / kWavesHere;  // a unit: 16 rows, 1 KB, a load of a wave
+  constexpr bool kApart = kWavesHere == 8;
+  static_assert(BM % (16 * kWavesHere) == 0 && BN % (16 * kWavesHere) == 0 && BM % 64 == 0 && 128 % TN == 0 && (STAGES == 4 || STAGES == 8), "");
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+  const bool second = kApart && wave >= 4;
 
   // Workgroups go to the 8 dies in turn: a die works on a contiguous part of the order of tiles, so that what its 32 compute
   // units work on at a time is a block of C whose rows of A and B its L2 holds.
   const unsigned tiles = (unsigned)plan.tiles_m * plan.tiles_n * plan.splits;
-  const unsigned per = tiles / 8, extra = tiles % 8, die = blockIdx.x % 8;
-  unsigned id = die * per + min(die, extra) + blockIdx.x / 8;
-  const unsigned split = id % plan.splits;
-  id /= plan.splits;
-  const unsigned strip = plan.group_m * plan.tiles_n, first_m = id / strip * plan.group_m;
-  const unsigned here = min((unsigned)plan.group_m, plan.tiles_m - first_m);
-  const unsigned in = id - id / strip * strip;
-  const int m0 = (int)(first_m + in % here) * BM, n0 = (int)(in / here) * BN;
+  const unsigned dies = min(8u, gridDim.x), die = blockIdx.x % dies, slots = (gridDim.x - die + dies - 1) / dies;
+  const unsigned tile_end = (die + 1) * (tiles / dies) + min(die + 1, tiles % dies);
+  unsigned tile = die * (tiles / dies) + min(die, tiles % dies) + blockIdx.x / dies;
+  if (tile >= tile_end) return;
+  struct Place {
+    int m0, n0, split, g0, g1, half, end;  // half blocks; end: rounded up to whole turns of the ring
+  };
+  const int groups = ((g.k + kStep - 1) / kStep + kGroup - 1) / kGroup;
+  const auto place = [&](unsigned id) {
+    Place p;
+    p.split = (int)(id % plan.splits);
+    id /= plan.splits;
+    const unsigned strip = plan.group_m * plan.tiles_n, first_m = id / strip * plan.group_m;
+    const unsigned here = min((unsigned)plan.group_m, plan.tiles_m - first_m);
+    const unsigned in = id - id / strip * strip;
+    p.m0 = (int)(first_m + in % here) * BM;
+    p.n0 = (int)(in / here) * BN;
+    p.g0 = p.split * plan.groups;
+    p.g1 = min(groups, p.g0 + plan.groups);
+    p.half = min((g.k + kHalf - 1) / kHalf - p.g0 * 2 * kGroup, (p.g1 - p.g0) * 2 * kGroup);
+    p.end = (p.half + STAGES - 1) / STAGES * STAGES;
+    return p;
+  };
 
-  const int steps = (g.k + kStep - 1) / kStep;
-  const int s0 = split * plan.groups * kGroup, s1 = min(steps, s0 + plan.groups * kGroup);
-
-  // this lane's part of each unit: byte offsets from the tile's first row
+  // The stream of half blocks: this lane's part of each unit in bytes from the tile's first row, and where the next fetch is
+  const uint32_t chunk = (uint32_t)(((lane & 3) ^ (lane >> 4)) * 16);
   uint32_t off[kUnits];
+  const uint8_t *a0, *b0;
+  Place next;
+  unsigned next_tile = tile;
+  int next_half = 0;
+  bool drained = false;  // a fetch was not by loads into LDS: their count says nothing any more
+  const auto aim = [&] {
+    next = place(next_tile);
 #pragma unroll
-  for (int i = 0; i < kUnits; ++i) {
-    const bool of_a = i < kUnitsA;
-    const int r = ((of_a ? i : i - kUnitsA) * kWavesHere + wave) * 8 + lane / 8;
-    const int row = of_a ? min(m0 + r, g.m - 1) - m0 : min(n0 + r, g.n - 1) - n0;
-    off[i] = (uint32_t)row * (uint32_t)(of_a ? g.a_stride : g.b_stride) + (uint32_t)(((lane & 7) ^ (r / 2 % 8)) * 16);
-  }
-  const uint8_t* a0 = g.a + (long long)m0 * g.a_stride;
-  const uint8_t* b0 = g.b + (long long)n0 * g.b_stride;
-  const auto fetch = [&](int s, int half) {
-    const uint32_t to = half * ((BM + BN) * kStep);
-    if ((s + 1) * kStep <= g.k) {
+    for (int i = 0; i < kUnits; ++i) {
+      const bool of_a = i < kUnitsA;
+      const int r = ((of_a ? i : i - kUnitsA) * kWavesHere + wave) * 16 + lane / 4;
+      const int row = of_a ? min(r, g.m - 1 - next.m0) : min(r, g.n - 1 - next.n0);
+      off[i] = (uint32_t)row * (uint32_t)(of_a ? g.a_stride : g.b_stride) + chunk;
+    }
+    a0 = g.a + (long long)next.m0 * g.a_stride + next.g0 * kGroup * kStep;
+    b0 = g.b + (long long)next.n0 * g.b_stride + next.g0 * kGroup * kStep;
+    next_half = 0;
+  };
+  const uint32_t lds_wave = (uint32_t)wave * 1024;
+  // one more half block of the same tile, `ahead` half blocks from where the stream is
+  const auto fetch_on = [&](int stage, auto ahead) {
 #pragma unroll
-      for (int i = 0; i < kUnits; ++i) dma16((i < kUnitsA ? a0 : b0) + (long long)s * kStep, off[i], to + (i * kWavesHere + wave) * 1024);
-    } else {  // the last, partial step: zeros behind the end of k
+    for (int i = 0; i < kUnits; ++i)
+      dma16_ahead<decltype(ahead)::value * kHalf>(i < kUnitsA ? a0 : b0, off[i], lds_wave + L::kRing + stage * L::kStage + i * kWavesHere * 1024);
+  };
+  // the next half block, whatever it is
+  const auto fetch = [&](int stage) {
+    const uint32_t to = L::kRing + (uint32_t)stage * L::kStage + lds_wave;
+    const int left = g.k - (next.g0 * kGroup * kStep + next_half * kHalf);  // bytes of k
+    if (left > 0 && left < kHalf && next_half < next.half) {  // the last, partial one: zeros behind the end of k
 #pragma unroll
-      for (int i = 0; i < kUnits; ++i) {
-        const int r = lane / 8, chunk = ((lane & 7) ^ (((i * kWavesHere + wave) * 8 + r) / 2 % 8)) * 16;
-        const uint8_t* row = (i < kUnitsA ? a0 : b0) + (off[i] - (uint32_t)chunk);
-        *(i32x4_t*)(lds + to + (i * kWavesHere + wave) * 1024 + lane * 16) = load_chunk(row, s * kStep + chunk, g.k);
+      for (int i = 0; i < kUnits; ++i)
+        *(i32x4_t*)(lds + to + i * kWavesHere * 1024 + lane * 16) =
+            load_chunk((i < kUnitsA ? a0 : b0) + (off[i] - chunk), (int)chunk, left);
+      drained = true;
+    } else if (next_half < next.half) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) dma16(i < kUnitsA ? a0 : b0, off[i], to + i * kWavesHere * 1024);
+    } else {
+      drained = true;  // (a half block that only fills up the turn of the ring)
+    }
+    a0 += kHalf;
+    b0 += kHalf;
+    if (++next_half == next.end) {
+      // (past the last tile it is fetched again, for nobody)
+      if (next_tile + slots < tile_end) next_tile += slots;
+      aim();
+    }
+  };
+  // Scales: the waves take 64 rows each, the one after them the tile's blocks of 128 columns
+  int ring = 0;  // of the two places for a group's scales, the one that the next fetch goes to
+  const auto fetch_scales = [&](const Place& p, int group) {
+    const uint32_t to = ring * L::kScales;
+    ring ^= 1;
+#pragma unroll
+    for (int u = 0; u < BM / 64 + 1; ++u) {
+      if (u % kWavesHere != wave) continue;
+      if (u < BM / 64) {
+        const uint32_t row = (uint32_t)(min(p.m0 + u * 64 + lane, g.m - 1) - p.m0);
+        dma4(g.a_scales + (long long)p.m0 * g.a_scale_stride + group * 4, row * (uint32_t)g.a_scale_stride, to + u * 256);
+      } else {
+        const uint32_t row = (uint32_t)(min(p.n0 / 128 + lane, (g.n - 1) / 128) - p.n0 / 128);
+        dma4(g.b_scales + (long long)(p.n0 / 128) * g.b_scale_stride + group * 4, row * (uint32_t)g.b_scale_stride, to + u * 256);
       }
     }
   };
 
   const int wm = wave % WM * TM, wn = wave / WM * TN;
-  const uint8_t* as[MT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i) as[i] = g.a_scales + (long long)min(m0 + wm + i * 16 + (lane & 15), g.m - 1) * g.a_scale_stride;
-  const uint8_t* bs = g.b_scales + (long long)min((n0 + wn) / 128, (g.n - 1) / 128) * g.b_scale_stride;
-
-  f32x4_t acc[NT][MT] = {};
-  uint32_t a_next[MT], a_now[MT], b_next, b_now = 0;
-#pragma unroll
-  for (int i = 0; i < MT; ++i) a_next[i] = *(const uint32_t*)(as[i] + s0);
-  b_next = *(const uint32_t*)(bs + s0);
-  fetch(s0, 0);
-  for (int s = s0; s < s1; ++s) {
-    const int half = (s - s0) & 1;
-    wait_vm_barrier<0>();
-    if ((s & (kGroup - 1)) == 0) {
-      // The scales of four steps, loaded four steps ago.  They are taken over here, where nothing is on its way: the compiler waits
-      // for all outstanding loads when it takes the result of one.
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        a_now[i] = a_next[i];
-        asm volatile("" : "+v"(a_now[i]));
-      }
-      b_now = b_next;
-      asm volatile("" : "+v"(b_now));
-      const int ahead = s + kGroup < steps ? s + kGroup : s;
-#pragma unroll
-      for (int i = 0; i < MT; ++i) a_next[i] = *(const uint32_t*)(as[i] + ahead);
-      b_next = *(const uint32_t*)(bs + ahead);
-    } else {
-#pragma unroll
-      for (int i = 0; i < MT; ++i) a_now[i] >>= 8;
-      b_now >>= 8;
-    }
-    if (s + 1 < s1) fetch(s + 1, half ^ 1);
-    const uint8_t* base = lds + half * ((BM + BN) * kStep);
-    const auto fragment = [&](int r) {
-      const uint8_t* row = base + r * kStep;
-      const int x = r / 2 % 8;
-      return join(*(const i32x4_t*)(row + ((lane >> 4) ^ x) * 16), *(const i32x4_t*)(row + ((4 + (lane >> 4)) ^ x) * 16));
-    };
-    typename W::Fragment b[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) b[j] = W::make(fragment(BM + wn + j * 16 + (lane & 15)), b_now & 255);
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const auto a = W::make(fragment(wm + i * 16 + (lane & 15)), a_now[i] & 255);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) acc[j][i] = W::mul(b[j], a, acc[j][i], b_now, a_now[i]);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int row = m0 + wm + i * 16 + (lane & 15);
-    if (row >= g.m) continue;
+  // fragments: chunks lane / 32 and lane / 32 + 2 of row lane % 32
+  const int lr = lane & 31, x = lr / 4 % 4;
+  const uint32_t lo = (uint32_t)(lr * kHalf + ((lane >> 5) ^ x) * 16), hi = (uint32_t)(lr * kHalf + ((2 + (lane >> 5)) ^ x) * 16);
+  i32x8_t a[kApart ? 1 : 2][MT], b[kApart ? 1 : 2][NT];
+  const auto read = [&](int set, int stage) {
+    const uint8_t* s = lds + L::kRing + stage * L::kStage;
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const int col = n0 + wn + j * 16 + (lane >> 4) * 4;
-      if (col >= g.n) continue;
-      if (plan.splits > 1) store_columns(plan.partial + ((long long)split * g.m + row) * g.n + col, g.n - col, acc[j][i]);
-      else store_columns((T*)g.c + (long long)row * g.c_stride + col, g.n - col, acc[j][i]);
+      const uint8_t* p = s + (BM + wn + j * 32) * kHalf;
+      b[set][j] = join(*(const i32x4_t*)(p + lo), *(const i32x4_t*)(p + hi));
     }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const uint8_t* p = s + (wm + i * 32) * kHalf;
+      a[set][i] = join(*(const i32x4_t*)(p + lo), *(const i32x4_t*)(p + hi));
+    }
+  };
+  uint32_t as[MT], bs;
+  f32x16_t acc[NT][MT];
+  const auto multiply = [&](int set, int block) {
+    typename W::Fragment fa[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) fa[i] = W::make(a[set][i], as[i] >> (8 * block) & 255);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const auto fb = W::make(b[set][j], bs >> (8 * block) & 255);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) acc[j][i] = W::mul(fb, fa[i], acc[j][i], bs, as[i], block);
+    }
+    // (here, and not past the barriers that follow, where the compiler would take them to the end of the group)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i) asm volatile("" : "+v"(acc[j][i]));
+  };
+  int ready = 0;  // stages from here on that have landed already
+  const auto landed = [&] {
+    if (ready > 0) --ready;
+    else if (drained) wait_vm<0>();
+    else wait_vm<(STAGES - 2) * kUnits>();
+  };
+  const auto landed_on = [&](auto u) {  // the same in a group whose fetches are all alike
+    if (decltype(u)::value >= STAGES - 1 || decltype(u)::value >= ready) wait_vm<(STAGES - 2) * kUnits>();
+  };
+  const auto barrier = [] { asm volatile("s_barrier" ::: "memory"); };
+
+  aim();
+  fetch_scales(next, next.g0);
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+  if constexpr (kApart) {
+    if (second) {
+      landed();
+      barrier();
+    }
+  } else {
+    landed();
+    barrier();
+    fetch(STAGES - 1);
+    read(0, 0);
   }
+  int taken = 0;  // of the two places for scales, the one with the present group's
+  for (; tile < tile_end; tile += slots) {
+    const Place p = place(tile);
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[j][i][q] = 0.f;
+    // One half block: h of the tile, `stage` of the ring, the `block`-th of a group's four blocks.  ON: so are the STAGES ones after it, in
+    // the same tile, `ahead` of where the stream is noted to be, and nothing need be asked.
+    const auto half_block = [&](int h, int stage, int set, int block, auto on, auto ahead) {
+      constexpr bool ON = decltype(on)::value;
+      // four waves: the next half block's stage has landed, for everybody, and everybody has read this one's;
+      // eight: this one's has landed, everybody has read the one before
+      if (!second) {
+        if constexpr (ON) landed_on(ahead);
+        else landed();
+      }
+      if constexpr (!kApart) wait_lds();
+      barrier();
+      const bool there = ON || h < p.half;
+      if ((ON ? ahead == 0 : h % (2 * kGroup) == 0) && there) {
+        const uint32_t* s = (const uint32_t*)(lds + taken * L::kScales);
+        taken ^= 1;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) as[i] = s[wm + i * 32 + lr];
+        bs = s[BM + wn / 128];
+        const int group = p.g0 + h / (2 * kGroup) + 1;
+        if (ON || group < p.g1) {
+          fetch_scales(p, group);
+        } else if (tile + slots < tile_end) {
+          const Place after = place(tile + slots);
+          fetch_scales(after, after.g0);
+        }
+      } else if (!ON && h % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) as[i] >>= 8;
+        bs >>= 8;
+      }
+      if constexpr (kApart) {
+        if (there) read(0, stage);
+        if constexpr (ON) fetch_on((stage + STAGES - 1) % STAGES, ahead);
+        else fetch((stage + STAGES - 1) % STAGES);
+        wait_lds();
+        if (second) {
+          if constexpr (ON) landed_on(ahead);
+          else landed();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        barrier();
+        __builtin_amdgcn_s_setprio(1);
+        if (there) multiply(0, block);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        read(set ^ 1, (stage + 1) % STAGES);
+        if constexpr (ON) fetch_on(stage, ahead);
+        else fetch(stage);
+        if (there) multiply(set, block);
+      }
+    };
+    int h = 0;
+    const int whole = min(p.half, (g.k - p.g0 * kGroup * kStep) / kHalf);
+#pragma unroll 1
+    for (; h + 2 * kGroup + STAGES < whole; h += 2 * kGroup) {  // (the stream stays short of the tile's end)
+      with_each<2 * kGroup>([&](auto u) {
+        constexpr int U = decltype(u)::value;
+        half_block(h + U, U % STAGES, U & 1, U / 2, std::true_type(), u);
+      });
+      ready = 0;
+      a0 += 2 * kGroup * kHalf;
+      b0 += 2 * kGroup * kHalf;
+      next_half += 2 * kGroup;
+    }
+    const std::integral_constant<int, 0> none;
+#pragma unroll 1
+    for (; h < p.end; h += 2) {
+      half_block(h, h % STAGES, 0, 0, std::false_type(), none);
+      half_block(h + 1, (h + 1) % STAGES, 1, 0, std::false_type(), none);
+    }
+    // the next tile's first stages before the stores, which they would otherwise be waited for with
+    wait_vm<0>();
+    ready = second ? STAGES - 2 : STAGES - 1;  // (the second waves look one stage ahead)
+    drained = false;
+    const auto store = [&](auto* c, long long stride) {
+      typedef typename std::remove_pointer<decltype(c)>::type U;
+      constexpr int kPass = 64 / (int)sizeof(U);  // columns of C in 64 bytes
+      uint8_t* own = lds + L::kOut + wave * 2048;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+#pragma unroll
+        for (int e = 0; e < TN; e += kPass) {
+          const f32x16_t& v = acc[e / 32][i];
+          if constexpr (sizeof(U) == 2) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *(uint2*)(own + lr * 64 + ((q ^ x) * 16) + (lane >> 5) * 8) =
+                  make_uint2(pack_bf16(v[4 * q], v[4 * q + 1]), pack_bf16(v[4 * q + 2], v[4 * q + 3]));
+          } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              const int r = (e % 32 / 8 + q) * 4;
+              *(f32x4_t*)(own + lr * 64 + (((2 * q + (lane >> 5)) ^ x) * 16)) = f32x4_t{v[r], v[r + 1], v[r + 2], v[r + 3]};
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int r = k * 16 + lane / 4, row = p.m0 + wm + i * 32 + r, col = p.n0 + wn + e + (lane & 3) * (kPass / 4);
+            const u32x4_t out = *(const u32x4_t*)(own + r * 64 + (((lane & 3) ^ (r / 4 % 4)) * 16));
+            if (row < g.m && col < g.n) store_bytes(c + row * stride + col, g.n - col, out);
+          }
+        }
+      }
+    };
+    if (plan.splits > 1) store(plan.partial + (long long)p.split * g.m * g.n, (long long)g.n);
+    else store((T*)g.c, g.c_stride);
+  }
+  if (kApart && !second) barrier();
+  wait_vm<0>();
 }
 
 // The parts of a split product added in their order.
@@ -327,57 +574,98 @@ __global__ __launch_bounds__(256) void matmul_add_kernel(MatmulArgs g, const flo
 template <typename T, int MT>
 void rows_form(const MatmulArgs& g, hipStream_t st) {
   const int groups = ((g.k + kStep - 1) / kStep + kGroup - 1) / kGroup;
-  const int waves = groups < 2 ? 1 : groups < 4 ? 2 : groups < 16 ? 4 : groups < 48 ? 8 : 16;
+  const int rounds = (groups + 7) / 8, waves = (groups + rounds - 1) / rounds;  // up to eight, all with as many groups
   const int bytes = waves * MT * 1024;
   matmul_rows_kernel<T, MT><<<(g.n + 15) / 16, waves * 64, bytes, st>>>(g);
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, int ST>
 void tile_form(const MatmulArgs& g, TilePlan plan, hipStream_t st) {
   plan.tiles_m = (g.m + BM - 1) / BM;
   plan.tiles_n = (g.n + BN - 1) / BN;
   plan.group_m = 4;
-  static const hipError_t raised = hipFuncSetAttribute((const void*)matmul_tile_kernel<T, BM, BN, WM, WN>,
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, tile_bytes<BM, BN>());
+  static const hipError_t raised = hipFuncSetAttribute((const void*)matmul_tile_kernel<T, BM, BN, WM, WN, ST>,
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, (TileLds<BM, BN, ST>::kBytes + WM * WN * 2048));
   (void)raised;
-  matmul_tile_kernel<T, BM, BN, WM, WN><<<(unsigned)plan.tiles_m * plan.tiles_n * plan.splits, WM * WN * 64, tile_bytes<BM, BN>(), st>>>(g, plan);
+  matmul_tile_kernel<T, BM, BN, WM, WN, ST><<<std::min((unsigned)plan.tiles_m * plan.tiles_n * plan.splits, (unsigned)(kComputeUnits * (163840 / (TileLds<BM, BN, ST>::kBytes + WM * WN * 2048)))), WM * WN * 64, (TileLds<BM, BN, ST>::kBytes + WM * WN * 2048), st>>>(g, plan);
   if (plan.splits > 1) {
     const long long count = (long long)g.m * ((g.n + 3) / 4);
     matmul_add_kernel<T><<<(unsigned)((count + 255) / 256), 256, 0, st>>>(g, plan.partial, plan.splits);
   }
 }
 
-// Parts of k for products with too few 128 x 128 tiles.
-int plan_splits(int m, int n, int k) {
-  if (m <= 64) return 1;
-  const long long tiles = (long long)((m + 127) / 128) * ((n + 127) / 128);
+// ---- which form ------------------------------------------------------------------------------------------------------------------
+// Up to 16 rows: the stream of B.  Else the form that a model of its time says is the fastest.  A tile's time is its half
+// blocks' times what an iteration takes, from measurements (k = 4096, us an iteration; few / all compute units at work):
+//   256 x 256  0.57 / 0.84 (power)   128 x 128  0.26 / 0.34   64 x 64  0.147 / 0.147 (rate of L2)   fp32: 128 x 128  0.30 / 0.44
+// A tile's start and end cost about 3 us; parts of k cost a second launch and the traffic of the parts; the stream of B takes 2.6 us for a
+// group of four blocks and 16 rows on each of a compute unit's eight waves, and 2 us more for each further 16 rows.
+// 512 x 4096 x 4096: 64-tiles 21.1, 128-tiles 20.3; 1024 x 11008 x 4096: 128-tiles 66.7, 256-tiles 55.4; 32 x 12288 x 4096: the stream of B 24.6,
+// 64-tiles 13.2.
+enum Form { kRows, kTile64, kTile128, kTile256 };
+struct Choice {
+  Form form;
+  int splits, groups;  // parts of k, groups of four blocks each
+};
+constexpr size_t kMostScratch = 32u << 20;
+Choice choose(int m, int n, int k, bool exact, size_t scratch) {
   const int groups = ((k + kStep - 1) / kStep + kGroup - 1) / kGroup;
-  int splits = 1;
-  while (tiles * splits * 2 <= 256 && splits * 4 <= groups && splits < 8) splits *= 2;
-  while (splits > 1 && (long long)splits * m * n * 4 > (32 << 20)) splits /= 2;
-  return splits;
+  if (m <= 16) return {kRows, 1, groups};
+  Choice best = {kTile128, 1, groups};
+  double least = 1e30;
+  if (m <= 64) {
+    const double rounds = ceil((n + 15) / 16 / (double)kComputeUnits);
+    least = 3 + rounds * (1.5 + ((groups + 7) / 8) * (0.6 + 2.0 * ((m + 15) / 16)));
+    best.form = kRows;
+  }
+  const struct { Form form; int edge; double few, all; } forms[] = {
+      {kTile64, 64, exact ? 0.23 : 0.147, exact ? 0.36 : 0.147}, {kTile128, 128, exact ? 0.30 : 0.26, exact ? 0.44 : 0.34}, {kTile256, 256, 0.57, 0.84}};
+  for (const auto& f : forms) {
+    if (exact && f.form == kTile256) continue;  // (its converted operands do not fit the registers)
+    const double tiles = ceil(m / (double)f.edge) * ceil(n / (double)f.edge);
+    for (int want = 1; want <= 8 && want <= groups; want *= 2) {
+      const int per = (groups + want - 1) / want, splits = (groups + per - 1) / per;  // no empty parts
+      const double parts = splits > 1 ? (double)splits * m * n * 4 : 0;
+      if (parts > (double)scratch) break;
+      const double t = f.few + (f.all - f.few) * fmin(1.0, tiles * splits / kComputeUnits);
+      const double us = 3 + ceil(tiles * splits / kComputeUnits) * (3 + 2 * kGroup * (double)per * t) + (splits > 1 ? 2.5 + 2 * parts / 4e6 : 0);
+      if (us < least) {
+        least = us;
+        best = {f.form, splits, per};
+      }
+    }
+  }
+  return best;
 }
 
 template <typename T>
 void matmul(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t st) {
-  if (g.m <= 16) return rows_form<T, 1>(g, st);
-  if (g.m <= 32) return rows_form<T, 2>(g, st);
-  if (g.m <= 64) return rows_form<T, 4>(g, st);
-  const int groups = ((g.k + kStep - 1) / kStep + kGroup - 1) / kGroup;
+  constexpr bool kExact = sizeof(T) == 4;
+  Choice c = choose(g.m, g.n, g.k, kExact, kMostScratch);
+  // (without the room that was asked for: no parts)
+  if (c.splits > 1 && (!workspace || workspace_bytes < matmul_workspace(g.m, g.n, g.k))) c = choose(g.m, g.n, g.k, kExact, 0);
+  if (c.form == kRows) {
+    if (g.m <= 16) return rows_form<T, 1>(g, st);
+    if (g.m <= 32) return rows_form<T, 2>(g, st);
+    if (g.m <= 48) return rows_form<T, 3>(g, st);
+    return rows_form<T, 4>(g, st);
+  }
   TilePlan plan = {};
-  plan.splits = workspace && workspace_bytes >= matmul_workspace(g.m, g.n, g.k) ? plan_splits(g.m, g.n, g.k) : 1;
-  plan.groups = (groups + plan.splits - 1) / plan.splits;
-  plan.splits = (groups + plan.groups - 1) / plan.groups;  // no empty parts
+  plan.splits = c.splits;
+  plan.groups = c.groups;
   plan.partial = (float*)workspace;
-  const long long large = (long long)((g.m + 255) / 256) * ((g.n + 255) / 256);
-  if (std::is_same<T, bf16_t>::value && large >= 256) return tile_form<T, 256, 256, 2, 4>(g, plan, st);
-  tile_form<T, 128, 128, 2, 2>(g, plan, st);
+  if constexpr (!kExact) {
+    if (c.form == kTile256) return tile_form<T, 256, 256, 2, 4, 4>(g, plan, st);
+  }
+  if (c.form == kTile64) return tile_form<T, 64, 64, 2, 2, 4>(g, plan, st);
+  tile_form<T, 128, 128, 2, 2, 4>(g, plan, st);
 }
 
 }  // namespace
 
 size_t matmul_workspace(int m, int n, int k) {
-  const int splits = plan_splits(m, n, k);
+  int splits = 1;  // the most of either type of C
+  for (const bool exact : {false, true}) splits = std::max(splits, choose(m, n, k, exact, kMostScratch).splits);
   return splits > 1 ? (size_t)splits * m * n * 4 : 0;
 }
 
