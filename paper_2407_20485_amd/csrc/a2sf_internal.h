@@ -175,17 +175,19 @@ struct RotaryPart {
   const void* x;
   void* y;
   long long x_stride[3], y_stride[3];  // batch, position, head
-  int rotate, in_place;
+  int heads, rotate, in_place;
+  int lanes, tokens_per_block;  // set by the launcher
 };
 struct RotaryArgs {
   RotaryPart part[A2SF_MAX_ROTARY_PARTS];
-  int first_head[A2SF_MAX_ROTARY_PARTS + 1];  // heads of all parts in a row; the unused end repeats the total
-  int heads, batch, length, d, rot, inverse;
+  int parts, batch, length, d, rot, inverse;
   const int32_t* pos;
   long long pos_stride;
   const float* table;
   int table_rows;
-  int items, lanes, tokens_per_block;  // set by the launcher
+  // set by the launcher
+  int turning, items;
+  uint32_t first_block[A2SF_MAX_ROTARY_PARTS];
 };
 void launch_rotary(RotaryArgs a, int dtype, bool neighbours, hipStream_t st);
 struct RotaryTableArgs {

@@ -174,20 +174,18 @@ a2sf_status a2sf_rotary(const a2sf_rotary_part* parts, int32_t n_parts, int32_t 
   if (pairs != A2SF_ROTARY_HALVES && pairs != A2SF_ROTARY_NEIGHBOURS) return A2SF_EINVAL;
   if (batch < 1 || length < 1 || d < 1 || d > 512 || table_rows < 1) return A2SF_ESHAPE;
   if (rotary_dims < 2 || rotary_dims % 2 != 0 || rotary_dims > d) return A2SF_ESHAPE;
-  if ((long long)batch * length > 0x7FFFFFFFLL) return A2SF_ESHAPE;
+  if ((long long)batch * length > 0x0FFFFFFFLL) return A2SF_ESHAPE;
   if (batch > 1 && pos_stride < length) return A2SF_ESHAPE;
   if (!pos || !table || misaligned(pos, 4) || misaligned(table, 4)) return A2SF_EINVAL;
   RotaryArgs a = {};
-  long long heads = 0;
-  for (int i = 0; i < A2SF_MAX_ROTARY_PARTS; ++i) {
-    a.first_head[i] = (int)heads;
-    if (i >= n_parts) continue;
+  for (int i = 0; i < n_parts; ++i) {
     const a2sf_rotary_part& p = parts[i];
     if (!p.x || !p.y || misaligned(p.x, size_of(dtype)) || misaligned(p.y, size_of(dtype))) return A2SF_EINVAL;
-    if (p.heads < 1) return A2SF_ESHAPE;
+    if (p.heads < 1 || p.heads > 0xFFFFFF) return A2SF_ESHAPE;
     RotaryPart& to = a.part[i];
     to.x = p.x;
     to.y = p.y;
+    to.heads = p.heads;
     to.in_place = p.x == p.y;
     to.rotate = p.rotate != 0;
     for (int j = 0; j < 3; ++j) {
@@ -198,12 +196,8 @@ a2sf_status a2sf_rotary(const a2sf_rotary_part* parts, int32_t n_parts, int32_t 
       if (count > 1 && p.x_stride[j] != p.y_stride[j]) to.in_place = 0;
     }
     if (p.x == p.y && !to.in_place) return A2SF_EINVAL;  // elements would be overwritten before they are read
-    heads += p.heads;
-    if (heads > 0xFFFFFF) return A2SF_ESHAPE;
   }
-  a.first_head[A2SF_MAX_ROTARY_PARTS] = (int)heads;
-  for (int i = n_parts; i < A2SF_MAX_ROTARY_PARTS; ++i) a.first_head[i] = (int)heads;
-  a.heads = (int)heads;
+  a.parts = n_parts;
   a.batch = batch;
   a.length = length;
   a.d = d;

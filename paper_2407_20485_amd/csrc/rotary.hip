@@ -7,100 +7,147 @@
 namespace a2sf {
 namespace {
 
-template <typename T, int W> struct Chunk;  // W consecutive elements
-template <typename T> struct Chunk<T, 8> {
-  float f[8];
-  __device__ __forceinline__ void load(const T* p) { load_unit(p, f); }
-  __device__ __forceinline__ void store(T* p) const { store_unit(p, f); }
-};
-template <typename T> struct Chunk<T, 1> {
-  float f[1];
-  __device__ __forceinline__ void load(const T* p) { f[0] = load_one(p); }
-  __device__ __forceinline__ void store(T* p) const { store_one(p, f[0]); }
-};
-
-// An item is what a lane reads before it writes: with halves W elements of the first half of the turned part and the W of the
-// second that they pair with, with neighbours 2 W elements, behind the turned part 2 W elements as they are (W where an odd
-// one is left).  A lane keeps its item's cosines and sines and goes through the heads.  Items read and write their own elements only,
-// so a part may be turned in place.
-// W = 8 where the item's parts are whole units of eight (any stride and alignment), W = 1 else.
-template <typename T, int W, bool NEIGHBOURS>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
-  const int local = threadIdx.x;
-  const long long token = (long long)blockIdx.x * a.tokens_per_block + local / a.lanes;
-  const int lane = local % a.lanes;
-  if (local >= a.tokens_per_block * a.lanes || token >= (long long)a.batch * a.length) return;
-  const int item = lane % a.items, head_step = a.lanes / a.items;
-  int head = lane / a.items;
-  if (head >= head_step) return;  // lanes past the last whole head
-  const int b = (int)(token / a.length), i = (int)(token - (long long)b * a.length);
-  const int half = a.rot / 2;
-  const int pairs = half / W;  // items that turn
-  const bool turns = item < pairs;
-  // first elements of the item's two parts
-  int e0, e1;
-  bool two = true;
-  if (turns) {
-    e0 = NEIGHBOURS ? 2 * item * W : item * W;
-    e1 = NEIGHBOURS ? e0 + W : half + e0;
-  } else {
-    e0 = a.rot + 2 * (item - pairs) * W;
-    e1 = e0 + W;
-    two = e1 + W <= a.d;
-  }
-  float c[W], s[W];
-  bool known = true;
-  if (turns) {
-    const int32_t p = a.pos[b * a.pos_stride + i];
-    known = p >= 0 && p < a.table_rows;
-    const float* row = a.table + (long long)(known ? p : 0) * a.rot + item * W;
+// Sixteen bytes of neighbouring elements, or fewer of them
+template <typename T>
+struct Chunk {
+  static constexpr int kCount = 16 / (int)sizeof(T);
+  float f[kCount];
+  __device__ __forceinline__ void load(const T* p, int have) {
+    if (have >= kCount) {
+      const u32x4_t r = *(const u32x4_at2_t*)p;
+      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      c[j] = row[j];
-      s[j] = row[half + j];
-      if (a.inverse) s[j] = -s[j];
-    }
-  }
-  int part = 0;
-  for (; head < a.heads; head += head_step) {
-    while (head >= a.first_head[part + 1]) ++part;
-    const int h = head - a.first_head[part];
-    const RotaryPart& P = a.part[part];
-    const T* x = (const T*)P.x + b * P.x_stride[0] + i * P.x_stride[1] + h * P.x_stride[2];
-    T* y = (T*)P.y + b * P.y_stride[0] + i * P.y_stride[1] + h * P.y_stride[2];
-    if (!(turns && P.rotate) && P.in_place) continue;
-    Chunk<T, W> u, v;
-    u.load(x + e0);
-    if (two) v.load(x + e1);
-    if (turns && P.rotate) {
-      if (NEIGHBOURS && W > 1) {
-        // pairs (0, 1) (2, 3) ... of the 2 W elements
-        float z[2 * W];
-#pragma unroll
-        for (int j = 0; j < W; ++j) { z[j] = u.f[j]; z[W + j] = v.f[j]; }
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-          const float p = z[2 * j], q = z[2 * j + 1];
-          z[2 * j] = p * c[j] - q * s[j];
-          z[2 * j + 1] = q * c[j] + p * s[j];
-        }
-#pragma unroll
-        for (int j = 0; j < W; ++j) { u.f[j] = z[j]; v.f[j] = z[W + j]; }
+        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(r[i]);
       } else {
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-          const float p = u.f[j], q = v.f[j];
-          u.f[j] = p * c[j] - q * s[j];
-          v.f[j] = q * c[j] + p * s[j];
+        for (int i = 0; i < 4; ++i) {
+          f[2 * i] = __uint_as_float(r[i] << 16);
+          f[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
         }
       }
-      if (!known) {
-#pragma unroll
-        for (int j = 0; j < W; ++j) u.f[j] = v.f[j] = __uint_as_float(0x7FC00000u);
-      }
+      return;
     }
-    u.store(y + e0);
-    if (two) v.store(y + e1);
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) f[i] = i < have ? load_one(p + i) : 0.f;
+  }
+  __device__ __forceinline__ void store(T* p, int have) const {
+    if (have >= kCount) {
+      u32x4_t r;
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(f[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+      }
+      *(u32x4_at2_t*)p = r;
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kCount; ++i)
+      if (i < have) store_one(p + i, f[i]);
+  }
+};
+
+// An item is what a lane reads before it writes: with halves 16 bytes of the first half of the turned part and the 16 of the
+// second that they pair with, with neighbours 16 bytes, and 16 bytes behind the turned part as they are; so the lanes of a head
+// read its elements in one row.  A workgroup takes some tokens of one part (its strides are then scalar), a lane one item of
+// up to kHeads heads, with the item's cosines and sines: all of them are read before the first is written.  Items read and write
+// their own elements only, so a part may be turned in place.  Any stride and alignment; WHOLE: no item is shorter than 16 bytes.
+// 8 x 2048 tokens of 96 heads of 128 in bf16 (805 MB): halves 156 us = 5.2 TB/s, neighbours 150 = 5.4 (a copy of 1 GiB: 5.2).  With one item of all
+// parts' heads in turn per lane, whose strides are then looked up lane by lane, 165 and 181.
+constexpr int kHeads = 4;
+
+template <typename T, bool NEIGHBOURS, bool WHOLE>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
+  constexpr int W = Chunk<T>::kCount, kTable = NEIGHBOURS ? W / 2 : W;
+  int part = 0;
+#pragma unroll
+  for (int k = 1; k < A2SF_MAX_ROTARY_PARTS; ++k) part += blockIdx.x >= a.first_block[k];
+  const RotaryPart& P = a.part[part];
+  const int local = threadIdx.x;
+  const long long token = (long long)(blockIdx.x - a.first_block[part]) * P.tokens_per_block + local / P.lanes;
+  const int lane = local % P.lanes;
+  if (local >= P.tokens_per_block * P.lanes || token >= (long long)a.batch * a.length) return;
+  const int item = lane % a.items, head_step = P.lanes / a.items;
+  const int b = (int)(token / a.length), i = (int)(token - (long long)b * a.length);
+  const int half = a.rot / 2;
+  const bool turns = item < a.turning;
+  if (!(turns && P.rotate) && P.in_place) return;
+  // the item's elements: `have` from e0 on, with halves as many from e1 on
+  int e0, e1 = 0, have;
+  if (!turns) {
+    e0 = a.rot + (item - a.turning) * W;
+    have = a.d - e0;
+  } else if (NEIGHBOURS) {
+    e0 = item * W;
+    have = a.rot - e0;
+  } else {
+    e0 = item * W;
+    e1 = half + e0;
+    have = half - e0;
+  }
+  if (WHOLE) have = W;
+  const bool two = !NEIGHBOURS && turns;
+  const T* x = (const T*)P.x + b * P.x_stride[0] + i * P.x_stride[1];
+  T* y = (T*)P.y + b * P.y_stride[0] + i * P.y_stride[1];
+  float c[kTable], s[kTable];
+  bool known = true;
+  if (turns && P.rotate) {
+    const int32_t p = a.pos[b * a.pos_stride + i];
+    known = p >= 0 && p < a.table_rows;
+    const int first = item * kTable;
+    const float* row = a.table + (long long)(known ? p : 0) * a.rot + first;
+#pragma unroll
+    for (int j = 0; j < kTable; ++j) {
+      const bool there = WHOLE || first + j < half;
+      c[j] = there ? row[j] : 0.f;
+      s[j] = there ? row[half + j] : 0.f;
+    }
+    if (a.inverse)
+#pragma unroll
+      for (int j = 0; j < kTable; ++j) s[j] = -s[j];
+  }
+  const int h0 = lane / a.items;
+  for (int head = h0; head < P.heads; head += kHeads * head_step) {
+    Chunk<T> u[kHeads], v[kHeads];
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) {
+      const int h = head + k * head_step;
+      if (h >= P.heads) break;
+      const T* from = x + h * P.x_stride[2];
+      u[k].load(from + e0, have);
+      if (two) v[k].load(from + e1, have);
+    }
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) {
+      const int h = head + k * head_step;
+      if (h >= P.heads) break;
+      if (turns && P.rotate) {
+        if constexpr (NEIGHBOURS) {
+#pragma unroll
+          for (int j = 0; j < W / 2; ++j) {
+            const float p = u[k].f[2 * j], q = u[k].f[2 * j + 1];
+            u[k].f[2 * j] = p * c[j] - q * s[j];
+            u[k].f[2 * j + 1] = q * c[j] + p * s[j];
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < W; ++j) {
+            const float p = u[k].f[j], q = v[k].f[j];
+            u[k].f[j] = p * c[j] - q * s[j];
+            v[k].f[j] = q * c[j] + p * s[j];
+          }
+        }
+        if (!known) {
+#pragma unroll
+          for (int j = 0; j < W; ++j) u[k].f[j] = v[k].f[j] = __uint_as_float(0x7FC00000u);
+        }
+      }
+      T* to = y + h * P.y_stride[2];
+      u[k].store(to + e0, have);
+      if (two) v[k].store(to + e1, have);
+    }
   }
 }
 
@@ -127,31 +174,39 @@ __global__ __launch_bounds__(256) void rotary_table_kernel(RotaryTableArgs a) {
   a.table[(long long)p * a.rot + half + i] = (float)(sn * a.magnitude);
 }
 
-template <typename T, int W>
-void rotary(const RotaryArgs& a, uint32_t grid, bool neighbours, hipStream_t st) {
-  if (neighbours) rotary_kernel<T, W, true><<<grid, 256, 0, st>>>(a);
-  else rotary_kernel<T, W, false><<<grid, 256, 0, st>>>(a);
+template <typename T>
+void rotary(RotaryArgs a, bool neighbours, hipStream_t st) {
+  constexpr int W = Chunk<T>::kCount;
+  const int turned = neighbours ? a.rot : a.rot / 2;
+  a.turning = (turned + W - 1) / W;
+  a.items = a.turning + (a.d - a.rot + W - 1) / W;
+  const bool whole = turned % W == 0 && (a.d - a.rot) % W == 0;
+  const long long tokens = (long long)a.batch * a.length;
+  uint32_t grid = 0;
+  for (int k = 0; k < A2SF_MAX_ROTARY_PARTS; ++k) {
+    a.first_block[k] = k < a.parts ? grid : 0xFFFFFFFFu;
+    if (k >= a.parts) continue;
+    // as many lanes for a token as have kHeads heads each, fewer where a workgroup has no more; several tokens per workgroup
+    RotaryPart& P = a.part[k];
+    const long long want = (long long)((P.heads + kHeads - 1) / kHeads) * a.items;
+    P.lanes = want < 256 ? (int)want : 256 / a.items * a.items;
+    P.tokens_per_block = 256 / P.lanes;
+    grid += (uint32_t)((tokens + P.tokens_per_block - 1) / P.tokens_per_block);
+  }
+  if (neighbours) {
+    if (whole) rotary_kernel<T, true, true><<<grid, 256, 0, st>>>(a);
+    else rotary_kernel<T, true, false><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (whole) rotary_kernel<T, false, true><<<grid, 256, 0, st>>>(a);
+    else rotary_kernel<T, false, false><<<grid, 256, 0, st>>>(a);
+  }
 }
 
 }  // namespace
 
 void launch_rotary(RotaryArgs a, int dtype, bool neighbours, hipStream_t st) {
-  const bool wide = a.rot % 16 == 0 && a.d % 16 == 0;
-  const int W = wide ? 8 : 1;
-  a.items = a.rot / 2 / W + (a.d - a.rot + 2 * W - 1) / (2 * W);
-  // A token's heads over as many lanes as there are, up to a workgroup; several tokens per workgroup where they are fewer.
-  const int want = a.heads * a.items;
-  a.lanes = want < 256 ? want : 256 / a.items * a.items;
-  a.tokens_per_block = 256 / a.lanes;
-  const long long tokens = (long long)a.batch * a.length;
-  const uint32_t grid = (uint32_t)((tokens + a.tokens_per_block - 1) / a.tokens_per_block);
-  if (dtype == A2SF_F32) {
-    if (wide) rotary<float, 8>(a, grid, neighbours, st);
-    else rotary<float, 1>(a, grid, neighbours, st);
-  } else {
-    if (wide) rotary<bf16_t, 8>(a, grid, neighbours, st);
-    else rotary<bf16_t, 1>(a, grid, neighbours, st);
-  }
+  if (dtype == A2SF_F32) rotary<float>(a, neighbours, st);
+  else rotary<bf16_t>(a, neighbours, st);
 }
 
 void launch_rotary_table(const RotaryTableArgs& a, hipStream_t st) {
