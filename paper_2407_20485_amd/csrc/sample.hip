@@ -18,7 +18,7 @@
 //
 // A workgroup of 1024 lanes takes a row.  Few rows are a chain of passes and barriers whose instructions are mostly fetched for the first
 // time: what counts is little code, so passes are loops that read the row again (from the caches) instead of unrolled ones over
-// registers (32 000 logits in fp32: 17 us, 24 with the row in registers), and one function serves counts and masses.
+// registers (32 000 logits in fp32, all filters: 14 us, 24 with the row in registers; 256 rows of 50 272 in bf16, top-p and min-p: 43 us), and one function serves counts and masses.
 #include "a2sf_internal.h"
 #include "rows_dev.h"
 
@@ -137,31 +137,38 @@ struct List {
   SampleShared& s;
   int n;
   int count = 0;  // of this wave
-  // a unit's tokens that `which` has a bit for, one of each lane at a time: most units have none, few lanes have two
-  template <typename U, typename L>
-  __device__ __forceinline__ void add(uint32_t which, const U& u, int first, L logit) {
+  // Tokens are noted as bits, one of each lane's elements after the other, the newest lowest; 32 at a time they go to the list: one of each
+  // lane per turn, their indices first.
+  uint32_t bits = 0;
+  int noted = 0, group = 0;  // units in `bits`, the first one's first element
+  __device__ __forceinline__ void flush() {
     unsigned long long who;
-    while ((who = __ballot(which != 0)) != 0) {
+    while ((who = __ballot(bits != 0)) != 0) {
       const int to = count + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
-      const int j = __builtin_ctz(which | 256u);
-      float l = u.at(0);
-#pragma unroll
-      for (int i = 1; i < kUnit; ++i) l = j == i ? u.at(i) : l;
-      if (which && to < kListed) {
-        s.list[threadIdx.x >> 6][to] = logit(l);
-        s.list_index[threadIdx.x >> 6][to] = first + j;
-      }
-      which &= which - 1;
+      const int top = 31 - __builtin_clz(bits | 1u), element = noted * kUnit - 1 - top;
+      if (bits && to < kListed)
+        s.list_index[threadIdx.x >> 6][to] = group + element / kUnit * (kSampleThreads * kUnit) + element % kUnit;
+      bits &= ~(1u << top);
       count += __popcll(who);
     }
+    noted = 0;
+  }
+  // after a unit's bits have gone in
+  __device__ __forceinline__ void unit_done(int first) {
+    if (noted == 0) group = first;
+    if (++noted == 32 / kUnit) flush();
   }
   template <typename F>
   __device__ __forceinline__ void each(F f) const {
     for (int i = threadIdx.x & 63; i < count; i += 64) f(s.list[threadIdx.x >> 6][i], s.list_index[threadIdx.x >> 6][i]);
   }
-  // after the last add: whether all waves had room
-  __device__ __forceinline__ bool complete() {
+  // after the last unit: fetches the listed logits; whether all waves had room
+  template <typename R>
+  __device__ __forceinline__ bool complete(const R& row) {
+    flush();
     if (count > kListed) s.overflow = 1;
+    const int wave = threadIdx.x >> 6;
+    for (int i = threadIdx.x & 63; i < min(count, kListed); i += 64) s.list[wave][i] = row.logit(load_one(row.p + s.list_index[wave][i]));
     __syncthreads();
     return !s.overflow;
   }
@@ -199,15 +206,26 @@ __device__ __forceinline__ uint32_t block_sum_u32(uint32_t v, uint32_t* left) {
   return of_waves(left, OpSumI());
 }
 
-// The distance below the largest logit in octaves of probability, its weight, its bin
+// The distance below the largest logit in octaves of probability, its weight; its bin
 struct Scale {
-  float top, per;  // largest logit; octaves per unit of logit (log2(e) / temperature)
+  float top, per;         // largest logit; octaves per unit of logit (log2(e) / temperature)
+  float first, bins_per;  // the bins: from this logit down, so many per unit of logit
   __device__ __forceinline__ float below(float l) const { return (top - l) * per; }
+  // (of -infinity: the last; of NaN: some)
+  __device__ __forceinline__ int bin(float l) const {
+    return (int)fminf(fmaxf((first - l) * bins_per, 0.f), (float)(kBins - 1));
+  }
+  // bins over the whole row, by probability
+  __device__ __forceinline__ Scale over_row() const { return {top, per, top, per * kBinsPerOctave}; }
+  // ... over the logits from `high` to `low`
+  __device__ __forceinline__ Scale over(float high, float low) const {
+    high = fminf(high, top);
+    const float range = high - low;
+    return {top, per, high, range > 0.f && range < 1e30f ? fminf((float)(kBins - 1) / range, 1e30f) : per * kBinsPerOctave};
+  }
 };
 __device__ __forceinline__ float weight(float below) { return __builtin_amdgcn_exp2f(-below); }
 __device__ __forceinline__ uint32_t mass_of(float below) { return (uint32_t)rintf(weight(below) * 2147483648.f); }
-// (of -infinity and NaN: 0, and the last bin)
-__device__ __forceinline__ int bin_of(float below) { return (int)fminf(below * kBinsPerOctave, (float)(kBins - 1)); }
 
 // What is looked for: the token at which the count (by_mass: the mass) reaches a number
 struct Target {
@@ -280,9 +298,8 @@ __device__ __forceinline__ void fill_bins(const R& row, const Scale& sc, SampleS
   uint32_t far_count = 0;
   unsigned long long far_mass = 0;
   row.each([&](float l, int) {
-    const float below = sc.below(l);
-    const int bin = bin_of(below);
-    const uint32_t m = mass_of(below);
+    const int bin = sc.bin(l);
+    const uint32_t m = mass_of(sc.below(l));
     if (bin < kBins - 1) {
       atomicAdd(&s.count[bin], 1u);
       atomicAdd(&s.mass[bin], (unsigned long long)m);
@@ -311,7 +328,7 @@ __device__ __forceinline__ bool cut_in_bin(const R& row, const Scale& sc, Sample
     // Too many: split the range of their keys, 10 bits at a time
     uint32_t lo = 0xFFFFFFFFu, hi = 0;
     row.each([&](float l, int) {
-      if (l > -kInf && bin_of(sc.below(l)) == bin) {
+      if (l > -kInf && sc.bin(l) == bin) {
         const uint32_t key = ordered_key(l);
         lo = min(lo, key);
         hi = max(hi, key);
@@ -373,7 +390,7 @@ __device__ __forceinline__ bool cut_in_bin(const R& row, const Scale& sc, Sample
   row.each([&](float l, int at) {
     const float below = sc.below(l);
     const uint32_t key = ordered_key(l);
-    if (l > -kInf && (low > high ? bin_of(below) == bin : key >= low && key <= high)) {
+    if (l > -kInf && (low > high ? sc.bin(l) == bin : key >= low && key <= high)) {
       const uint32_t slot = atomicAdd(&s.ranked, 1u);  // in any order: the ranks below do not depend on it
       s.rank[slot] = l;
       s.rank_index[slot] = at;
@@ -390,13 +407,12 @@ __device__ __forceinline__ bool cut_in_bin(const R& row, const Scale& sc, Sample
   if (mine < (int)members) {
     const float l = s.rank[mine];
     const int at = s.rank_index[mine];
-#pragma unroll 2
+#pragma unroll 4
     for (int j = t & (share - 1); j < (int)members; j += share) {
       const float o = s.rank[j];
-      if (o > l || (o == l && s.rank_index[j] < at)) {
-        ++c;
-        m += s.rank_mass[j];
-      }
+      const bool ahead = o > l || (o == l && s.rank_index[j] < at);
+      c += ahead;
+      m += ahead ? s.rank_mass[j] : 0u;
     }
   }
   for (int by = 1; by < share; by *= 2) {
@@ -465,7 +481,7 @@ __device__ __forceinline__ bool find_zone_cut(const R& row, const Scale& sc, con
     });
   } else {
     row.each([&](float l, int) {
-      const int bin = bin_of(sc.below(l));
+      const int bin = sc.over_row().bin(l);
       if (bin < kBins - 1) atomicAdd(&s.count[bin], 1u);
     });
   }
@@ -496,7 +512,6 @@ __device__ __forceinline__ bool find_zone_cut(const R& row, const Scale& sc, con
   unsigned long long above = 0, all = 0;
   uint32_t count = 0;
   row.each_unit([&](const auto& u, int first) {
-    uint32_t zone = 0;
 #pragma unroll
     for (int j = 0; j < kUnit; ++j) {
       const float l = u.at(j);
@@ -505,9 +520,9 @@ __device__ __forceinline__ bool find_zone_cut(const R& row, const Scale& sc, con
       all += m;
       above += over ? m : 0u;
       count += over;
-      zone |= l >= low && !over ? 1u << j : 0u;
+      list.bits = 2 * list.bits + (l >= low && !over);
     }
-    list.add(zone, u, first, [](float l) { return l; });
+    list.unit_done(first);
   });
   uint32_t c = count, none = 0;
   wave_scan(c, above);
@@ -518,7 +533,7 @@ __device__ __forceinline__ bool find_zone_cut(const R& row, const Scale& sc, con
     s.wave64[threadIdx.x >> 6] = above;
     s.wave64b[threadIdx.x >> 6] = all;
   }
-  if (!list.complete()) return false;
+  if (!list.complete(row)) return false;
   c = of_waves(s.wave32, OpSumI());
   above = s.wave64[threadIdx.x & 15];
   all = s.wave64b[threadIdx.x & 15];
@@ -538,10 +553,11 @@ __device__ __forceinline__ bool find_zone_cut(const R& row, const Scale& sc, con
   all = last_of_row(all);
   s_above = c;
   to = {by_mass, (uint32_t)f.k, by_mass ? mass_for(f.p, inside ? inside : all) : 0};
-  fill_bins(list, sc, s);
+  const Scale zone = sc.over(high, low);
+  fill_bins(list, zone, s);
   scan_bins(s, to, c, above);
   if (s.bin < 0) return !by_mass && c < to.tokens && low < -3e38f ? (s.cut = -kInf, s.kept_mass = all, true) : false;
-  cut_in_bin(list, sc, s, to);
+  cut_in_bin(list, zone, s, to);
   return true;
 }
 
@@ -564,6 +580,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
   const int t = threadIdx.x;
   const long long r = blockIdx.x;
   Scale sc;
+  sc.first = sc.bins_per = 0.f;
   sc.top = TOP_IS_INF ? 0.f : top;
   sc.per = greedy ? 1.f : fminf(1.44269504088896340736f / temperature, 1e30f);  // (0 times it stays 0)
   const float* noise = a.noise && !greedy ? a.noise + r * a.noise_stride : nullptr;
@@ -572,17 +589,17 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
   Runner run;
   List list{s, a.n};
   bool listed = false;
+  const float least = fmaxf(low, -3.402823466e38f);  // (no -infinity)
   if (!TOP_IS_INF && f.k > 0 && f.k <= 512) {
     row.each_unit([&](const RawUnit<T>& u, int first) {
-      uint32_t which = 0;
 #pragma unroll
-      for (int j = 0; j < kUnit; ++j) which |= u.at(j) >= low && u.at(j) > -kInf ? 1u << j : 0u;
-      list.add(which, u, first, [](float l) { return l; });
+      for (int j = 0; j < kUnit; ++j) list.bits = 2 * list.bits + (u.at(j) >= least);
+      list.unit_done(first);
     });
-    listed = list.complete();
+    listed = list.complete(row);
   }
   if (listed) {
-    find_cut(list, sc, f, s);
+    find_cut(list, sc.over(kInf, least), f, s);
     const float cut = s.cut;
     const int cut_index = s.cut_index;
     list.each([&](float l, int at) {
@@ -606,7 +623,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
       if (!found) {
         __syncthreads();
         if (t == 0) s.cut = -kInf;
-        find_cut(row, sc, f, s);
+        find_cut(row, sc.over_row(), f, s);
       }
       ahead = found && above >= (uint32_t)a.n / 64 && !(min_p > 0.f);
     }
