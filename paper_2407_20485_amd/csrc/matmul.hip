@@ -146,11 +146,14 @@ __device__ __forceinline__ void store_bytes(T* p, int have, u32x4_t v) {
 // A workgroup takes 16 columns of C and all rows (MT tiles of 16), its waves share k in groups of four steps and add their parts
 // in LDS in a fixed order.  Bound by the stream of B; A comes from the caches.  The next group's part of B is on its way while the
 // present one is multiplied, and A is a step ahead.
+// Where rows of B lie a multiple of 4096 bytes apart, workgroups that all began at the same place of k would all ask the same few of the
+// caches' channels: each begins with another of its wave's groups.
+// 1 x 12288 x 4096: 10.3 us (4.9 TB/s; all from the first group: 12.8), 1 x 22016 x 4096: 17.1 us (5.3 TB/s; 21.5).
 template <typename T, int MT>
 __global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs g) {
   typedef typename Way<T>::type W;
   extern __shared__ f32x4_t part[];  // [waves][MT][64]
-  const int t = threadIdx.x, wave = t >> 6, lane = t & 63, waves = blockDim.x >> 6;
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, waves = blockDim.x >> 6;
   const int n0 = blockIdx.x * 16;
   const int steps = (g.k + kStep - 1) / kStep, groups = (steps + kGroup - 1) / kGroup;
   const int kl = (lane >> 4) * 16;  // and 64 on: an access takes 64 bytes of each of 16 rows
@@ -189,8 +192,13 @@ __global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs g) {
       for (int i = 0; i < MT; ++i) to[i] = join(load_chunk(g.a + a_at[i], s * kStep, g.k - kl), load_chunk(g.a + a_at[i], s * kStep + 64, g.k - kl));
     }
   };
-  if (wave < groups) load_b(bv, wave);
-  for (int group = wave; group < groups; group += waves) {
+  const int rounds = (groups + waves - 1) / waves, first = wave * rounds, last = min(first + rounds, groups) - 1;  // this wave's
+  int group = first + blockIdx.x / 8 % rounds;
+  if (group > last) group = first;
+  if (first <= last) load_b(bv, group);
+#pragma unroll 1
+  for (int left = last - first + 1; left > 0; --left) {
+    const int after = group == last ? first : group + 1;
     const int s0 = group * kGroup;
     const uint32_t b4 = *(const uint32_t*)(bs + s0);
     uint32_t a4[MT];
@@ -198,7 +206,7 @@ __global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs g) {
     for (int i = 0; i < MT; ++i) a4[i] = *(const uint32_t*)(g.a_scales + as_at[i] + s0);
     i32x8_t av[2][MT];
     load_a(av[0], s0);
-    if (group + waves < groups) load_b(bn, group + waves);
+    if (left > 1) load_b(bn, after);
 #pragma unroll
     for (int j = 0; j < kGroup; ++j) {
       if (j + 1 < kGroup) load_a(av[(j + 1) & 1], s0 + j + 1);  // (past the end of k: zeros)
@@ -212,6 +220,7 @@ __global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs g) {
     }
 #pragma unroll
     for (int j = 0; j < kGroup; ++j) bv[j] = bn[j];
+    group = after;
   }
 #pragma unroll
   for (int i = 0; i < MT; ++i) part[(wave * MT + i) * 64 + lane] = acc[i];
@@ -230,8 +239,10 @@ __global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs g) {
 // half blocks ahead.  Persistent: a workgroup goes from tile to tile and the stream of half blocks runs on across them.
 //
 // Eight waves: the two of a SIMD are half an iteration apart, with a barrier at each half: while one has the matrix pipe, the other
-// reads the fragments of its next half block and fetches.  (8192 x 8192 x 8192, all waves in step 490 us, so 461; the matrix pipe is busy
-// 58 % of the cycles and the chip at its power limit, 1.95 GHz.)  Four waves: two or more workgroups share a compute unit instead.
+// reads the fragments of its next half block and fetches.  (8192 x 8192 x 8192: all waves in step 490 us, so 461; with a group's half blocks
+// written out, which takes the questions about the end of the stream out of them, 440 = 2500 TFLOP/s, the chip at its power
+// limit.)  Four waves: the next half block's fragments are read while this one's are multiplied, and workgroups share a
+// compute unit.
 //
 // A row of a stage is 64 bytes, four chunks of 16; chunk c of row r lies at c ^ (r / 4 % 4): 16 lanes that read the same chunk of 16
 // rows then meet all 64 banks once.  The scales of four blocks of the tile's rows come the same way, a group ahead.  Results go through
@@ -574,7 +585,10 @@ __global__ __launch_bounds__(256) void matmul_add_kernel(MatmulArgs g, const flo
 template <typename T, int MT>
 void rows_form(const MatmulArgs& g, hipStream_t st) {
   const int groups = ((g.k + kStep - 1) / kStep + kGroup - 1) / kGroup;
-  const int rounds = (groups + 7) / 8, waves = (groups + rounds - 1) / rounds;  // up to eight, all with as many groups
+  // Up to eight waves, all with as many groups; up to four where there are two such workgroups for every compute unit (1 x 12288 x 4096:
+  // 10.3 us with four, with two groups each, 11.9 with two; 1 x 4096 x 11008: 11.7 with four, 10.6 with eight).
+  const int most = MT == 1 && g.n >= 2 * kComputeUnits * 16 ? 4 : 8;
+  const int rounds = (groups + most - 1) / most, waves = (groups + rounds - 1) / rounds;
   const int bytes = waves * MT * 1024;
   matmul_rows_kernel<T, MT><<<(g.n + 15) / 16, waves * 64, bytes, st>>>(g);
 }
