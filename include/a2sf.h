@@ -373,7 +373,7 @@ a2sf_status a2sf_quantize_weight(const a2sf_rows* w, int32_t n, int32_t k, int32
  *   c          out [m, n], c_dtype (A2SF_F32 or A2SF_BF16).
  *   workspace  may be NULL; with a2sf_matmul_workspace_bytes(m, n, k) bytes (0: none is of use) products that have too few
  *              tiles for the whole chip split their sums over k.  The same sizes with the same choice give the same bits.
- * Bytes of the rows past k are not used.  k <= 2^20. */
+ * Bytes of the rows past k are not used.  k <= 2^20, rows of a and b and rows of scales at most 2^23 bytes apart. */
 size_t a2sf_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
 a2sf_status a2sf_matmul_scaled(const a2sf_rows8* a, const a2sf_rows8* b, int32_t m, int32_t n, int32_t k,
                                const a2sf_rows* c, int32_t c_dtype, void* workspace, size_t workspace_bytes,

@@ -146,7 +146,10 @@ a2sf_status a2sf_matmul_scaled(const a2sf_rows8* a, const a2sf_rows8* b, int32_t
   if ((long long)blocks(m) * blocks(n) > 0x3FFFFFFFLL) return A2SF_ESHAPE;
   A2SF_TRY(check_rows8(a, m, m, k, true));
   A2SF_TRY(check_rows8(b, n, blocks(n), k, true));
-  if ((m > 1 && a->stride > (1 << 23)) || (n > 1 && b->stride > (1 << 23))) return A2SF_ESHAPE;
+  constexpr int64_t kFarthest = 1 << 23;
+  if ((m > 1 && (a->stride > kFarthest || a->scale_stride > kFarthest)) || (n > 1 && b->stride > kFarthest) ||
+      (n > 128 && b->scale_stride > kFarthest))
+    return A2SF_ESHAPE;
   A2SF_TRY(check_rows(c, m, n, c_dtype, true));
   if (misaligned(workspace)) return A2SF_EWORKSPACE;
   MatmulArgs g;

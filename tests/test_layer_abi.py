@@ -78,6 +78,12 @@ def test_matmul_refusals():
     assert B.a2sf_matmul_workspace_bytes(64, 4096, 16384) <= 32 << 20
 
 
+def test_matmul_refuses_scales_too_far_apart():
+    far = rows8(scale_stride=(1 << 23) + 4)
+    assert B.lib().a2sf_matmul_scaled(far, rows8(), 4, 200, 200, rows(), B.A2SF_BF16, None, 0, None) == B.A2SF_ESHAPE
+    assert B.lib().a2sf_matmul_scaled(rows8(), far, 4, 200, 200, rows(), B.A2SF_BF16, None, 0, None) == B.A2SF_ESHAPE
+
+
 def part(x=FAKE, y=FAKE + 4096, xs=(4096, 512, 64), ys=(4096, 512, 64), heads=8, rotate=1):
     return B.RotaryPart(x, y, (ctypes.c_int64 * 3)(*xs), (ctypes.c_int64 * 3)(*ys), heads, rotate)
 
