@@ -7,8 +7,10 @@
 // last token: a cut (logit, index).  It is found without sorting, in a list of candidates that is certain to hold it:
 //  * top_k <= 512: the largest logit of each of 64, 256 or 512 groups of lanes is looked at; the smallest of these has so many
 //    tokens at or above it, and only a few times as many on the average: these are the list;
-//  * else: a rough histogram of the row (32 bins per octave of probability) says between which bins the cut lies; what lies above
-//    them is counted exactly, what lies in them is the list.
+//  * else: a rough histogram of the row (32 bins per octave of probability) says between which bins the cut lies.  The list is all
+//    that is not below these bins; if that is too many, what lies above them is counted exactly, what lies in them is the list;
+//  * min_p alone, or where it ends before these bins: what it keeps is the list, and no cut is needed.
+// What is left in a list that holds all from the largest on also races from there.
 // In the list a histogram finds the bin of the cut and the tokens of that bin are ranked against each other.  A list that
 // overflows or misses the cut (rows of few different values) is replaced by the row itself, whose bins are split until one
 // can be ranked, or holds one value only.
@@ -18,7 +20,8 @@
 //
 // A workgroup of 1024 lanes takes a row.  Few rows are a chain of passes and barriers whose instructions are mostly fetched for the first
 // time: what counts is little code, so passes are loops that read the row again (from the caches) instead of unrolled ones over
-// registers (32 000 logits in fp32, all filters: 14 us, 24 with the row in registers; 256 rows of 50 272 in bf16, top-p and min-p: 43 us), and one function serves counts and masses.
+// registers (32 000 logits in fp32, all filters: 13.4 us, 24 with the row in registers; 256 rows of 50 272 in bf16, top-p and min-p: 23 us, 43 with
+// exact counts and a race over the whole row), and one function serves counts and masses.
 #include "a2sf_internal.h"
 #include "rows_dev.h"
 
@@ -225,7 +228,7 @@ struct Scale {
   }
 };
 __device__ __forceinline__ float weight(float below) { return __builtin_amdgcn_exp2f(-below); }
-__device__ __forceinline__ uint32_t mass_of(float below) { return (uint32_t)rintf(weight(below) * 2147483648.f); }
+__device__ __forceinline__ uint32_t mass_of(float below) { return (uint32_t)fmaf(weight(below), 2147483648.f, 0.5f); }
 
 // What is looked for: the token at which the count (by_mass: the mass) reaches a number
 struct Target {
@@ -244,8 +247,8 @@ __device__ __forceinline__ void clear_bins(SampleShared& s) {
 // The bin in which the target is reached and what lies before it; s.bin = -1 if there is none.  Returns the total mass.  Four waves
 // do it, a lane four bins: with all sixteen at it the vector units would be four times as long busy with the same few bins.
 __device__ __forceinline__ unsigned long long scan_bins(SampleShared& s, Target to, uint32_t count0, unsigned long long mass0) {
-  if (threadIdx.x == 0) s.bin = -1;
   __syncthreads();
+  if (threadIdx.x == 0) s.bin = -1;  // (everybody has read the last scan's)
   const int t = threadIdx.x, wave = t >> 6;
   uint32_t c = 0, own_c[4];
   unsigned long long m = 0, own_m[4];
@@ -443,132 +446,135 @@ __device__ __forceinline__ unsigned long long mass_for(float p, unsigned long lo
   return mass < 1 ? 1 : mass > inside ? inside : mass;
 }
 
-// Top-k and top-p on a row, or on a list that holds the first k tokens.
+// Top-k and top-p on a row, or on a list of a row's first tokens.  inside: the mass that p is a share of where there is no k, 0: that
+// of R.  Whether the cut lies in R: the tokens above -infinity may be fewer than k, and if R holds `all` of them they stay.
 template <typename R>
-__device__ __forceinline__ void find_cut(const R& row, const Scale& sc, const Filters& f, SampleShared& s) {
+__device__ __forceinline__ bool find_cut(const R& row, const Scale& sc, const Filters& f, unsigned long long inside, bool all, SampleShared& s) {
   Target to{false, f.k ? (uint32_t)f.k : 0xFFFFFFFFu, 0};
+  if (inside) to = {true, 0, mass_for(f.p, inside)};
   bool filled = false;
 #pragma unroll 1
-  for (int by_mass = 0; by_mass < 2; ++by_mass) {
+  for (;;) {
     if (!filled) fill_bins(row, sc, s);
     filled = true;
-    unsigned long long inside = scan_bins(s, to, 0, 0);
-    if (s.bin >= 0) {  // (fewer than k tokens above -inf: all of them stay)
+    inside = scan_bins(s, to, 0, 0);
+    if (s.bin >= 0) {
       filled = !cut_in_bin(row, sc, s, to);
       inside = s.kept_mass;
+    } else if (!all) {
+      return false;
     }
-    if (!(f.p < 1.f)) break;
+    if (to.by_mass || !(f.p < 1.f)) return true;
     to = {true, 0, mass_for(f.p, inside)};
   }
 }
 
-// The cut by mass (or by more tokens than lists are made for) in a whole row: a rough histogram, then the bins around the cut
-// exactly.  inside: the mass that p is a share of, 0: the row's.  s_above: tokens above the zone.  Returns false where that does not do.
-template <typename R>
-__device__ __forceinline__ bool find_zone_cut(const R& row, const Scale& sc, const Filters& f, bool by_mass, unsigned long long inside,
-                                              SampleShared& s, uint32_t& s_above) {
-  clear_bins(s);
-  // a bin's masses in units of its own size, 13 bits of each token.  (Rows of more than 2^18 tokens may overflow 32 bits: then the bins
-  // are wrong, and the exact count below finds it out.)  The last bin stays empty: most of a row may lie there, and everybody would add at one
-  // address; a target that no bin reaches is there.
-  const float per = sc.per * kBinsPerOctave, top = sc.top * per;
-  if (by_mass) {
-    row.each([&](float l, int) {
-      const float below = fminf(fmaf(-l, per, top), (float)(kBins - 1));
-      const int bin = (int)fmaxf(below, 0.f);
-      const float m = __builtin_amdgcn_exp2f(fmaf((float)bin - below, 1.f / kBinsPerOctave, 13.f));
-      if (bin < kBins - 1) atomicAdd(&s.count[bin], (uint32_t)m);
-    });
-  } else {
-    row.each([&](float l, int) {
-      const int bin = sc.over_row().bin(l);
-      if (bin < kBins - 1) atomicAdd(&s.count[bin], 1u);
-    });
-  }
+// The sum of every lane's v, which is a whole number below 2^63.
+__device__ __forceinline__ unsigned long long block_sum_u64(unsigned long long v, unsigned long long* left) {
+  uint32_t none = 0;
+  wave_scan(none, v);
   __syncthreads();
+  if ((threadIdx.x & 63) == 63) left[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = left[threadIdx.x & 15];
+  scan_step<0x111, 0xF>(none, v);
+  scan_step<0x112, 0xF>(none, v);
+  scan_step<0x114, 0xF>(none, v);
+  scan_step<0x118, 0xF>(none, v);
+  return ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 15) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, 15);
+}
+
+// Where in a row the cut by mass (or by more tokens than groups of lanes give) lies.
+struct Zone {
+  float high, low;        // logits: the cut is below the one and not below the other, for certain
+  unsigned long long all; // the mass of the row
+  bool few;               // what is not below `low` may well fit a list
+};
+
+// By a rough histogram.  inside: the mass that p is a share of, 0: the row's.
+template <typename R>
+__device__ __forceinline__ Zone find_zone(const R& row, const Scale& sc, const Filters& f, bool by_mass, unsigned long long inside,
+                                          SampleShared& s) {
+  clear_bins(s);
+  // A bin's masses in units of its octave's own size, 12 bits of each token or all there are.  (Rows of more than 2^19 tokens may
+  // overflow 32 bits: then the bins are wrong, and the exact sums after this find it out.)  The last bin stays empty: most of a
+  // row may lie there, and everybody would add at one address; a target that no bin reaches is there.
+  unsigned long long all = 0;
+  row.each([&](float l, int) {
+    const float below = sc.below(l);
+    const uint32_t m = mass_of(below);
+    all += m;
+    const uint32_t bin = (uint32_t)fminf(below * kBinsPerOctave, (float)(kBins - 1));
+    if (bin < kBins - 1) atomicAdd(&s.count[bin], by_mass ? m << (bin / 32u) >> 19 : 1u);
+  });
+  all = block_sum_u64(all, s.wave64b);  // (its barriers are the bins' too)
   // (a token of 1 is 2^41 here)
-  s.mass[threadIdx.x] = (unsigned long long)((float)s.count[threadIdx.x] * __builtin_amdgcn_exp2f(28.f - (float)threadIdx.x * (1.f / kBinsPerOctave)));
-  Target to{by_mass, (uint32_t)f.k, ~0ull};
-  if (by_mass) {
-    unsigned long long rough = scan_bins(s, to, 0, 0);
-    if (inside) rough = inside << 10;
-    to.mass = mass_for(f.p, rough);
-  }
+  s.mass[threadIdx.x] = ((unsigned long long)s.count[threadIdx.x] << 29) >> (threadIdx.x / 32u);
+  Target to{by_mass, (uint32_t)f.k, 0};
   // The bins between which the cut lies for certain, and one more on either side, in logits (whose edges need not be exact).  The masses
-  // are good to 2^-13; the logits of one bin may all be the same, with nothing in the bins around it.
-  to.mass -= to.mass >> 11;
+  // are up to 2^-11 too small; the logits of one bin may all be the same, with nothing in the bins around it.
+  const unsigned long long mass = by_mass ? mass_for(f.p, inside ? inside : all) << 10 : 0;
+  to.mass = mass - (mass >> 10);
   scan_bins(s, to, 0, 0);
   const int from = s.bin < 0 ? kBins - 1 : s.bin;
   int upto = from;
   if (by_mass) {
-    to.mass += to.mass >> 10;
+    to.mass = mass;
     scan_bins(s, to, 0, 0);
     upto = s.bin < 0 ? kBins - 1 : s.bin;
   }
-  const float high = from < 2 ? kInf : sc.top - (float)(from - 1) / (kBinsPerOctave * sc.per);
-  const float low = upto > kBins - 3 ? -3.4e38f : sc.top - (float)(upto + 2) / (kBinsPerOctave * sc.per);
+  Zone zone;
+  zone.high = from < 2 ? kInf : sc.top - (float)(from - 1) / (kBinsPerOctave * sc.per);
+  zone.low = upto > kBins - 3 ? -3.402823466e38f : sc.top - (float)(upto + 2) / (kBinsPerOctave * sc.per);
+  zone.all = all;
+  zone.few = s.bin >= 0 && (by_mass ? s.before_count >> 11 : (uint32_t)f.k) <= kSampleWaves * kListed;
+  return zone;
+}
+
+// The cut in a zone: what lies above is counted exactly, what lies inside is listed.  s_above: tokens above.  Returns false where that does
+// not do.
+template <typename R>
+__device__ __forceinline__ bool cut_in_zone(const R& row, const Scale& sc, const Filters& f, bool by_mass, unsigned long long inside,
+                                            const Zone& zone, SampleShared& s, uint32_t& s_above) {
+  __syncthreads();
   if (threadIdx.x == 0) s.overflow = 0;
   List list{s, row.n};
-  unsigned long long above = 0, all = 0;
-  uint32_t count = 0;
+  unsigned long long above = 0;
+  uint32_t c = 0;
   row.each_unit([&](const auto& u, int first) {
 #pragma unroll
     for (int j = 0; j < kUnit; ++j) {
       const float l = u.at(j);
-      const uint32_t m = mass_of(sc.below(l));
-      const bool over = l > high;
-      all += m;
-      above += over ? m : 0u;
-      count += over;
-      list.bits = 2 * list.bits + (l >= low && !over);
+      const bool over = l > zone.high;
+      if (over) above += mass_of(sc.below(l));
+      c += over;
+      list.bits = 2 * list.bits + (l >= zone.low && !over);
     }
     list.unit_done(first);
   });
-  uint32_t c = count, none = 0;
-  wave_scan(c, above);
-  wave_scan(none, all);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) {
-    s.wave32[threadIdx.x >> 6] = c;
-    s.wave64[threadIdx.x >> 6] = above;
-    s.wave64b[threadIdx.x >> 6] = all;
-  }
-  if (!list.complete(row)) return false;
-  c = of_waves(s.wave32, OpSumI());
-  above = s.wave64[threadIdx.x & 15];
-  all = s.wave64b[threadIdx.x & 15];
-  none = 0;
-  scan_step<0x111, 0xF>(none, above);
-  scan_step<0x112, 0xF>(none, above);
-  scan_step<0x114, 0xF>(none, above);
-  scan_step<0x118, 0xF>(none, above);
-  scan_step<0x111, 0xF>(none, all);
-  scan_step<0x112, 0xF>(none, all);
-  scan_step<0x114, 0xF>(none, all);
-  scan_step<0x118, 0xF>(none, all);
-  const auto last_of_row = [](unsigned long long v) {
-    return ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 15) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, 15);
-  };
-  above = last_of_row(above);
-  all = last_of_row(all);
+  above = block_sum_u64(above, s.wave64);
+  c = block_sum_u32(c, s.wave32);
   s_above = c;
-  to = {by_mass, (uint32_t)f.k, by_mass ? mass_for(f.p, inside ? inside : all) : 0};
-  const Scale zone = sc.over(high, low);
-  fill_bins(list, zone, s);
+  if (!list.complete(row)) return false;
+  const Target to{by_mass, (uint32_t)f.k, by_mass ? mass_for(f.p, inside ? inside : zone.all) : 0};
+  const Scale bins = sc.over(zone.high, zone.low);
+  fill_bins(list, bins, s);
   scan_bins(s, to, c, above);
-  if (s.bin < 0) return !by_mass && c < to.tokens && low < -3e38f ? (s.cut = -kInf, s.kept_mass = all, true) : false;
-  cut_in_bin(list, zone, s, to);
+  if (s.bin < 0) return !by_mass && c < to.tokens && zone.low < -3.4e38f ? (s.cut = -kInf, s.kept_mass = zone.all, true) : false;
+  cut_in_bin(list, bins, s, to);
   return true;
 }
 
-// What a token brings to the race.  A lane meets its tokens by index: the first of equal ones stays.
+// What a token brings to the race.  Of equal ones the lowest index stays; a lane meets the tokens of a row by index, those of a list
+// (ANY_ORDER) not.
 struct Runner {
   float z = 0.f, best = -kInf;
   int at = -1;
+  template <bool ANY_ORDER>
   __device__ __forceinline__ void enter(bool in, float below, float log_noise, int index) {
     const float ring = -below - log_noise;  // (base 2; not a number: never taken)
     z += in ? weight(below) : 0.f;
-    const bool ahead = in && ring > best;
+    const bool ahead = in && (ring > best || (ANY_ORDER && ring == best && index < at));
     best = ahead ? ring : best;
     at = ahead ? index : at;
   }
@@ -587,43 +593,62 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
   const float min_p = f.min_p;
   const auto in_share = [&](float l, float below) { return weight(below) >= min_p || l == sc.top; };  // the first always stays
   Runner run;
+  // A list of all that is not below some logit, if the cut is certain to be there and it may be short enough; where min_p keeps less
+  // than the other filters, of all that it keeps (a hundredth of an octave more, for the roundings).
+  const bool cuts = f.k > 0 || f.p < 1.f, zoned = cuts && !(f.k > 0 && f.k <= 512) && !TOP_IS_INF;
+  float least = fmaxf(low, -3.402823466e38f);  // (no -infinity)
+  Zone zone;
+  zone.high = kInf;
+  bool listed = !TOP_IS_INF && cuts, cut_there = listed;
+  if (zoned) {
+    zone = find_zone(row, sc, f, f.k == 0, 0, s);
+    least = zone.low;
+    listed = zone.few;
+  }
+  if (!TOP_IS_INF && min_p > 0.f && (zoned ? f.k == 0 || !(f.p < 1.f) : !cuts)) {
+    const float share = fminf(sc.top, sc.top - (0.01f - __builtin_amdgcn_logf(min_p)) / sc.per);
+    if (!cuts || share > zone.high) {
+      least = share;
+      listed = true;
+      cut_there = false;
+    }
+  }
   List list{s, a.n};
-  bool listed = false;
-  const float least = fmaxf(low, -3.402823466e38f);  // (no -infinity)
-  if (!TOP_IS_INF && f.k > 0 && f.k <= 512) {
+  if (listed) {
     row.each_unit([&](const RawUnit<T>& u, int first) {
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) list.bits = 2 * list.bits + (u.at(j) >= least);
       list.unit_done(first);
     });
     listed = list.complete(row);
+    if (listed && cut_there) listed = find_cut(list, sc.over(kInf, least), f, f.k ? 0 : zone.all, least < -3.4e38f || !zoned, s);
   }
   if (listed) {
-    find_cut(list, sc.over(kInf, least), f, s);
     const float cut = s.cut;
     const int cut_index = s.cut_index;
     list.each([&](float l, int at) {
       const float below = sc.below(l);
       const bool in = (l > cut || (l == cut && at <= cut_index)) && below < kInf && in_share(l, below);
-      if (in) run.enter(true, below, noise ? __builtin_amdgcn_logf(noise[at]) : 0.f, at);
+      if (in) run.enter<true>(true, below, noise ? __builtin_amdgcn_logf(noise[at]) : 0.f, at);
     });
   } else {
     // Where many tokens are left their random numbers are fetched for every unit, one unit ahead; else where one of the wave's
     // is still in.
     bool ahead = !(min_p > 0.f);
-    if (f.k > 0 || f.p < 1.f) {
+    if (cuts) {
       bool found = !TOP_IS_INF;
       unsigned long long inside = 0;
       uint32_t above = 0;
 #pragma unroll 1
       for (int by_mass = f.k > 0 ? 0 : 1; found && by_mass < (f.p < 1.f ? 2 : 1); ++by_mass) {
-        found = find_zone_cut(row, sc, f, by_mass, inside, s, above);
+        if (!zoned || inside) zone = find_zone(row, sc, f, by_mass, inside, s);
+        found = cut_in_zone(row, sc, f, by_mass, inside, zone, s, above);
         inside = s.kept_mass;
       }
       if (!found) {
         __syncthreads();
         if (t == 0) s.cut = -kInf;
-        find_cut(row, sc.over_row(), f, s);
+        find_cut(row, sc.over_row(), f, 0, true, s);
       }
       ahead = found && above >= (uint32_t)a.n / 64 && !(min_p > 0.f);
     }
@@ -665,7 +690,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
       if (!ahead && noise && in) load_unit(noise + first, a.n - first, e);
 #pragma unroll
       for (int j = 0; j < kUnit; ++j)
-        run.enter(in >> j & 1, sc.below(row.logit(u.at(j))), __builtin_amdgcn_logf(e[j]), first + j);
+        run.enter<false>(in >> j & 1, sc.below(row.logit(u.at(j))), __builtin_amdgcn_logf(e[j]), first + j);
     });
   }
   // the furthest runner; of equal ones the lowest index
@@ -716,6 +741,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
   f.k = f.k > 0 && f.k < a.n ? f.k : 0;
   f.p = a.top_p ? a.top_p[r] : 1.f;
   f.min_p = a.min_p ? a.min_p[r] : 0.f;
+  f.min_p = f.min_p > 0.f ? f.min_p : 0.f;  // (not a number: no filter)
   if (greedy) f = {0, 1.f, 0.f};
 
   // The largest logit; and the smallest of the largest ones of `groups` groups of lanes: so many tokens at least are not below

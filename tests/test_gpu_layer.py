@@ -483,6 +483,29 @@ def test_sample_values_close_together():
     check_tokens(logits, noise, top_p=[0.3, 0.77, 0.5], top_k=[0, 5000, 2])
 
 
+@pytest.mark.parametrize("filters", [dict(top_k=[512] * 48), dict(top_p=[0.9] * 48), dict(min_p=[0.5] * 48),
+                                     dict(top_k=[3000] * 48, top_p=[0.9] * 48)])
+def test_sample_equal_weights_go_to_the_lowest_index(filters):
+    """Without random numbers the first of the largest logits, wherever the others stand."""
+    g = rng(17)
+    l = np.where(g.random((48, 8192)) < 0.5, 1.5, g.normal(size=(48, 8192)) - 5)
+    l[g.random(l.shape) < 0.05] = 2.0
+    check_tokens(on_gpu(l, torch.bfloat16), None, **filters)
+
+
+@pytest.mark.parametrize("p", [0.5, 0.9, 0.99, 0.9999, 0.9999999])
+def test_sample_long_and_short_cuts(p):
+    """A few tokens with nearly all of the mass, a few thousand, nearly all of the row."""
+    g = rng(18)
+    n = 40000
+    l = g.normal(size=(6, n)) * np.array([0.01, 0.5, 1.0, 2.0, 4.0, 12.0])[:, None]
+    noise = on_gpu(g.exponential(size=(6, n)) + 1e-9, torch.float32)
+    for dtype in (torch.float32, torch.bfloat16):
+        check_tokens(on_gpu(l, dtype), noise, top_p=[p] * 6)
+        check_tokens(on_gpu(l, dtype), noise, top_p=[p] * 6, min_p=[0.01] * 6)
+        check_tokens(on_gpu(l, dtype), noise, top_p=[p] * 6, top_k=[600, 5000, 8000, 9000, 20000, 39999])
+
+
 def test_sample_infinities_and_nan():
     inf, nan = math.inf, math.nan
     rows = [[-inf, nan, -inf, nan], [inf, 1.0, inf, 2.0], [nan, -inf, 3.0, -inf], [-inf, 0.0, 1.0, nan], [nan, inf, nan, -1.0],
