@@ -7,9 +7,9 @@
 // last token: a cut (logit, index).  It is found without sorting, in a list of candidates that is certain to hold it:
 //  * top_k <= 512: the largest logit of each of 64, 256 or 512 groups of lanes is looked at; the smallest of these has so many
 //    tokens at or above it, and only a few times as many on the average: these are the list;
-//  * else: a rough histogram of the row (32 bins per octave of probability) says between which bins the cut lies.  The list is all
-//    that is not below these bins; if that is too many, what lies above them is counted exactly, what lies in them is the list;
-//  * min_p alone, or where it ends before these bins: what it keeps is the list, and no cut is needed.
+//  * else: a histogram of the row's masses (32 bins per octave of probability) says in which bin the cut lies.  The list is all
+//    that is not below this bin, or if that is too many what lies in it;
+//  * min_p alone, or where it ends before this bin: what it keeps is the list, and no cut is needed.
 // What is left in a list that holds all from the largest on also races from there.
 // In the list a histogram finds the bin of the cut and the tokens of that bin are ranked against each other.  A list that
 // overflows or misses the cut (rows of few different values) is replaced by the row itself, whose bins are split until one
@@ -20,8 +20,8 @@
 //
 // A workgroup of 1024 lanes takes a row.  Few rows are a chain of passes and barriers whose instructions are mostly fetched for the first
 // time: what counts is little code, so passes are loops that read the row again (from the caches) instead of unrolled ones over
-// registers (32 000 logits in fp32, all filters: 13.4 us, 24 with the row in registers; 256 rows of 50 272 in bf16, top-p and min-p: 23 us, 43 with
-// exact counts and a race over the whole row), and one function serves counts and masses.
+// registers (32 000 logits in fp32, all filters: 13.4 us, 24 with the row in registers; 256 rows of 50 272 in bf16, top-p and min-p: 21.5 us, 43 with
+// a second pass for exact masses and a race over the whole row), and one function serves counts and masses.
 #include "a2sf_internal.h"
 #include "rows_dev.h"
 
@@ -484,83 +484,67 @@ __device__ __forceinline__ unsigned long long block_sum_u64(unsigned long long v
   return ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 15) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, 15);
 }
 
-// Where in a row the cut by mass (or by more tokens than groups of lanes give) lies.
+// The bin of a row in which the cut by mass (or by more tokens than groups of lanes give) lies.
 struct Zone {
-  float high, low;        // logits: the cut is below the one and not below the other, for certain
-  unsigned long long all; // the mass of the row
-  bool few;               // what is not below `low` may well fit a list
+  int bin;                        // -1: none, or the last
+  uint32_t above, in;             // tokens above the bin and in it; by mass: as many to twice as many
+  unsigned long long above_mass;  // their mass
+  unsigned long long all;         // the mass of the row
 };
 
-// By a rough histogram.  inside: the mass that p is a share of, 0: the row's.
+// inside: the mass that p is a share of, 0: the row's.
 template <typename R>
 __device__ __forceinline__ Zone find_zone(const R& row, const Scale& sc, const Filters& f, bool by_mass, unsigned long long inside,
                                           SampleShared& s) {
   clear_bins(s);
-  // A bin's masses in units of its octave's own size, 12 bits of each token or all there are.  (Rows of more than 2^19 tokens may
-  // overflow 32 bits: then the bins are wrong, and the exact sums after this find it out.)  The last bin stays empty: most of a
-  // row may lie there, and everybody would add at one address; a target that no bin reaches is there.
+  // The last bin stays empty: most of a row may lie there, and everybody would add at one address.
   unsigned long long all = 0;
   row.each([&](float l, int) {
     const float below = sc.below(l);
     const uint32_t m = mass_of(below);
     all += m;
     const uint32_t bin = (uint32_t)fminf(below * kBinsPerOctave, (float)(kBins - 1));
-    if (bin < kBins - 1) atomicAdd(&s.count[bin], by_mass ? m << (bin / 32u) >> 19 : 1u);
+    if (bin < kBins - 1) {
+      atomicAdd(&s.mass[bin], (unsigned long long)m);
+      if (!by_mass) atomicAdd(&s.count[bin], 1u);
+    }
   });
-  all = block_sum_u64(all, s.wave64b);  // (its barriers are the bins' too)
-  // (a token of 1 is 2^41 here)
-  s.mass[threadIdx.x] = ((unsigned long long)s.count[threadIdx.x] << 29) >> (threadIdx.x / 32u);
-  Target to{by_mass, (uint32_t)f.k, 0};
-  // The bins between which the cut lies for certain, and one more on either side, in logits (whose edges need not be exact).  The masses
-  // are up to 2^-11 too small; the logits of one bin may all be the same, with nothing in the bins around it.
-  const unsigned long long mass = by_mass ? mass_for(f.p, inside ? inside : all) << 10 : 0;
-  to.mass = mass - (mass >> 10);
-  scan_bins(s, to, 0, 0);
-  const int from = s.bin < 0 ? kBins - 1 : s.bin;
-  int upto = from;
-  if (by_mass) {
-    to.mass = mass;
-    scan_bins(s, to, 0, 0);
-    upto = s.bin < 0 ? kBins - 1 : s.bin;
-  }
   Zone zone;
-  zone.high = from < 2 ? kInf : sc.top - (float)(from - 1) / (kBinsPerOctave * sc.per);
-  zone.low = upto > kBins - 3 ? -3.402823466e38f : sc.top - (float)(upto + 2) / (kBinsPerOctave * sc.per);
-  zone.all = all;
-  zone.few = s.bin >= 0 && (by_mass ? s.before_count >> 11 : (uint32_t)f.k) <= kSampleWaves * kListed;
+  zone.all = block_sum_u64(all, s.wave64b);  // (its barriers are the bins' too)
+  // (a token of octave o has between 2^(30 - o) and 2^(31 - o))
+  if (by_mass) s.count[threadIdx.x] = (uint32_t)(s.mass[threadIdx.x] >> (30u - min(threadIdx.x / 32u, 30u)));
+  scan_bins(s, Target{by_mass, (uint32_t)f.k, by_mass ? mass_for(f.p, inside ? inside : zone.all) : 0}, 0, 0);
+  zone.bin = s.bin;
+  zone.above = s.before_count;
+  zone.in = s.in_bin;
+  zone.above_mass = s.before_mass;
   return zone;
 }
 
-// The cut in a zone: what lies above is counted exactly, what lies inside is listed.  s_above: tokens above.  Returns false where that does
-// not do.
+// The cut in that bin, whose tokens are listed.  Returns false where they do not fit.
 template <typename R>
 __device__ __forceinline__ bool cut_in_zone(const R& row, const Scale& sc, const Filters& f, bool by_mass, unsigned long long inside,
-                                            const Zone& zone, SampleShared& s, uint32_t& s_above) {
+                                            const Zone& zone, SampleShared& s) {
+  if (zone.bin < 0) return false;
   __syncthreads();
   if (threadIdx.x == 0) s.overflow = 0;
+  __syncthreads();
   List list{s, row.n};
-  unsigned long long above = 0;
-  uint32_t c = 0;
   row.each_unit([&](const auto& u, int first) {
 #pragma unroll
     for (int j = 0; j < kUnit; ++j) {
-      const float l = u.at(j);
-      const bool over = l > zone.high;
-      if (over) above += mass_of(sc.below(l));
-      c += over;
-      list.bits = 2 * list.bits + (l >= zone.low && !over);
+      const float at = sc.below(u.at(j)) * kBinsPerOctave;
+      list.bits = 2 * list.bits + (at >= (float)zone.bin && at < (float)(zone.bin + 1));
     }
     list.unit_done(first);
   });
-  above = block_sum_u64(above, s.wave64);
-  c = block_sum_u32(c, s.wave32);
-  s_above = c;
   if (!list.complete(row)) return false;
+  const float per = kBinsPerOctave * sc.per;
+  const Scale bins = sc.over(sc.top - (float)zone.bin / per, sc.top - (float)(zone.bin + 1) / per);
   const Target to{by_mass, (uint32_t)f.k, by_mass ? mass_for(f.p, inside ? inside : zone.all) : 0};
-  const Scale bins = sc.over(zone.high, zone.low);
   fill_bins(list, bins, s);
-  scan_bins(s, to, c, above);
-  if (s.bin < 0) return !by_mass && c < to.tokens && zone.low < -3.4e38f ? (s.cut = -kInf, s.kept_mass = zone.all, true) : false;
+  scan_bins(s, to, zone.above, zone.above_mass);
+  if (s.bin < 0) return false;
   cut_in_bin(list, bins, s, to);
   return true;
 }
@@ -598,16 +582,16 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
   const bool cuts = f.k > 0 || f.p < 1.f, zoned = cuts && !(f.k > 0 && f.k <= 512) && !TOP_IS_INF;
   float least = fmaxf(low, -3.402823466e38f);  // (no -infinity)
   Zone zone;
-  zone.high = kInf;
   bool listed = !TOP_IS_INF && cuts, cut_there = listed;
   if (zoned) {
     zone = find_zone(row, sc, f, f.k == 0, 0, s);
-    least = zone.low;
-    listed = zone.few;
+    // (a bin more, so that edges need not be exact)
+    least = fmaxf(sc.top - (float)(zone.bin + 2) / (kBinsPerOctave * sc.per), -3.402823466e38f);
+    listed = zone.bin >= 0 && zone.above + zone.in <= kSampleWaves * kListed;
   }
   if (!TOP_IS_INF && min_p > 0.f && (zoned ? f.k == 0 || !(f.p < 1.f) : !cuts)) {
     const float share = fminf(sc.top, sc.top - (0.01f - __builtin_amdgcn_logf(min_p)) / sc.per);
-    if (!cuts || share > zone.high) {
+    if (!cuts || (zone.bin > 1 && share > sc.top - (float)(zone.bin - 1) / (kBinsPerOctave * sc.per))) {
       least = share;
       listed = true;
       cut_there = false;
@@ -621,7 +605,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
       list.unit_done(first);
     });
     listed = list.complete(row);
-    if (listed && cut_there) listed = find_cut(list, sc.over(kInf, least), f, f.k ? 0 : zone.all, least < -3.4e38f || !zoned, s);
+    if (listed && cut_there) listed = find_cut(list, sc.over(kInf, least), f, f.k ? 0 : zone.all, !zoned, s);
   }
   if (listed) {
     const float cut = s.cut;
@@ -638,11 +622,10 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
     if (cuts) {
       bool found = !TOP_IS_INF;
       unsigned long long inside = 0;
-      uint32_t above = 0;
 #pragma unroll 1
       for (int by_mass = f.k > 0 ? 0 : 1; found && by_mass < (f.p < 1.f ? 2 : 1); ++by_mass) {
         if (!zoned || inside) zone = find_zone(row, sc, f, by_mass, inside, s);
-        found = cut_in_zone(row, sc, f, by_mass, inside, zone, s, above);
+        found = cut_in_zone(row, sc, f, by_mass, inside, zone, s);
         inside = s.kept_mass;
       }
       if (!found) {
@@ -650,7 +633,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
         if (t == 0) s.cut = -kInf;
         find_cut(row, sc.over_row(), f, 0, true, s);
       }
-      ahead = found && above >= (uint32_t)a.n / 64 && !(min_p > 0.f);
+      ahead = found && zone.above >= (uint32_t)a.n / 64 && !(min_p > 0.f);
     }
     __syncthreads();
     const float cut = s.cut;
