@@ -142,94 +142,137 @@ __device__ __forceinline__ void store_bytes(T* p, int have, u32x4_t v) {
     }
 }
 
-// ---- a few rows of A: B is streamed once, straight into registers ------------------------------------------------------------
-// A workgroup takes 16 columns of C and all rows (MT tiles of 16), its waves share k in groups of four steps and add their parts
-// in LDS in a fixed order.  Bound by the stream of B; A comes from the caches.  The next group's part of B is on its way while the
-// present one is multiplied, and A is a step ahead.
+// ---- few rows of A: B is streamed once --------------------------------------------------------------------------------------
+// A workgroup takes 16 columns of C after the other and all rows (MT tiles of 16); its waves share k and add their parts in LDS in a
+// fixed order.  Each wave streams its part of k of B and A through a ring of its own in LDS, 128 bytes of each row to a slot, and
+// the stream runs on from columns to columns: a wave waits for others at the sums only.
+// Bound by the stream of B as long as A is short: a step takes 2 us from its fetch to its arrival, whatever its size, and A's rows
+// take their share of the ring.  By way of LDS and not straight into registers, where an operand's lanes, each in another
+// row, ask for 16 bytes at a time of 64 places: 48 x 4096 x 11008 33 us, so 12.5; 1 x 4096 x 11008 10.5, so 8.7.
 // Where rows of B lie a multiple of 4096 bytes apart, workgroups that all began at the same place of k would all ask the same few of the
-// caches' channels: each begins with another of its wave's groups.
-// 1 x 12288 x 4096: 10.3 us (4.9 TB/s; all from the first group: 12.8), 1 x 22016 x 4096: 17.1 us (5.3 TB/s; 21.5).
-template <typename T, int MT>
-__global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs g) {
+// caches' channels: each begins at another one (1 x 12288 x 4096 straight into registers 12.8 us, so 10.3).
+// 1 x 12288 x 4096 9.0 us = 5.6 TB/s; 1 x 8192 x 8192 11.4 = 5.9; 32 x 12288 x 4096 10.4 = 4.9; 48 x 4096 x 11008 12.5 = 3.7.
+template <int MT, int WAVES, int ROOM>
+struct StripLds {
+  static constexpr int kPart = WAVES * MT * 1024;
+  static constexpr int kSlot = (1 + MT) * 2048 + 512;  // rows of B, of A; four scales of each of 64 rows of A, and of B
+  static constexpr int kSlots = (ROOM - kPart) / WAVES / kSlot;
+  static constexpr int kBytes = kPart + WAVES * kSlots * kSlot;
+  static constexpr int kLoads = 2 + 2 * MT + 2;  // per step
+  static_assert(kSlots >= 2 && (kSlots - 1) * kLoads < 64 && kBytes <= ROOM, "");
+};
+
+template <typename T, int MT, int WAVES, int ROOM>
+__global__ __launch_bounds__(WAVES * 64) void matmul_strip_kernel(MatmulArgs g) {
   typedef typename Way<T>::type W;
-  extern __shared__ f32x4_t part[];  // [waves][MT][64]
-  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, waves = blockDim.x >> 6;
-  const int n0 = blockIdx.x * 16;
-  const int steps = (g.k + kStep - 1) / kStep, groups = (steps + kGroup - 1) / kGroup;
-  const int kl = (lane >> 4) * 16;  // and 64 on: an access takes 64 bytes of each of 16 rows
-  const uint8_t* b = g.b + (long long)min(n0 + (lane & 15), g.n - 1) * g.b_stride + kl;
-  const uint8_t* bs = g.b_scales + (long long)(n0 / 128) * g.b_scale_stride;
-  uint32_t a_at[MT], as_at[MT];  // byte offsets of this lane's rows (at most 64 of them)
+  typedef StripLds<MT, WAVES, ROOM> L;
+  static_assert(MT <= WAVES, "a lane stores one part of a tile at most");
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
+  const int tiles = (g.n + 15) / 16, steps = g.k / kStep;
+  const int each = (steps + WAVES - 1) / WAVES, begin = min(wave * each, steps), end = min(begin + each, steps);
+  const int mine = ((int)blockIdx.x < tiles ? (tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0);
+  int total = mine * (end - begin), issue_left = total;  // steps still to multiply, to fetch
+  const uint32_t ring = L::kPart + wave * (L::kSlots * L::kSlot);
+
+  // A load takes 8 rows' 128 bytes; chunk c of row r lies at c ^ (r / 2 % 8), so that 16 lanes that read the same chunk of 16 rows
+  // meet all banks once.
+  const int chunk = (lane & 7) ^ (lane >> 4);
+  uint32_t a_off[2 * MT], b_off[2];
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const uint32_t row = (uint32_t)min(i * 16 + (lane & 15), g.m - 1);
-    a_at[i] = row * (uint32_t)g.a_stride + kl;
-    as_at[i] = row * (uint32_t)g.a_scale_stride;
-  }
-  f32x4_t acc[MT] = {};
-  const auto whole = [&](int group) { return (group + 1) * kGroup * kStep <= g.k; };
-  i32x8_t bv[kGroup], bn[kGroup];
-  const auto load_b = [&](i32x8_t* to, int group) {
-    const uint8_t* p = b + (long long)group * kGroup * kStep;
-    if (whole(group)) {
+  for (int u = 0; u < 2 * MT; ++u)
+    a_off[u] = (uint32_t)min(u * 8 + (lane >> 3), g.m - 1) * (uint32_t)g.a_stride + (uint32_t)(chunk ^ (u & 1) * 4) * 16;
+  const uint32_t scale_off = (uint32_t)min(lane, g.m - 1) * (uint32_t)g.a_scale_stride;
+  const int start = end > begin ? begin + (int)(blockIdx.x / 8) % (end - begin) : 0;
+  int at_tile = blockIdx.x, at_step = start, at_slot = 0;  // of the next fetch
+  const auto aim = [&] {
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) to[j] = join(*(const i32x4_t*)(p + j * kStep), *(const i32x4_t*)(p + j * kStep + 64));
-    } else {
+    for (int u = 0; u < 2; ++u)
+      b_off[u] = (uint32_t)min(u * 8 + (lane >> 3), g.n - 1 - at_tile * 16) * (uint32_t)g.b_stride + (uint32_t)(chunk ^ u * 4) * 16;
+  };
+  const auto fetch = [&] {
+    const uint32_t to = ring + at_slot * L::kSlot;
+    const uint8_t* b = g.b + (long long)at_tile * 16 * g.b_stride + at_step * kStep;
+    const uint8_t* a = g.a + at_step * kStep;
+    dma16(b, b_off[0], to);
+    dma16(b, b_off[1], to + 1024);
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) {
-        const int k0 = (group * kGroup + j) * kStep;
-        to[j] = join(load_chunk(b, k0, g.k - kl), load_chunk(b, k0 + 64, g.k - kl));
-      }
+    for (int u = 0; u < 2 * MT; ++u) dma16(a, a_off[u], to + 2048 + u * 1024);
+    const int group = at_step & ~(kGroup - 1);
+    dma4(g.a_scales + group, scale_off, to + (1 + MT) * 2048);
+    dma4(g.b_scales + (long long)(at_tile / 8) * g.b_scale_stride + group, 0, to + (1 + MT) * 2048 + 256);
+    --issue_left;
+    if (++at_slot == L::kSlots) at_slot = 0;
+    if (++at_step == end) at_step = begin;
+    if (at_step == start) {
+      at_tile += gridDim.x;
+      aim();
     }
   };
-  const auto load_a = [&](i32x8_t* to, int s) {
-    if ((s + 1) * kStep <= g.k) {
-      const uint8_t* p = g.a + (long long)s * kStep;
-#pragma unroll
-      for (int i = 0; i < MT; ++i) to[i] = join(*(const i32x4_t*)(p + a_at[i]), *(const i32x4_t*)(p + a_at[i] + 64));
-    } else {
-#pragma unroll
-      for (int i = 0; i < MT; ++i) to[i] = join(load_chunk(g.a + a_at[i], s * kStep, g.k - kl), load_chunk(g.a + a_at[i], s * kStep + 64, g.k - kl));
-    }
-  };
-  const int rounds = (groups + waves - 1) / waves, first = wave * rounds, last = min(first + rounds, groups) - 1;  // this wave's
-  int group = first + blockIdx.x / 8 % rounds;
-  if (group > last) group = first;
-  if (first <= last) load_b(bv, group);
+  const auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  if (issue_left > 0) aim();
 #pragma unroll 1
-  for (int left = last - first + 1; left > 0; --left) {
-    const int after = group == last ? first : group + 1;
-    const int s0 = group * kGroup;
-    const uint32_t b4 = *(const uint32_t*)(bs + s0);
-    uint32_t a4[MT];
+  for (int i = 0; i < L::kSlots && issue_left > 0; ++i) fetch();
+
+  const int row = lane & 15, swap = row >> 1 & 7;
+  const uint32_t lo = row * 128 + ((lane >> 4) ^ swap) * 16, hi = row * 128 + (((lane >> 4) + 4) ^ swap) * 16;
+  int slot = 0;
+  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    f32x4_t acc[MT] = {};
+    int step = start;
+#pragma unroll 1
+    for (int i = begin; i < end; ++i) {
+      if (total >= L::kSlots) wait_vm<(L::kSlots - 1) * L::kLoads>();
+      else wait_vm<0>();
+      --total;
+      const uint8_t* s = lds + ring + slot * L::kSlot;
+      if (++slot == L::kSlots) slot = 0;
+      const i32x8_t bv = join(*(const i32x4_t*)(s + lo), *(const i32x4_t*)(s + hi));
+      i32x8_t av[MT];
+      uint32_t sa[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) a4[i] = *(const uint32_t*)(g.a_scales + as_at[i] + s0);
-    i32x8_t av[2][MT];
-    load_a(av[0], s0);
-    if (left > 1) load_b(bn, after);
+      for (int k = 0; k < MT; ++k) {
+        const uint8_t* p = s + (1 + k) * 2048;
+        av[k] = join(*(const i32x4_t*)(p + lo), *(const i32x4_t*)(p + hi));
+        sa[k] = *(const uint32_t*)(s + (1 + MT) * 2048 + (k * 16 + row) * 4);
+      }
+      const int by = 8 * (step & (kGroup - 1));
+      const uint32_t sb = *(const uint32_t*)(s + (1 + MT) * 2048 + 256) >> by & 255;
+      if (++step == end) step = begin;
+      wait_lds();
+      if (issue_left > 0) fetch();
+      const auto fb = W::make(bv, sb);
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j) {
-      if (j + 1 < kGroup) load_a(av[(j + 1) & 1], s0 + j + 1);  // (past the end of k: zeros)
-      const uint32_t sb = s0 + j < steps ? b4 >> (8 * j) & 255 : 0;
-      const auto fb = W::make(bv[j], sb);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const uint32_t sa = s0 + j < steps ? a4[i] >> (8 * j) & 255 : 0;  // (there may be anything past the last scale)
-        acc[i] = W::mul(fb, W::make(av[j & 1][i], sa), acc[i], sb, sa);
+      for (int k = 0; k < MT; ++k) {
+        const uint32_t s1 = sa[k] >> by & 255;
+        acc[k] = W::mul(fb, W::make(av[k], s1), acc[k], sb, s1);
       }
     }
+    if (steps * kStep < g.k && wave == WAVES - 1) {  // the last, partial step: zeros behind the end of k
+      const int kl = (lane >> 4) * 16, k0 = steps * kStep, by = 8 * (steps & (kGroup - 1)), group = steps & ~(kGroup - 1);
+      const uint8_t* b = g.b + (long long)min(tile * 16 + row, g.n - 1) * g.b_stride + kl;
+      const uint32_t sb = *(const uint32_t*)(g.b_scales + (long long)(tile / 8) * g.b_scale_stride + group) >> by & 255;
+      const auto fb = W::make(join(load_chunk(b, k0, g.k - kl), load_chunk(b, k0 + 64, g.k - kl)), sb);
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j) bv[j] = bn[j];
-    group = after;
-  }
+      for (int k = 0; k < MT; ++k) {
+        const long long r = min(k * 16 + row, g.m - 1);
+        const uint8_t* a = g.a + r * g.a_stride + kl;
+        const uint32_t s1 = *(const uint32_t*)(g.a_scales + r * g.a_scale_stride + group) >> by & 255;
+        acc[k] = W::mul(fb, W::make(join(load_chunk(a, k0, g.k - kl), load_chunk(a, k0 + 64, g.k - kl)), s1), acc[k], sb, s1);
+      }
+    }
+    f32x4_t* part = (f32x4_t*)lds;
 #pragma unroll
-  for (int i = 0; i < MT; ++i) part[(wave * MT + i) * 64 + lane] = acc[i];
-  __syncthreads();
-  for (int at = t; at < MT * 64; at += blockDim.x) {
-    f32x4_t sum = part[at];
-    for (int w = 1; w < waves; ++w) sum += part[w * MT * 64 + at];
-    const int row = at / 64 * 16 + (at & 15), col = n0 + (at & 63) / 16 * 4;
-    if (row < g.m && col < g.n) store_columns((T*)g.c + (long long)row * g.c_stride + col, g.n - col, sum);
+    for (int k = 0; k < MT; ++k) part[(wave * MT + k) * 64 + lane] = acc[k];
+    barrier();
+    if (wave < MT) {
+      f32x4_t sum = part[t];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) sum += part[w * MT * 64 + t];
+      const int r = wave * 16 + row, col = tile * 16 + (lane >> 4) * 4;
+      if (r < g.m && col < g.n) store_columns((T*)g.c + (long long)r * g.c_stride + col, g.n - col, sum);
+    }
+    barrier();
   }
 }
 
@@ -582,15 +625,14 @@ __global__ __launch_bounds__(256) void matmul_add_kernel(MatmulArgs g, const flo
   store_columns((T*)g.c + row * g.c_stride + col, g.n - col, sum);
 }
 
-template <typename T, int MT>
-void rows_form(const MatmulArgs& g, hipStream_t st) {
-  const int groups = ((g.k + kStep - 1) / kStep + kGroup - 1) / kGroup;
-  // Up to eight waves, all with as many groups; up to four where there are two such workgroups for every compute unit (1 x 12288 x 4096:
-  // 10.3 us with four, with two groups each, 11.9 with two; 1 x 4096 x 11008: 11.7 with four, 10.6 with eight).
-  const int most = MT == 1 && g.n >= 2 * kComputeUnits * 16 ? 4 : 8;
-  const int rounds = (groups + most - 1) / most, waves = (groups + rounds - 1) / rounds;
-  const int bytes = waves * MT * 1024;
-  matmul_rows_kernel<T, MT><<<(g.n + 15) / 16, waves * 64, bytes, st>>>(g);
+template <typename T, int MT, int PER_UNIT, int kWaves>
+void strip_form(const MatmulArgs& g, hipStream_t st) {
+  constexpr int kRoom = 163840 / PER_UNIT;
+  typedef StripLds<MT, kWaves, kRoom> L;
+  static const hipError_t raised =
+      hipFuncSetAttribute((const void*)matmul_strip_kernel<T, MT, kWaves, kRoom>, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+  (void)raised;
+  matmul_strip_kernel<T, MT, kWaves, kRoom><<<std::min((g.n + 15) / 16, kComputeUnits * PER_UNIT), kWaves * 64, L::kBytes, st>>>(g);
 }
 
 template <typename T, int BM, int BN, int WM, int WN, int ST>
@@ -612,11 +654,11 @@ void tile_form(const MatmulArgs& g, TilePlan plan, hipStream_t st) {
 // Up to 16 rows: the stream of B.  Else the form that a model of its time says is the fastest.  A tile's time is its half
 // blocks' times what an iteration takes, from measurements (k = 4096, us an iteration; few / all compute units at work):
 //   256 x 256  0.57 / 0.84 (power)   128 x 128  0.26 / 0.34   64 x 64  0.147 / 0.147 (rate of L2)   fp32: 128 x 128  0.30 / 0.44
-// A tile's start and end cost about 3 us; parts of k cost a second launch and the traffic of the parts; the stream of B takes 2.6 us for a
-// group of four blocks and 16 rows on each of a compute unit's eight waves, and 2 us more for each further 16 rows.
-// 512 x 4096 x 4096: 64-tiles 21.1, 128-tiles 20.3; 1024 x 11008 x 4096: 128-tiles 66.7, 256-tiles 55.4; 32 x 12288 x 4096: the stream of B 24.6,
-// 64-tiles 13.2.
-enum Form { kRows, kTile64, kTile128, kTile256 };
+// A tile's start and end cost about 3 us; parts of k cost a second launch and the traffic of the parts; the stream of B takes 0.36, 0.5
+// or 0.68 us for a step of each of a compute unit's waves, with up to 32, 48 and 64 rows.
+// 512 x 4096 x 4096: 64-tiles 21.1, 128-tiles 20.3; 1024 x 11008 x 4096: 128-tiles 66.7, 256-tiles 55.4; 32 x 12288 x 4096: the stream of B 10.4,
+// 64-tiles 13.5; 64 x 12288 x 4096: 16.3 and 14.4; 48 x 4096 x 11008: 12.5 and 17.0.
+enum Form { kStrip, kTile64, kTile128, kTile256 };
 struct Choice {
   Form form;
   int splits, groups;  // parts of k, groups of four blocks each
@@ -624,13 +666,14 @@ struct Choice {
 constexpr size_t kMostScratch = 32u << 20;
 Choice choose(int m, int n, int k, bool exact, size_t scratch) {
   const int groups = ((k + kStep - 1) / kStep + kGroup - 1) / kGroup;
-  if (m <= 16) return {kRows, 1, groups};
+  if (m <= 16) return {kStrip, 1, groups};
   Choice best = {kTile128, 1, groups};
   double least = 1e30;
   if (m <= 64) {
-    const double rounds = ceil((n + 15) / 16 / (double)kComputeUnits);
-    least = 3 + rounds * (1.5 + ((groups + 7) / 8) * (0.6 + 2.0 * ((m + 15) / 16)));
-    best.form = kRows;
+    const double a_step[] = {0.36, 0.36, 0.5, 0.68};
+    const double rounds = ceil((n + 15) / 16 / (double)kComputeUnits), steps = ceil(k / (double)(4 * kStep));
+    least = 2.5 + fmax((double)n * k / 5.2e6, rounds * steps * a_step[(m - 1) / 16]);
+    best.form = kStrip;
   }
   const struct { Form form; int edge; double few, all; } forms[] = {
       {kTile64, 64, exact ? 0.23 : 0.147, exact ? 0.36 : 0.147}, {kTile128, 128, exact ? 0.30 : 0.26, exact ? 0.44 : 0.34}, {kTile256, 256, 0.57, 0.84}};
@@ -658,11 +701,14 @@ void matmul(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStr
   Choice c = choose(g.m, g.n, g.k, kExact, kMostScratch);
   // (without the room that was asked for: no parts)
   if (c.splits > 1 && (!workspace || workspace_bytes < matmul_workspace(g.m, g.n, g.k))) c = choose(g.m, g.n, g.k, kExact, 0);
-  if (c.form == kRows) {
-    if (g.m <= 16) return rows_form<T, 1>(g, st);
-    if (g.m <= 32) return rows_form<T, 2>(g, st);
-    if (g.m <= 48) return rows_form<T, 3>(g, st);
-    return rows_form<T, 4>(g, st);
+  if (c.form == kStrip) {
+    // Several workgroups to a compute unit where there are columns for them, eight waves else (1 x 5120 x 5120: three workgroups 6.4 us, two
+    // 7.6, one 8.9; 1 x 4096 x 4096: eight waves 4.7, four 5.2; 32 x 12288 x 4096: two workgroups 10.4, one 12.0).
+    const bool more = g.n > 16 * kComputeUnits;
+    if (g.m <= 16) return more ? strip_form<T, 1, 3, 4>(g, st) : strip_form<T, 1, 2, 8>(g, st);
+    if (g.m <= 32) return more ? strip_form<T, 2, 2, 4>(g, st) : strip_form<T, 2, 1, 8>(g, st);
+    if (g.m <= 48) return more ? strip_form<T, 3, 2, 4>(g, st) : strip_form<T, 3, 1, 8>(g, st);
+    return strip_form<T, 4, 1, 4>(g, st);
   }
   TilePlan plan = {};
   plan.splits = c.splits;

@@ -267,6 +267,23 @@ def test_matmul_of_whole_numbers_is_exact(m, n, k, dtype, workspace):
     assert bool((torch.as_strided(c._base, (m, 3), (n + 3, 1), 1 + n) == 99).all()) and float(c._base[0]) == 99
 
 
+@pytest.mark.parametrize("m", [1, 15, 16, 17, 33, 48, 49, 64])
+@pytest.mark.parametrize("n,k", [(4096, 127), (4097, 128), (5003, 700), (8200, 1152), (13000, 513), (21000, 2048)])
+def test_matmul_of_few_rows_and_many_columns_is_exact(m, n, k):
+    """Several strips of columns to a workgroup, parts of k of no, one and several steps."""
+    g = rng(16, m, n, k)
+    (a, sa), (b, sb) = operands(g, m, n, k, True)
+    ta, tsa = filled(m, k, a, sa, 16)
+    tb, tsb = filled(n, k, b, sb, 0)
+    want = torch.from_numpy(L.values(a, sa)).cuda() @ torch.from_numpy(L.values(b, sb, 128)).cuda().t()
+    for dtype in (torch.bfloat16, torch.float32):
+        c = on_gpu(np.zeros((m, n)), dtype, stride=n + 5, offset=3)
+        c._base.fill_(99.0)
+        B.a2sf_matmul_scaled(ta, tsa, tb, tsb, c)
+        assert torch.equal(c, want.to(dtype)), (c.double() - want).abs().max()
+        assert bool((torch.as_strided(c._base, (m, 5), (n + 5, 1), 3 + n) == 99).all()) and bool((c._base[:3] == 99).all())
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 300, 1000), (7, 777, 4096), (40, 200, 333), (150, 700, 2000), (300, 300, 8000), (1030, 600, 500)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_matmul(m, n, k, dtype):
