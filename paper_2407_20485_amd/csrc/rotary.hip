@@ -56,6 +56,7 @@ struct Chunk {
 // their own elements only, so a part may be turned in place.  Any stride and alignment; WHOLE: no item is shorter than 16 bytes.
 // 8 x 2048 tokens of 96 heads of 128 in bf16 (805 MB): halves 156 us = 5.2 TB/s, neighbours 150 = 5.4 (a copy of 1 GiB: 5.2).  With one item of all
 // parts' heads in turn per lane, whose strides are then looked up lane by lane, 165 and 181.
+// 16 tokens of 48 heads of 128: 3.3 us with a head to a lane, 4.6 with four.
 constexpr int kHeads = 4;
 
 template <typename T, bool NEIGHBOURS, bool WHOLE>
@@ -66,11 +67,11 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   for (int k = 1; k < A2SF_MAX_ROTARY_PARTS; ++k) part += blockIdx.x >= a.first_block[k];
   const RotaryPart& P = a.part[part];
   const int local = threadIdx.x;
-  const long long token = (long long)(blockIdx.x - a.first_block[part]) * P.tokens_per_block + local / P.lanes;
+  const uint32_t token = (blockIdx.x - a.first_block[part]) * (uint32_t)P.tokens_per_block + (uint32_t)(local / P.lanes);  // (below 2^29)
   const int lane = local % P.lanes;
-  if (local >= P.tokens_per_block * P.lanes || token >= (long long)a.batch * a.length) return;
+  if (local >= P.tokens_per_block * P.lanes || token >= (uint32_t)a.batch * (uint32_t)a.length) return;
   const int item = lane % a.items, head_step = P.lanes / a.items;
-  const int b = (int)(token / a.length), i = (int)(token - (long long)b * a.length);
+  const int b = (int)(token / (uint32_t)a.length), i = (int)(token - (uint32_t)b * (uint32_t)a.length);
   const int half = a.rot / 2;
   const bool turns = item < a.turning;
   if (!(turns && P.rotate) && P.in_place) return;
@@ -182,13 +183,15 @@ void rotary(RotaryArgs a, bool neighbours, hipStream_t st) {
   a.items = a.turning + (a.d - a.rot + W - 1) / W;
   const bool whole = turned % W == 0 && (a.d - a.rot) % W == 0;
   const long long tokens = (long long)a.batch * a.length;
+  const bool few = tokens <= 256;
   uint32_t grid = 0;
   for (int k = 0; k < A2SF_MAX_ROTARY_PARTS; ++k) {
     a.first_block[k] = k < a.parts ? grid : 0xFFFFFFFFu;
     if (k >= a.parts) continue;
-    // as many lanes for a token as have kHeads heads each, fewer where a workgroup has no more; several tokens per workgroup
+    // as many lanes for a token as have kHeads heads each (one each if there are too few tokens to fill the chip anyway), fewer where a
+    // workgroup has no more; several tokens per workgroup
     RotaryPart& P = a.part[k];
-    const long long want = (long long)((P.heads + kHeads - 1) / kHeads) * a.items;
+    const long long want = (long long)(few ? P.heads : (P.heads + kHeads - 1) / kHeads) * a.items;
     P.lanes = want < 256 ? (int)want : 256 / a.items * a.items;
     P.tokens_per_block = 256 / P.lanes;
     grid += (uint32_t)((tokens + P.tokens_per_block - 1) / P.tokens_per_block);
