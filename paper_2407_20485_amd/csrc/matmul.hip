@@ -657,7 +657,8 @@ void tile_form(const MatmulArgs& g, TilePlan plan, hipStream_t st) {
 // A tile's start and end cost about 3 us; parts of k cost a second launch and the traffic of the parts; the stream of B takes 0.36, 0.5
 // or 0.68 us for a step of each of a compute unit's waves, with up to 32, 48 and 64 rows.
 // 512 x 4096 x 4096: 64-tiles 21.1, 128-tiles 20.3; 1024 x 11008 x 4096: 128-tiles 66.7, 256-tiles 55.4; 32 x 12288 x 4096: the stream of B 10.4,
-// 64-tiles 13.5; 64 x 12288 x 4096: 16.3 and 14.4; 48 x 4096 x 11008: 12.5 and 17.0.
+// 64-tiles 13.5; 64 x 12288 x 4096: 16.3 and 14.4; 48 x 4096 x 11008: 12.5 and 17.0; 512 x 12288 x 4096: 128-tiles (one or two to a
+// compute unit) 36.4, 256-tiles 42.6; 700 x 8192 x 8192: 70 and 78; 512 x 22016 x 4096: 67 and 58.
 enum Form { kStrip, kTile64, kTile128, kTile256 };
 struct Choice {
   Form form;
@@ -685,7 +686,11 @@ Choice choose(int m, int n, int k, bool exact, size_t scratch) {
       const double parts = splits > 1 ? (double)splits * m * n * 4 : 0;
       if (parts > (double)scratch) break;
       const double t = f.few + (f.all - f.few) * fmin(1.0, tiles * splits / kComputeUnits);
-      const double us = 3 + ceil(tiles * splits / kComputeUnits) * (3 + 2 * kGroup * (double)per * t) + (splits > 1 ? 2.5 + 2 * parts / 4e6 : 0);
+      // (two 128-tiles share a compute unit, whose other half may have nothing to do)
+      const double units = tiles * splits / kComputeUnits;
+      const bool together = f.form == kTile128 && units <= 2;
+      const double rounds = together ? fmax(1.0, units) : ceil(units);
+      const double us = 3 + (together ? 3 : 3 * rounds) + rounds * 2 * kGroup * per * t + (splits > 1 ? 2.5 + 2 * parts / 4e6 : 0);
       if (us < least) {
         least = us;
         best = {f.form, splits, per};
