@@ -6,13 +6,37 @@
 namespace a2sf {
 namespace {
 
+__device__ __forceinline__ double wave_sum_f64(double v) {
+  const auto halves = [](double x) { return __builtin_bit_cast(unsigned long long, x); };
+  const auto whole = [](uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo); };
+  const auto add = [&](auto move) {
+    const unsigned long long x = halves(v);
+    v += whole(move((uint32_t)x), move((uint32_t)(x >> 32)));
+  };
+  add([](uint32_t x) { return dpp_move_u32<0xB1>(x); });
+  add([](uint32_t x) { return dpp_move_u32<0x4E>(x); });
+  add([](uint32_t x) { return dpp_move_u32<0x141>(x); });
+  add([](uint32_t x) { return dpp_move_u32<0x140>(x); });
+  unsigned long long x = halves(v);
+  u32x2_t lo = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+  u32x2_t hi = __builtin_amdgcn_permlane16_swap((uint32_t)(x >> 32), (uint32_t)(x >> 32), false, false);
+  v = whole(lo[0], hi[0]) + whole(lo[1], hi[1]);
+  x = halves(v);
+  lo = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+  hi = __builtin_amdgcn_permlane32_swap((uint32_t)(x >> 32), (uint32_t)(x >> 32), false, false);
+  return whole(lo[0], hi[0]) + whole(lo[1], hi[1]);
+}
+
 // ---- y = h / sqrt(mean(h^2) + eps) * w,  h = x + residual ----------------------------------------------------------------
 // A row stays in registers between the sum of its squares and its scaling: V units of eight elements per lane, unit
 // i * THREADS + t in lane t, so that 16 neighbouring lanes hold the 128 columns of a scale and the wave's accesses are
-// contiguous.  h is formed, squared, summed and scaled in fp32; only the stored sum is rounded to the rows' type (the norm is
-// of the sum before that rounding, which costs nothing here and is nearer to the definition).
+// contiguous.  h is formed and squared in fp32; only the stored sum is rounded to the rows' type (the norm is of the sum before that
+// rounding, which costs nothing here and is nearer to the definition).  The squares of a unit are added in fp32, the units in 64 bits, and
+// h is multiplied with what the roundings of its products cut off: then y is off by about one rounding to 32 bits, and next to
+// none of its roundings to 8 bits go another way than the definition's.  (The memory leaves time for it.)
 // THREADS = 64: a wave per row, four rows per workgroup, no barrier.
-// 16384 x 5120 in bf16 with a residual, its sum and 8-bit rows (587 MB): 111 us = 5.3 TB/s (a copy of 1 GiB: 5.2).
+// 16384 x 5120 in bf16 with a residual, its sum and 8-bit rows (588 MB): 113 us = 5.2 TB/s (a copy of 1 GiB: 5.2); 109 without the products' remainders,
+// but then every 300 000th 8-bit value is rounded the other way, now every 3 000 000th.
 template <typename T, int THREADS, int V>
 __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel(NormArgs a) {
   constexpr int kRows = THREADS == 64 ? 4 : 1;
@@ -22,7 +46,6 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel
   const T* x = (const T*)a.x + row * a.x_stride;
   const T* r = a.residual ? (const T*)a.residual + row * a.residual_stride : nullptr;
   float h[V][kUnit];
-  float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < V; ++i) load_unit(x + (i * THREADS + t) * kUnit, a.n - (i * THREADS + t) * kUnit, h[i]);
   if (r) {
@@ -34,20 +57,25 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel
       for (int j = 0; j < kUnit; ++j) h[i][j] += g[j];
     }
   }
+  double sum = 0.0;
 #pragma unroll
-  for (int i = 0; i < V; ++i)
+  for (int i = 0; i < V; ++i) {
+    float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) sum = fmaf(h[i][j], h[i][j], sum);
-  sum = wave_sum(sum);
+    for (int j = 0; j < kUnit; ++j) s = fmaf(h[i][j], h[i][j], s);
+    sum += s;
+  }
+  sum = wave_sum_f64(sum);
   if constexpr (THREADS > 64) {
-    __shared__ float part[THREADS / 64];
+    __shared__ double part[THREADS / 64];
     if ((t & 63) == 0) part[t >> 6] = sum;
     __syncthreads();
-    sum = 0.f;
+    sum = 0.0;
 #pragma unroll
     for (int w = 0; w < THREADS / 64; ++w) sum += part[w];
   }
-  const float scale = 1.0f / sqrtf(sum / (float)a.n + a.eps);
+  const double factor = 1.0 / sqrt(sum / a.n + a.eps);
+  const float scale = (float)factor, rest = (float)(factor - scale);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int c = (i * THREADS + t) * kUnit;
@@ -58,13 +86,27 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel
     float w[kUnit];
     load_unit((const T*)a.weight + c, have, w);
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) h[i][j] = h[i][j] * scale * w[j];
+    for (int j = 0; j < kUnit; ++j) {
+      const float p = h[i][j] * scale, y = p * w[j];
+      // (not a number where y is infinite: which it then stays)
+      const float low = fmaxf(fmaf(fmaf(h[i][j], rest, fmaf(h[i][j], scale, -p)), w[j], fmaf(p, w[j], -y)), -3.402823466e38f);
+      h[i][j] = y + low;
+      w[j] = low - (h[i][j] - y);  // what this addition cut off
+    }
     if (have < kUnit) {
       // columns past the end are 0 also where the row's scale is not a number
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) h[i][j] = j < have ? h[i][j] : 0.f;
     }
-    if (a.out && have > 0) store_unit((T*)a.out + row * a.out_stride + c, have, h[i]);
+    if (sizeof(T) == 4 && a.out && have > 0) store_unit((T*)a.out + row * a.out_stride + c, have, h[i]);
+    // What is rounded once more is cut off at 32 bits, and its last bit set if anything was: then it does not look like half-way between
+    // two neighbours where it is not.
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) {
+      const int bits = __float_as_int(h[i][j]);
+      h[i][j] = fabsf(w[j]) > 0.f ? __int_as_float((bits + ((__float_as_int(w[j]) ^ bits) >> 31)) | 1) : h[i][j];
+    }
+    if (sizeof(T) == 2 && a.out && have > 0) store_unit((T*)a.out + row * a.out_stride + c, have, h[i]);
     if (a.q) {
       const uint32_t b = scale_byte(block_top(unit_top(h[i])));
       if (have > 0) store_eight_bits(a.q + row * a.q_stride + c, have, to_eight_bits(h[i], b));
