@@ -32,11 +32,11 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
 // i * THREADS + t in lane t, so that 16 neighbouring lanes hold the 128 columns of a scale and the wave's accesses are
 // contiguous.  h is formed and squared in fp32; only the stored sum is rounded to the rows' type (the norm is of the sum before that
 // rounding, which costs nothing here and is nearer to the definition).  The squares of a unit are added in fp32, the units in 64 bits, and
-// h is multiplied with what the roundings of its products cut off: then y is off by about one rounding to 32 bits, and next to
-// none of its roundings to 8 bits go another way than the definition's.  (The memory leaves time for it.)
+// h is multiplied with what the roundings of its products cut off: then y is off by about one rounding to 32 bits, and
+// next to none of its 8-bit values is another than the definition's.
 // THREADS = 64: a wave per row, four rows per workgroup, no barrier.
 // 16384 x 5120 in bf16 with a residual, its sum and 8-bit rows (588 MB): 113 us = 5.2 TB/s (a copy of 1 GiB: 5.2); 109 without the products' remainders,
-// but then every 300 000th 8-bit value is rounded the other way, now every 3 000 000th.
+// but then one 8-bit value in 1 500 000 goes the other way, now one in 12 000 000.
 template <typename T, int THREADS, int V>
 __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel(NormArgs a) {
   constexpr int kRows = THREADS == 64 ? 4 : 1;
@@ -125,24 +125,24 @@ void norm_units(const NormArgs& a, hipStream_t st) {
   const int v = (a.n + THREADS * kUnit - 1) / (THREADS * kUnit);
   if (v <= 1) return norm<T, THREADS, 1>(a, st);
   if (v <= 2) return norm<T, THREADS, 2>(a, st);
-  if constexpr (THREADS > 64) {
-    if (v <= 3) return norm<T, THREADS, 3>(a, st);
+  if (v <= 3) return norm<T, THREADS, 3>(a, st);
+  if constexpr (THREADS != 256) {
     if (v <= 4) return norm<T, THREADS, 4>(a, st);
-    if constexpr (THREADS == 256) {
-      if (v <= 6) return norm<T, THREADS, 6>(a, st);
-    }
-    return norm<T, THREADS, 8>(a, st);
   }
+  if constexpr (THREADS == 1024) return norm<T, THREADS, 8>(a, st);
 }
 template <typename T>
 void norm_type(const NormArgs& a, hipStream_t st) {
-  if (a.n <= 2 * 64 * kUnit) return norm_units<T, 64>(a, st);
+  // A wave per row needs no barrier; of 16 bits also where it has four units (16384 x 1280: 31 us, by 256 lanes 40; fp32 47 and 44)
+  if (a.n <= 2 * 64 * kUnit || (sizeof(T) == 2 && a.rows >= 4096 && a.n <= 4 * 64 * kUnit)) return norm_units<T, 64>(a, st);
   if (a.rows < 512 && a.n > 256 * kUnit) {
     // few rows: the time is a chain of round trips, the more lanes the shorter
     if (a.n <= 512 * kUnit) return norm<T, 512, 1>(a, st);
     return norm_units<T, 1024>(a, st);
   }
-  if (a.n <= 8 * 256 * kUnit) return norm_units<T, 256>(a, st);
+  // two or three units per lane (7000 x 10000: 98 us by 512 lanes, 120 by 256 with six units; 16384 x 4096: 88 by 256, 99 by 512 with one)
+  if (a.n <= 3 * 256 * kUnit) return norm_units<T, 256>(a, st);
+  if (a.n <= 3 * 512 * kUnit) return norm_units<T, 512>(a, st);
   return norm_units<T, 1024>(a, st);
 }
 

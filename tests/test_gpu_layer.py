@@ -111,6 +111,30 @@ def test_rms_norm(rows, n, dtype):
     assert torch.equal(q2, q3) and torch.equal(s2, s3)
 
 
+@pytest.mark.parametrize("rows,n", [(4100, 1100), (4097, 1999), (513, 2600), (513, 6143), (514, 6145), (512, 12290)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rms_norm_many_rows(rows, n, dtype):
+    test_rms_norm(rows, n, dtype)
+
+
+def test_rms_norm_rounds_to_8_bits_once():
+    """Next to no 8-bit value is another than that of the result in 64 bits: of those the result lies within 2^-22 of half-way (the
+    units' sums of eight squares in 32 bits are off by 8 * 2^-24 at most, their root's by half of that, and the products by less)."""
+    g = rng(19)
+    x, w = on_gpu(g.normal(size=(400, 2048)), torch.bfloat16), on_gpu(1 + 0.1 * g.normal(size=(1, 2048)), torch.bfloat16)[0]
+    q, s = eight(400, 2048)
+    B.a2sf_rms_norm(x, w, 1e-6, q=q, scales=s)
+    h = host(x)
+    y = h / np.sqrt((h ** 2).mean(1, keepdims=True) + float(np.float32(1e-6))) * host(w)
+    at = lambda f: L.quantize(y * (1 + f * 2.0 ** -22))
+    (lo, slo), (hi, shi) = at(-1), at(1)
+    got, gots = q.cpu().numpy(), s.cpu().numpy()
+    same = np.repeat(slo == shi, 128, 1)
+    assert ((got == lo) | (got == hi))[same].all() and ((gots == slo) | (gots == shi)).all()
+    want, _ = L.quantize(y)
+    assert (got != want).sum() <= 5
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rms_norm_in_place(dtype):
     g = rng(1)
