@@ -143,9 +143,9 @@ __device__ __forceinline__ void store_bytes(T* p, int have, u32x4_t v) {
 }
 
 // ---- few rows of A: B is streamed once --------------------------------------------------------------------------------------
-// A workgroup takes 16 columns of C after the other and all rows (MT tiles of 16); its waves share k and add their parts in LDS in a
+// A workgroup takes tiles of up to 64 rows (MT times 16) and 16 columns of C, one after the other; its waves share k and add their parts in LDS in a
 // fixed order.  Each wave streams its part of k of B and A through a ring of its own in LDS, 128 bytes of each row to a slot, and
-// the stream runs on from columns to columns: a wave waits for others at the sums only.
+// the stream runs on from tile to tile: a wave waits for others at the sums only.
 // Bound by the stream of B as long as A is short: a step takes 2 us from its fetch to its arrival, whatever its size, and A's rows
 // take their share of the ring.  By way of LDS and not straight into registers, where an operand's lanes, each in another
 // row, ask for 16 bytes at a time of 64 places: 48 x 4096 x 11008 33 us, so 12.5; 1 x 4096 x 11008 10.5, so 8.7.
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(WAVES * 64) void matmul_strip_kernel(MatmulArgs g) 
   static_assert(MT <= WAVES, "a lane stores one part of a tile at most");
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63;
-  const int tiles = (g.n + 15) / 16, steps = g.k / kStep;
+  const int strips = (g.n + 15) / 16, tiles = strips * ((g.m + MT * 16 - 1) / (MT * 16)), steps = g.k / kStep;
   const int each = (steps + WAVES - 1) / WAVES, begin = min(wave * each, steps), end = min(begin + each, steps);
   const int mine = ((int)blockIdx.x < tiles ? (tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0);
   int total = mine * (end - begin), issue_left = total;  // steps still to multiply, to fetch
@@ -179,34 +179,41 @@ __global__ __launch_bounds__(WAVES * 64) void matmul_strip_kernel(MatmulArgs g) 
   // meet all banks once.
   const int chunk = (lane & 7) ^ (lane >> 4);
   uint32_t a_off[2 * MT], b_off[2];
-#pragma unroll
-  for (int u = 0; u < 2 * MT; ++u)
-    a_off[u] = (uint32_t)min(u * 8 + (lane >> 3), g.m - 1) * (uint32_t)g.a_stride + (uint32_t)(chunk ^ (u & 1) * 4) * 16;
-  const uint32_t scale_off = (uint32_t)min(lane, g.m - 1) * (uint32_t)g.a_scale_stride;
+  uint32_t scale_off;
+  const uint8_t *a_tile, *as_tile, *b_tile, *bs_tile;
   const int start = end > begin ? begin + (int)(blockIdx.x / 8) % (end - begin) : 0;
   int at_tile = blockIdx.x, at_step = start, at_slot = 0;  // of the next fetch
+  const auto part_of = [&](int tile) { return tile < strips ? 0 : (int)((unsigned)tile / (unsigned)strips); };
   const auto aim = [&] {
+    const int part = part_of(at_tile), strip = at_tile - part * strips, m0 = part * (MT * 16);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-      b_off[u] = (uint32_t)min(u * 8 + (lane >> 3), g.n - 1 - at_tile * 16) * (uint32_t)g.b_stride + (uint32_t)(chunk ^ u * 4) * 16;
+      b_off[u] = (uint32_t)min(u * 8 + (lane >> 3), g.n - 1 - strip * 16) * (uint32_t)g.b_stride + (uint32_t)(chunk ^ u * 4) * 16;
+#pragma unroll
+    for (int u = 0; u < 2 * MT; ++u)
+      a_off[u] = (uint32_t)min(u * 8 + (lane >> 3), g.m - 1 - m0) * (uint32_t)g.a_stride + (uint32_t)(chunk ^ (u & 1) * 4) * 16;
+    scale_off = (uint32_t)min(lane, g.m - 1 - m0) * (uint32_t)g.a_scale_stride;
+    a_tile = g.a + (long long)m0 * g.a_stride;
+    as_tile = g.a_scales + (long long)m0 * g.a_scale_stride;
+    b_tile = g.b + (long long)strip * 16 * g.b_stride;
+    bs_tile = g.b_scales + (long long)(strip / 8) * g.b_scale_stride;
   };
   const auto fetch = [&] {
     const uint32_t to = ring + at_slot * L::kSlot;
-    const uint8_t* b = g.b + (long long)at_tile * 16 * g.b_stride + at_step * kStep;
-    const uint8_t* a = g.a + at_step * kStep;
+    const uint8_t *b = b_tile + at_step * kStep, *a = a_tile + at_step * kStep;
     dma16(b, b_off[0], to);
     dma16(b, b_off[1], to + 1024);
 #pragma unroll
     for (int u = 0; u < 2 * MT; ++u) dma16(a, a_off[u], to + 2048 + u * 1024);
     const int group = at_step & ~(kGroup - 1);
-    dma4(g.a_scales + group, scale_off, to + (1 + MT) * 2048);
-    dma4(g.b_scales + (long long)(at_tile / 8) * g.b_scale_stride + group, 0, to + (1 + MT) * 2048 + 256);
+    dma4(as_tile + group, scale_off, to + (1 + MT) * 2048);
+    dma4(bs_tile + group, 0, to + (1 + MT) * 2048 + 256);
     --issue_left;
     if (++at_slot == L::kSlots) at_slot = 0;
     if (++at_step == end) at_step = begin;
     if (at_step == start) {
       at_tile += gridDim.x;
-      aim();
+      if (issue_left > 0) aim();
     }
   };
   const auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
@@ -218,6 +225,7 @@ __global__ __launch_bounds__(WAVES * 64) void matmul_strip_kernel(MatmulArgs g) 
   const uint32_t lo = row * 128 + ((lane >> 4) ^ swap) * 16, hi = row * 128 + (((lane >> 4) + 4) ^ swap) * 16;
   int slot = 0;
   for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const int part = part_of(tile), strip = tile - part * strips, m0 = part * (MT * 16);
     f32x4_t acc[MT] = {};
     int step = start;
 #pragma unroll 1
@@ -250,26 +258,26 @@ __global__ __launch_bounds__(WAVES * 64) void matmul_strip_kernel(MatmulArgs g) 
     }
     if (steps * kStep < g.k && wave == WAVES - 1) {  // the last, partial step: zeros behind the end of k
       const int kl = (lane >> 4) * 16, k0 = steps * kStep, by = 8 * (steps & (kGroup - 1)), group = steps & ~(kGroup - 1);
-      const uint8_t* b = g.b + (long long)min(tile * 16 + row, g.n - 1) * g.b_stride + kl;
-      const uint32_t sb = *(const uint32_t*)(g.b_scales + (long long)(tile / 8) * g.b_scale_stride + group) >> by & 255;
+      const uint8_t* b = g.b + (long long)min(strip * 16 + row, g.n - 1) * g.b_stride + kl;
+      const uint32_t sb = *(const uint32_t*)(g.b_scales + (long long)(strip / 8) * g.b_scale_stride + group) >> by & 255;
       const auto fb = W::make(join(load_chunk(b, k0, g.k - kl), load_chunk(b, k0 + 64, g.k - kl)), sb);
 #pragma unroll
       for (int k = 0; k < MT; ++k) {
-        const long long r = min(k * 16 + row, g.m - 1);
+        const long long r = min(m0 + k * 16 + row, g.m - 1);
         const uint8_t* a = g.a + r * g.a_stride + kl;
         const uint32_t s1 = *(const uint32_t*)(g.a_scales + r * g.a_scale_stride + group) >> by & 255;
         acc[k] = W::mul(fb, W::make(join(load_chunk(a, k0, g.k - kl), load_chunk(a, k0 + 64, g.k - kl)), s1), acc[k], sb, s1);
       }
     }
-    f32x4_t* part = (f32x4_t*)lds;
+    f32x4_t* left = (f32x4_t*)lds;
 #pragma unroll
-    for (int k = 0; k < MT; ++k) part[(wave * MT + k) * 64 + lane] = acc[k];
+    for (int k = 0; k < MT; ++k) left[(wave * MT + k) * 64 + lane] = acc[k];
     barrier();
     if (wave < MT) {
-      f32x4_t sum = part[t];
+      f32x4_t sum = left[t];
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) sum += part[w * MT * 64 + t];
-      const int r = wave * 16 + row, col = tile * 16 + (lane >> 4) * 4;
+      for (int w = 1; w < WAVES; ++w) sum += left[w * MT * 64 + t];
+      const int r = m0 + wave * 16 + row, col = strip * 16 + (lane >> 4) * 4;
       if (r < g.m && col < g.n) store_columns((T*)g.c + (long long)r * g.c_stride + col, g.n - col, sum);
     }
     barrier();
@@ -632,7 +640,8 @@ void strip_form(const MatmulArgs& g, hipStream_t st) {
   static const hipError_t raised =
       hipFuncSetAttribute((const void*)matmul_strip_kernel<T, MT, kWaves, kRoom>, hipFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
   (void)raised;
-  matmul_strip_kernel<T, MT, kWaves, kRoom><<<std::min((g.n + 15) / 16, kComputeUnits * PER_UNIT), kWaves * 64, L::kBytes, st>>>(g);
+  const int tiles = (g.n + 15) / 16 * ((g.m + MT * 16 - 1) / (MT * 16));
+  matmul_strip_kernel<T, MT, kWaves, kRoom><<<std::min(tiles, kComputeUnits * PER_UNIT), kWaves * 64, L::kBytes, st>>>(g);
 }
 
 template <typename T, int BM, int BN, int WM, int WN, int ST>
@@ -653,31 +662,41 @@ void tile_form(const MatmulArgs& g, TilePlan plan, hipStream_t st) {
 // ---- which form ------------------------------------------------------------------------------------------------------------------
 // Up to 16 rows: the stream of B.  Else the form that a model of its time says is the fastest.  A tile's time is its half
 // blocks' times what an iteration takes, from measurements (k = 4096, us an iteration; few / all compute units at work):
-//   256 x 256  0.57 / 0.84 (power)   128 x 128  0.26 / 0.34   64 x 64  0.147 / 0.147 (rate of L2)   fp32: 128 x 128  0.30 / 0.44
-// A tile's start and end cost about 3 us; parts of k cost a second launch and the traffic of the parts; the stream of B takes 0.36, 0.5
-// or 0.68 us for a step of each of a compute unit's waves, with up to 32, 48 and 64 rows.
+//   256 x 256  0.57 / 0.84 (power)   128 x 128  0.26 / 0.34   64 x 64  0.147 / 0.17 (rate of L2)   fp32: 128 x 128  0.30 / 0.44
+// A tile's start and end cost 1.6, 2.4 and 3.4 us; parts of k cost a second launch and the traffic of the parts; strips take 0.36, 0.38
+// or 0.62 us for a step of each of a compute unit's four waves, with up to 32, 48 and 64 rows (more rows: several parts of as many), and a
+// little more the longer the stream.
 // 512 x 4096 x 4096: 64-tiles 21.1, 128-tiles 20.3; 1024 x 11008 x 4096: 128-tiles 66.7, 256-tiles 55.4; 32 x 12288 x 4096: the stream of B 10.4,
 // 64-tiles 13.5; 64 x 12288 x 4096: 16.3 and 14.4; 48 x 4096 x 11008: 12.5 and 17.0; 512 x 12288 x 4096: 128-tiles (one or two to a
-// compute unit) 36.4, 256-tiles 42.6; 700 x 8192 x 8192: 70 and 78; 512 x 22016 x 4096: 67 and 58.
+// compute unit) 36.4, 256-tiles 42.6; 700 x 8192 x 8192: 70 and 78; 512 x 22016 x 4096: 67 and 58; 512 x 512 x 2048 (fp32): strips
+// 5.7, tiles 14.1; 128 x 4096 x 4096: 11.8 and 13.6; 1000 x 1000 x 256: 6.4 and 5.1.
 enum Form { kStrip, kTile64, kTile128, kTile256 };
 struct Choice {
   Form form;
   int splits, groups;  // parts of k, groups of four blocks each
 };
 constexpr size_t kMostScratch = 32u << 20;
+constexpr int kStripParts = 16;
+// tiles of 16 rows of each of the parts of up to 64 rows that A is cut into
+int strip_tiles(int m) {
+  const int parts = (m + 63) / 64;
+  return ((m + 15) / 16 + parts - 1) / parts;
+}
 Choice choose(int m, int n, int k, bool exact, size_t scratch) {
   const int groups = ((k + kStep - 1) / kStep + kGroup - 1) / kGroup;
   if (m <= 16) return {kStrip, 1, groups};
   Choice best = {kTile128, 1, groups};
   double least = 1e30;
-  if (m <= 64) {
-    const double a_step[] = {0.36, 0.36, 0.5, 0.68};
-    const double rounds = ceil((n + 15) / 16 / (double)kComputeUnits), steps = ceil(k / (double)(4 * kStep));
-    least = 2.5 + fmax((double)n * k / 5.2e6, rounds * steps * a_step[(m - 1) / 16]);
-    best.form = kStrip;
+  if (m <= 64 * kStripParts && n < 1 << 26) {
+    const double a_step[] = {0.36, 0.36, exact ? 0.5 : 0.38, exact ? 0.74 : 0.62};
+    const int parts = (m + 63) / 64, tiles16 = strip_tiles(m);
+    const double rounds = ceil((n + 15) / 16 * parts / (double)kComputeUnits), steps = ceil(k / (double)(4 * kStep));
+    least = 2.5 + fmax((double)n * k / 5.2e6, rounds * (steps * a_step[tiles16 - 1] * (1 + (tiles16 < 3 ? 0.02 : 0.05) * (rounds - 1)) + 0.25));
+    best = {kStrip, 1, groups};
   }
-  const struct { Form form; int edge; double few, all; } forms[] = {
-      {kTile64, 64, exact ? 0.23 : 0.147, exact ? 0.36 : 0.147}, {kTile128, 128, exact ? 0.30 : 0.26, exact ? 0.44 : 0.34}, {kTile256, 256, 0.57, 0.84}};
+  const struct { Form form; int edge; double ends, few, all; } forms[] = {{kTile64, 64, 1.6, exact ? 0.23 : 0.147, exact ? 0.36 : 0.17},
+                                                                          {kTile128, 128, 2.4, exact ? 0.30 : 0.26, exact ? 0.44 : 0.34},
+                                                                          {kTile256, 256, 3.4, 0.57, 0.84}};
   for (const auto& f : forms) {
     if (exact && f.form == kTile256) continue;  // (its converted operands do not fit the registers)
     const double tiles = ceil(m / (double)f.edge) * ceil(n / (double)f.edge);
@@ -690,7 +709,7 @@ Choice choose(int m, int n, int k, bool exact, size_t scratch) {
       const double units = tiles * splits / kComputeUnits;
       const bool together = f.form == kTile128 && units <= 2;
       const double rounds = together ? fmax(1.0, units) : ceil(units);
-      const double us = 3 + (together ? 3 : 3 * rounds) + rounds * 2 * kGroup * per * t + (splits > 1 ? 2.5 + 2 * parts / 4e6 : 0);
+      const double us = 2.5 + (together ? 1 : rounds) * f.ends + rounds * 2 * kGroup * per * t + (splits > 1 ? 3.5 + 2 * parts / 4e6 : 0);
       if (us < least) {
         least = us;
         best = {f.form, splits, per};
@@ -709,11 +728,13 @@ void matmul(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStr
   if (c.form == kStrip) {
     // Several workgroups to a compute unit where there are columns for them, eight waves else (1 x 5120 x 5120: three workgroups 6.4 us, two
     // 7.6, one 8.9; 1 x 4096 x 4096: eight waves 4.7, four 5.2; 32 x 12288 x 4096: two workgroups 10.4, one 12.0).
-    const bool more = g.n > 16 * kComputeUnits;
-    if (g.m <= 16) return more ? strip_form<T, 1, 3, 4>(g, st) : strip_form<T, 1, 2, 8>(g, st);
-    if (g.m <= 32) return more ? strip_form<T, 2, 2, 4>(g, st) : strip_form<T, 2, 1, 8>(g, st);
-    if (g.m <= 48) return more ? strip_form<T, 3, 2, 4>(g, st) : strip_form<T, 3, 1, 8>(g, st);
-    return strip_form<T, 4, 1, 4>(g, st);
+    const bool more = (long long)g.n * ((g.m + 63) / 64) > 16 * kComputeUnits;
+    switch (strip_tiles(g.m)) {
+      case 1: return more ? strip_form<T, 1, 3, 4>(g, st) : strip_form<T, 1, 2, 8>(g, st);
+      case 2: return more ? strip_form<T, 2, 2, 4>(g, st) : strip_form<T, 2, 1, 8>(g, st);
+      case 3: return more ? strip_form<T, 3, 2, 4>(g, st) : strip_form<T, 3, 1, 8>(g, st);
+      default: return strip_form<T, 4, 1, 4>(g, st);
+    }
   }
   TilePlan plan = {};
   plan.splits = c.splits;

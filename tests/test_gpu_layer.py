@@ -308,6 +308,13 @@ def test_matmul_of_few_rows_and_many_columns_is_exact(m, n, k):
         assert bool((torch.as_strided(c._base, (m, 5), (n + 5, 1), 3 + n) == 99).all()) and bool((c._base[:3] == 99).all())
 
 
+@pytest.mark.parametrize("m,n,k", [(65, 300, 1100), (66, 2000, 130), (97, 515, 2049), (129, 40, 4000), (200, 4100, 640), (333, 100, 3000),
+                                   (513, 513, 2047), (1000, 33, 5000), (1024, 64, 1024)])
+def test_matmul_of_several_parts_of_rows_is_exact(m, n, k):
+    test_matmul_of_whole_numbers_is_exact(m, n, k, "bf16", False)
+    test_matmul_of_whole_numbers_is_exact(m, n, k, "f32", True)
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 300, 1000), (7, 777, 4096), (40, 200, 333), (150, 700, 2000), (300, 300, 8000), (1030, 600, 500)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_matmul(m, n, k, dtype):
