@@ -227,6 +227,11 @@ struct Scale {
     return {top, per, high, range > 0.f && range < 1e30f ? fminf((float)(kBins - 1) / range, 1e30f) : per * kBinsPerOctave};
   }
 };
+// (of finite numbers)
+__device__ __forceinline__ float next_above(float l) {
+  const int bits = __float_as_int(l);
+  return bits << 1 == 0 ? __int_as_float(1) : __int_as_float(bits + (bits < 0 ? -1 : 1));
+}
 __device__ __forceinline__ float weight(float below) { return __builtin_amdgcn_exp2f(-below); }
 __device__ __forceinline__ uint32_t mass_of(float below) { return (uint32_t)fmaf(weight(below), 2147483648.f, 0.5f); }
 
@@ -237,6 +242,12 @@ struct Target {
   unsigned long long mass;
 };
 
+// The mass with which a share p of `inside` is reached
+__device__ __forceinline__ unsigned long long mass_for(float p, unsigned long long inside) {
+  const unsigned long long mass = p > 0.f ? (unsigned long long)ceil((double)p * (double)inside) : 1ull;
+  return mass < 1 ? 1 : mass > inside ? inside : mass;
+}
+
 __device__ __forceinline__ void clear_bins(SampleShared& s) {
   __syncthreads();
   s.mass[threadIdx.x] = 0;
@@ -244,9 +255,11 @@ __device__ __forceinline__ void clear_bins(SampleShared& s) {
   __syncthreads();
 }
 
-// The bin in which the target is reached and what lies before it; s.bin = -1 if there is none.  Returns the total mass.  Four waves
+// The bin in which the target (share < 1: that share of the total mass) is reached and what lies before it; s.bin = -1 if there is none.
+// Returns the total mass.  Four waves
 // do it, a lane four bins: with all sixteen at it the vector units would be four times as long busy with the same few bins.
-__device__ __forceinline__ unsigned long long scan_bins(SampleShared& s, Target to, uint32_t count0, unsigned long long mass0) {
+__device__ __forceinline__ unsigned long long scan_bins(SampleShared& s, Target to, uint32_t count0, unsigned long long mass0,
+                                                        float share = 1.f) {
   __syncthreads();
   if (threadIdx.x == 0) s.bin = -1;  // (everybody has read the last scan's)
   const int t = threadIdx.x, wave = t >> 6;
@@ -267,6 +280,7 @@ __device__ __forceinline__ unsigned long long scan_bins(SampleShared& s, Target 
   unsigned long long total = mass0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) total += s.wave64[w];
+  if (share < 1.f) to.mass = mass_for(share, total);
   if (t < kBins / 4) {
     c += count0;
     m += mass0;
@@ -441,10 +455,6 @@ struct Filters {
   int k;          // tokens, 0: all
   float p, min_p; // p >= 1: all
 };
-__device__ __forceinline__ unsigned long long mass_for(float p, unsigned long long inside) {
-  const unsigned long long mass = p > 0.f ? (unsigned long long)ceil((double)p * (double)inside) : 1ull;
-  return mass < 1 ? 1 : mass > inside ? inside : mass;
-}
 
 // Top-k and top-p on a row, or on a list of a row's first tokens.  inside: the mass that p is a share of where there is no k, 0: that
 // of R.  Whether the cut lies in R: the tokens above -infinity may be fewer than k, and if R holds `all` of them they stay.
@@ -469,21 +479,6 @@ __device__ __forceinline__ bool find_cut(const R& row, const Scale& sc, const Fi
   }
 }
 
-// The sum of every lane's v, which is a whole number below 2^63.
-__device__ __forceinline__ unsigned long long block_sum_u64(unsigned long long v, unsigned long long* left) {
-  uint32_t none = 0;
-  wave_scan(none, v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) left[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = left[threadIdx.x & 15];
-  scan_step<0x111, 0xF>(none, v);
-  scan_step<0x112, 0xF>(none, v);
-  scan_step<0x114, 0xF>(none, v);
-  scan_step<0x118, 0xF>(none, v);
-  return ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 15) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, 15);
-}
-
 // The bin of a row in which the cut by mass (or by more tokens than groups of lanes give) lies.
 struct Zone {
   int bin;                        // -1: none, or the last
@@ -497,24 +492,20 @@ template <typename R>
 __device__ __forceinline__ Zone find_zone(const R& row, const Scale& sc, const Filters& f, bool by_mass, unsigned long long inside,
                                           SampleShared& s) {
   clear_bins(s);
-  // The last bin stays empty: most of a row may lie there, and everybody would add at one address.
-  unsigned long long all = 0;
+  // In the last bin lies, mostly, what has no mass, and may be most of a row: nobody adds it there.
   row.each([&](float l, int) {
     const float below = sc.below(l);
     const uint32_t m = mass_of(below);
-    all += m;
     const uint32_t bin = (uint32_t)fminf(below * kBinsPerOctave, (float)(kBins - 1));
-    if (bin < kBins - 1) {
-      atomicAdd(&s.mass[bin], (unsigned long long)m);
-      if (!by_mass) atomicAdd(&s.count[bin], 1u);
-    }
+    if (m) atomicAdd(&s.mass[bin], (unsigned long long)m);
+    if (!by_mass && bin < kBins - 1) atomicAdd(&s.count[bin], 1u);
   });
-  Zone zone;
-  zone.all = block_sum_u64(all, s.wave64b);  // (its barriers are the bins' too)
+  __syncthreads();
   // (a token of octave o has between 2^(30 - o) and 2^(31 - o))
   if (by_mass) s.count[threadIdx.x] = (uint32_t)(s.mass[threadIdx.x] >> (30u - min(threadIdx.x / 32u, 30u)));
-  scan_bins(s, Target{by_mass, (uint32_t)f.k, by_mass ? mass_for(f.p, inside ? inside : zone.all) : 0}, 0, 0);
-  zone.bin = s.bin;
+  Zone zone;
+  zone.all = scan_bins(s, Target{by_mass, (uint32_t)f.k, inside ? mass_for(f.p, inside) : 0}, 0, 0, by_mass && !inside ? f.p : 1.f);
+  zone.bin = s.bin < kBins - 1 ? s.bin : -1;
   zone.above = s.before_count;
   zone.in = s.in_bin;
   zone.above_mass = s.before_mass;
@@ -556,9 +547,9 @@ struct Runner {
   int at = -1;
   template <bool ANY_ORDER>
   __device__ __forceinline__ void enter(bool in, float below, float log_noise, int index) {
-    const float ring = -below - log_noise;  // (base 2; not a number: never taken)
+    const float ring = in ? -below - log_noise : -kInf;  // (base 2; not a number: never taken)
     z += in ? weight(below) : 0.f;
-    const bool ahead = in && (ring > best || (ANY_ORDER && ring == best && index < at));
+    const bool ahead = ring > best || (ANY_ORDER && ring == best && index < at);
     best = ahead ? ring : best;
     at = ahead ? index : at;
   }
@@ -576,7 +567,9 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
   const float* noise = a.noise && !greedy ? a.noise + r * a.noise_stride : nullptr;
   const float min_p = f.min_p;
   const auto in_share = [&](float l, float below) { return weight(below) >= min_p || l == sc.top; };  // the first always stays
+  const auto ring_of = [&](float l, float e) { return fmaf(l - sc.top, sc.per, -__builtin_amdgcn_logf(e)); };
   Runner run;
+  int unit_cut = -1;  // not negative: run.at is the first of a unit of eight, and this the index of the cut
   // A list of all that is not below some logit, if the cut is certain to be there and it may be short enough; where min_p keeps less
   // than the other filters, of all that it keeps (a hundredth of an octave more, for the roundings).
   const bool cuts = f.k > 0 || f.p < 1.f, zoned = cuts && !(f.k > 0 && f.k <= 512) && !TOP_IS_INF;
@@ -618,7 +611,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
   } else {
     // Where many tokens are left their random numbers are fetched for every unit, one unit ahead; else where one of the wave's
     // is still in.
-    bool ahead = !(min_p > 0.f);
+    bool ahead = !(min_p > 0.f), known = false;
     if (cuts) {
       bool found = !TOP_IS_INF;
       unsigned long long inside = 0;
@@ -634,6 +627,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
         find_cut(row, sc.over_row(), f, 0, true, s);
       }
       ahead = found && zone.above >= (uint32_t)a.n / 64 && !(min_p > 0.f);
+      known = ahead && noise;
     }
     __syncthreads();
     const float cut = s.cut;
@@ -647,34 +641,58 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
       else if (first < a.n) load_unit(noise + first, a.n - first, next);
     };
     if (ahead) fetch(t * kUnit);
-    row.each_unit([&](const RawUnit<T>& u, int first) {
-      float e[kUnit];
-#pragma unroll
-      for (int j = 0; j < kUnit; ++j) e[j] = ahead ? next[j] : 1.f;
-      if (ahead) fetch(first + kSampleThreads * kUnit);
-      uint32_t in = 0;
-      if (greedy) {
-#pragma unroll
-        for (int j = 0; j < kUnit; ++j) in |= row.logit(u.at(j)) == sc.top ? 1u << j : 0u;
-      } else {
+    // a token is in if it is not below `least`, from the one behind the cut on not below `behind`
+    const float least = greedy ? sc.top : fmaxf(cut, -3.402823466e38f);
+    const float behind = greedy ? sc.top : cut > -kInf ? next_above(cut) : least;
+    if (known) {
+      // Many tokens, and their mass is known: a unit's furthest runner only, the token is looked up at the end.
+      row.each_unit([&](const RawUnit<T>& u, int first) {
+        float ring[kUnit], most = -kInf;
+        const int upto = cut_index - first;
+        const float lowest = upto >= kUnit - 1 ? least : behind;
 #pragma unroll
         for (int j = 0; j < kUnit; ++j) {
           const float l = row.logit(u.at(j));
-          in |= l > cut || (l == cut && first + j <= cut_index && l > -kInf) ? 1u << j : 0u;
+          ring[j] = l >= lowest ? ring_of(l, next[j]) : -kInf;
         }
-        if (min_p > 0.f)
+        if (upto >= 0 && upto < kUnit - 1) {  // the cut's own unit
 #pragma unroll
           for (int j = 0; j < kUnit; ++j) {
             const float l = row.logit(u.at(j));
-            in &= in_share(l, sc.below(l)) ? ~0u : ~(1u << j);
+            ring[j] = l >= (j <= upto ? least : behind) ? ring_of(l, next[j]) : -kInf;
           }
-      }
-      if (!__any(in != 0)) return;
-      if (!ahead && noise && in) load_unit(noise + first, a.n - first, e);
+        }
 #pragma unroll
-      for (int j = 0; j < kUnit; ++j)
-        run.enter<false>(in >> j & 1, sc.below(row.logit(u.at(j))), __builtin_amdgcn_logf(e[j]), first + j);
-    });
+        for (int j = 0; j < kUnit; ++j) most = fmaxf(most, ring[j]);
+        fetch(first + kSampleThreads * kUnit);
+        run.at = most > run.best ? first : run.at;
+        run.best = fmaxf(run.best, most);
+      });
+      if (t == 0) run.z = (float)s.kept_mass * 4.656612873077393e-10f;
+      unit_cut = cut_index;
+    } else {
+      row.each_unit([&](const RawUnit<T>& u, int first) {
+        float e[kUnit];
+#pragma unroll
+        for (int j = 0; j < kUnit; ++j) e[j] = ahead ? next[j] : 1.f;
+        if (ahead) fetch(first + kSampleThreads * kUnit);
+        float l[kUnit], most = -kInf;
+#pragma unroll
+        for (int j = 0; j < kUnit; ++j) {
+          l[j] = row.logit(u.at(j));
+          most = fmaxf(most, l[j]);
+        }
+        if (!__any(most >= least)) return;
+        if (!ahead && noise && most >= least) load_unit(noise + first, a.n - first, e);
+        const int upto = cut_index - first;
+#pragma unroll
+        for (int j = 0; j < kUnit; ++j) {
+          const float below = sc.below(l[j]), w = weight(below);
+          const bool in = l[j] >= (j <= upto ? least : behind) && (w >= min_p || l[j] == sc.top);
+          run.enter<false>(in, below, __builtin_amdgcn_logf(e[j]), first + j);
+        }
+      });
+    }
   }
   // the furthest runner; of equal ones the lowest index
   const float wave_z = wave_sum(run.z);
@@ -697,6 +715,14 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
   at = max(at, dpp_move_u32<0x141>(at));
   at = max(at, dpp_move_u32<0x140>(at));
   int token = (int)~at;
+  if (unit_cut >= 0 && best != 0 && t < 64) {  // which of the unit
+    bool here = false;
+    if (t < kUnit && token + t < a.n) {
+      const float l = row.logit(load_one(row.p + token + t));
+      here = (l > s.cut || (l == s.cut && token + t <= unit_cut)) && ordered_key(ring_of(l, noise[token + t])) == best;
+    }
+    token += __builtin_ctzll(__ballot(here) | 1ull << 63);
+  }
   if (best == 0) {  // no random number of the tokens that are left is one: the first token
     row.each([&](float l, int at) {
       if (l == sc.top) atomicMin(&s.cut_index, at);
