@@ -660,17 +660,17 @@ void tile_form(const MatmulArgs& g, TilePlan plan, hipStream_t st) {
 }
 
 // ---- which form ------------------------------------------------------------------------------------------------------------------
-// Up to 16 rows: the stream of B.  Else the form that a model of its time says is the fastest.  A tile's time is its half
-// blocks' times what an iteration takes, from measurements (k = 4096, us an iteration; few / all compute units at work):
-//   256 x 256  0.57 / 0.84 (power)   128 x 128  0.26 / 0.34   64 x 64  0.147 / 0.17 (rate of L2)   fp32: 128 x 128  0.30 / 0.44
-// A tile's start and end cost 1.6, 2.4 and 3.4 us; parts of k cost a second launch and the traffic of the parts; strips take 0.36, 0.38
-// or 0.62 us for a step of each of a compute unit's four waves, with up to 32, 48 and 64 rows (more rows: several parts of as many), and a
-// little more the longer the stream.
-// 512 x 4096 x 4096: 64-tiles 21.1, 128-tiles 20.3; 1024 x 11008 x 4096: 128-tiles 66.7, 256-tiles 55.4; 32 x 12288 x 4096: the stream of B 10.4,
-// 64-tiles 13.5; 64 x 12288 x 4096: 16.3 and 14.4; 48 x 4096 x 11008: 12.5 and 17.0; 512 x 12288 x 4096: 128-tiles (one or two to a
-// compute unit) 36.4, 256-tiles 42.6; 700 x 8192 x 8192: 70 and 78; 512 x 22016 x 4096: 67 and 58; 512 x 512 x 2048 (fp32): strips
-// 5.7, tiles 14.1; 128 x 4096 x 4096: 11.8 and 13.6; 1000 x 1000 x 256: 6.4 and 5.1.
-enum Form { kStrip, kTile64, kTile128, kTile256 };
+// Up to 16 rows: strips.  Else the form that a model of its time says is the fastest.  A tile's time is its half blocks' times what an
+// iteration takes, from measurements (k = 4096, us an iteration; few compute units at work / all / each of two or three workgroups on one):
+//   256 x 256  0.57 / 0.84 (power)   128 x 128  0.26 / 0.30 / 0.34   64 x 128  0.175 / 0.21 / 0.25   64 x 64  0.147 / 0.17 (rate of L2)
+//   fp32: 128 x 128  0.30 / 0.44 / 0.44   64 x 128  0.26 / 0.30 / 0.30
+// but no less than B takes from memory (5.2 TB/s).  A tile's start and end cost 1.6 to 3.4 us; parts of k cost a second launch and the traffic of the
+// parts; strips take 0.36, 0.38 or 0.62 us for a step of each of a compute unit's four waves, with up to 32, 48 and 64 rows (more rows:
+// several parts of as many), and a little more the longer the stream.
+// 512 x 4096 x 4096: 64 x 128 17.4, 128 x 128 20.2; 512 x 12288 x 4096: 43.5, 36.5, 256 x 256 42.6; 512 x 22016 x 4096: 256 x 256 58, 128 x 128 67;
+// 300 x 12288 x 4096 (fp32): 64 x 128 40.7, 128 x 128 48; 32 x 12288 x 4096: strips 10.4, 64 x 64 13.5; 64 x 12288 x 4096: 16.3 and 14.4;
+// 48 x 4096 x 11008: 12.5 and 17.0; 512 x 512 x 2048 (fp32): 5.7 and 14.1; 1000 x 1000 x 256: 6.4 and 5.1.
+enum Form { kStrip, kTile64, kTileWide, kTile128, kTile256 };  // wide: 64 x 128
 struct Choice {
   Form form;
   int splits, groups;  // parts of k, groups of four blocks each
@@ -694,22 +694,24 @@ Choice choose(int m, int n, int k, bool exact, size_t scratch) {
     least = 2.5 + fmax((double)n * k / 5.2e6, rounds * (steps * a_step[tiles16 - 1] * (1 + (tiles16 < 3 ? 0.02 : 0.05) * (rounds - 1)) + 0.25));
     best = {kStrip, 1, groups};
   }
-  const struct { Form form; int edge; double ends, few, all; } forms[] = {{kTile64, 64, 1.6, exact ? 0.23 : 0.147, exact ? 0.36 : 0.17},
-                                                                          {kTile128, 128, 2.4, exact ? 0.30 : 0.26, exact ? 0.44 : 0.34},
-                                                                          {kTile256, 256, 3.4, 0.57, 0.84}};
+  // few, all: an iteration with few workgroups and with one for each compute unit; more: for each, where `room` share a unit; pair: at least
+  const struct { Form form; int rows, columns, room; double ends, few, all, more, pair; } forms[] = {
+      {kTile64, 64, 64, 1, 1.6, exact ? 0.23 : 0.147, exact ? 0.36 : 0.17, 0, 0},
+      {kTileWide, 64, 128, 3, 2.0, exact ? 0.26 : 0.175, exact ? 0.30 : 0.21, exact ? 0.30 : 0.25, exact ? 0.50 : 0.40},
+      {kTile128, 128, 128, 2, 2.4, exact ? 0.30 : 0.26, exact ? 0.44 : 0.30, exact ? 0.44 : 0.34, exact ? 0.67 : 0.48},
+      {kTile256, 256, 256, 1, 3.4, 0.57, 0.84, 0, 0}};
   for (const auto& f : forms) {
     if (exact && f.form == kTile256) continue;  // (its converted operands do not fit the registers)
-    const double tiles = ceil(m / (double)f.edge) * ceil(n / (double)f.edge);
+    const double tiles = ceil(m / (double)f.rows) * ceil(n / (double)f.columns);
     for (int want = 1; want <= 8 && want <= groups; want *= 2) {
       const int per = (groups + want - 1) / want, splits = (groups + per - 1) / per;  // no empty parts
       const double parts = splits > 1 ? (double)splits * m * n * 4 : 0;
       if (parts > (double)scratch) break;
-      const double t = f.few + (f.all - f.few) * fmin(1.0, tiles * splits / kComputeUnits);
-      // (two 128-tiles share a compute unit, whose other half may have nothing to do)
-      const double units = tiles * splits / kComputeUnits;
-      const bool together = f.form == kTile128 && units <= 2;
-      const double rounds = together ? fmax(1.0, units) : ceil(units);
-      const double us = 2.5 + (together ? 1 : rounds) * f.ends + rounds * 2 * kGroup * per * t + (splits > 1 ? 3.5 + 2 * parts / 4e6 : 0);
+      const double units = tiles * splits / kComputeUnits, iterations = 2 * kGroup * (double)per;
+      double us = units <= 1        ? f.ends + iterations * (f.few + (f.all - f.few) * units)
+                  : units <= f.room ? f.ends + iterations * fmax(f.pair, f.more * units)
+                                    : ceil(units) * (f.ends + iterations * fmax(f.all, f.more));
+      us = 2.5 + fmax(us, (double)n * k / 5.2e6) + (splits > 1 ? 3.5 + 2 * parts / 4e6 : 0);
       if (us < least) {
         least = us;
         best = {f.form, splits, per};
@@ -744,6 +746,7 @@ void matmul(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStr
     if (c.form == kTile256) return tile_form<T, 256, 256, 2, 4, 4>(g, plan, st);
   }
   if (c.form == kTile64) return tile_form<T, 64, 64, 2, 2, 4>(g, plan, st);
+  if (c.form == kTileWide) return tile_form<T, 64, 128, 2, 2, 4>(g, plan, st);
   tile_form<T, 128, 128, 2, 2, 4>(g, plan, st);
 }
 
