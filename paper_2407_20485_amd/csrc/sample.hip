@@ -546,9 +546,9 @@ struct Runner {
   float z = 0.f, best = -kInf;
   int at = -1;
   template <bool ANY_ORDER>
-  __device__ __forceinline__ void enter(bool in, float below, float log_noise, int index) {
+  __device__ __forceinline__ void enter(bool in, float below, float w, float log_noise, int index) {
     const float ring = in ? -below - log_noise : -kInf;  // (base 2; not a number: never taken)
-    z += in ? weight(below) : 0.f;
+    z += in ? w : 0.f;
     const bool ahead = ring > best || (ANY_ORDER && ring == best && index < at);
     best = ahead ? ring : best;
     at = ahead ? index : at;
@@ -564,6 +564,12 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
   sc.first = sc.bins_per = 0.f;
   sc.top = TOP_IS_INF ? 0.f : top;
   sc.per = greedy ? 1.f : fminf(1.44269504088896340736f / temperature, 1e30f);  // (0 times it stays 0)
+  // A weight to the last bits: with what the roundings of log2(e) / temperature and of the product have cut off.
+  const float per_rest = !greedy && sc.per > 1e-30f && sc.per < 1e30f ? (fmaf(-sc.per, temperature, 1.44269504f) + 1.92596299e-8f) * (0.69314718f * sc.per) : 0.f;
+  const auto exact_weight = [&](float l) {
+    const float d = sc.top - l, below = d * sc.per, w = weight(below);
+    return below < 150.f ? fmaf(w, -0.69314718f * fmaf(d, per_rest, fmaf(d, sc.per, -below)), w) : w;
+  };
   const float* noise = a.noise && !greedy ? a.noise + r * a.noise_stride : nullptr;
   const float min_p = f.min_p;
   const auto in_share = [&](float l, float below) { return weight(below) >= min_p || l == sc.top; };  // the first always stays
@@ -606,7 +612,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
     list.each([&](float l, int at) {
       const float below = sc.below(l);
       const bool in = (l > cut || (l == cut && at <= cut_index)) && below < kInf && in_share(l, below);
-      if (in) run.enter<true>(true, below, noise ? __builtin_amdgcn_logf(noise[at]) : 0.f, at);
+      if (in) run.enter<true>(true, below, exact_weight(l), noise ? __builtin_amdgcn_logf(noise[at]) : 0.f, at);
     });
   } else {
     // Where many tokens are left their random numbers are fetched for every unit, one unit ahead; else where one of the wave's
@@ -689,7 +695,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
         for (int j = 0; j < kUnit; ++j) {
           const float below = sc.below(l[j]), w = weight(below);
           const bool in = l[j] >= (j <= upto ? least : behind) && (w >= min_p || l[j] == sc.top);
-          run.enter<false>(in, below, __builtin_amdgcn_logf(e[j]), first + j);
+          run.enter<false>(in, below, w, __builtin_amdgcn_logf(e[j]), first + j);
         }
       });
     }
@@ -732,7 +738,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
   }
   if (t == 0) {
     a.token[r] = token;
-    if (a.prob) a.prob[r] = greedy ? 1.f : weight(sc.below(row.logit(load_one(row.p + token)))) / z;
+    if (a.prob) a.prob[r] = greedy ? 1.f : exact_weight(row.logit(load_one(row.p + token))) / z;
   }
 }
 
