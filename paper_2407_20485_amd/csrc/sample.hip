@@ -612,7 +612,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
     list.each([&](float l, int at) {
       const float below = sc.below(l);
       const bool in = (l > cut || (l == cut && at <= cut_index)) && below < kInf && in_share(l, below);
-      if (in) run.enter<true>(true, below, exact_weight(l), noise ? __builtin_amdgcn_logf(noise[at]) : 0.f, at);
+      if (in) run.enter<true>(true, below, weight(below), noise ? __builtin_amdgcn_logf(noise[at]) : 0.f, at);
     });
   } else {
     // Where many tokens are left their random numbers are fetched for every unit, one unit ahead; else where one of the wave's
