@@ -54,9 +54,10 @@ struct Chunk {
 // read its elements in one row.  A workgroup takes some tokens of one part (its strides are then scalar), a lane one item of
 // up to kHeads heads, with the item's cosines and sines: all of them are read before the first is written.  Items read and write
 // their own elements only, so a part may be turned in place.  Any stride and alignment; WHOLE: no item is shorter than 16 bytes.
-// 8 x 2048 tokens of 96 heads of 128 in bf16 (805 MB): halves 156 us = 5.2 TB/s, neighbours 150 = 5.4 (a copy of 1 GiB: 5.2).  With one item of all
+// 8 x 2048 tokens of 96 heads of 128 in bf16 (805 MB): halves 152 us = 5.3 TB/s, neighbours 147 = 5.5 (a copy of 1 GiB: 5.2).  With one item of all
 // parts' heads in turn per lane, whose strides are then looked up lane by lane, 165 and 181.
 // 16 tokens of 48 heads of 128: 3.3 us with a head to a lane, 4.6 with four.
+// A turned part of 100 of 128, halves: 213 us, neighbours 173 (345 and 332 with the last item element by element, as it still is in place).
 constexpr int kHeads = 4;
 
 template <typename T, bool NEIGHBOURS, bool WHOLE>
@@ -77,18 +78,18 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   if (!(turns && P.rotate) && P.in_place) return;
   // the item's elements: `have` from e0 on, with halves as many from e1 on
   int e0, e1 = 0, have;
-  if (!turns) {
-    e0 = a.rot + (item - a.turning) * W;
-    have = a.d - e0;
-  } else if (NEIGHBOURS) {
-    e0 = item * W;
-    have = a.rot - e0;
-  } else {
-    e0 = item * W;
-    e1 = half + e0;
-    have = half - e0;
+  const int from = turns ? 0 : a.rot, upto = !turns ? a.d : NEIGHBOURS ? a.rot : half;
+  e0 = from + (turns ? item : item - a.turning) * W;
+  have = upto - e0;
+  if (WHOLE) {
+    have = W;
+  } else if (have < W && upto - from >= W && !P.in_place) {
+    // the last item moves back over elements of the one before it, which both then write the same (not in place, where it might read
+    // what the other has written)
+    e0 = upto - W;
+    have = W;
   }
-  if (WHOLE) have = W;
+  if (turns && !NEIGHBOURS) e1 = half + e0;
   const bool two = !NEIGHBOURS && turns;
   const T* x = (const T*)P.x + b * P.x_stride[0] + i * P.x_stride[1];
   T* y = (T*)P.y + b * P.y_stride[0] + i * P.y_stride[1];
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   if (turns && P.rotate) {
     const int32_t p = a.pos[b * a.pos_stride + i];
     known = p >= 0 && p < a.table_rows;
-    const int first = item * kTable;
+    const int first = NEIGHBOURS ? e0 / 2 : e0;
     const float* row = a.table + (long long)(known ? p : 0) * a.rot + first;
 #pragma unroll
     for (int j = 0; j < kTable; ++j) {

@@ -409,6 +409,22 @@ def test_rotary_splits_a_product(batch, length, heads, kv, d, rot, neighbours, d
         assert torch.equal(p, o.transpose(1, 2))
 
 
+@pytest.mark.parametrize("rot", [2, 6, 14, 16, 18, 26, 38, 60, 100, 112, 118, 122, 126])
+@pytest.mark.parametrize("neighbours", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rotary_parts_of_any_size(rot, neighbours, dtype):
+    """Against the oracle; and in place, where items keep to their own elements, the same bits."""
+    test_rotary_splits_a_product(2, 5, 6, 3, 128, rot, neighbours, dtype)
+    g = rng(20, rot)
+    x = on_gpu(g.normal(size=(60, 128)), DT[dtype]).view(3, 4, 5, 128)
+    y, table = torch.empty_like(x), torch.empty(90, rot, device="cuda")
+    B.a2sf_rotary_table(table)
+    pos = torch.from_numpy(g.integers(0, 90, size=(3, 4)).astype(np.int32)).cuda()
+    B.a2sf_rotary([(x, y)], pos, table, interleaved=neighbours)
+    B.a2sf_rotary([(x, x)], pos, table, interleaved=neighbours)
+    assert torch.equal(x, y)
+
+
 def test_rotary_there_and_back():
     x = torch.randn(2, 50, 3, 128, device="cuda")
     pos = torch.arange(100, dtype=torch.int32, device="cuda").view(2, 50) * 1000
