@@ -481,6 +481,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void matmul_tile_kernel(MatmulArgs 
   fetch_scales(next, next.g0);
 #pragma unroll
   for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+  wait_lds();  // (a first half block that k ends in went through registers: written before the barrier that its readers wait at)
   if constexpr (kApart) {
     if (second) {
       landed();

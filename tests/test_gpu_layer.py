@@ -315,6 +315,22 @@ def test_matmul_of_several_parts_of_rows_is_exact(m, n, k):
     test_matmul_of_whole_numbers_is_exact(m, n, k, "f32", True)
 
 
+# (m, n) whose tiles are of 64 x 64, 64 x 128, 128 x 128 and 256 x 256 (fp32: 128 x 128) where k is that short
+@pytest.mark.parametrize("m,n", [(1100, 128), (1100, 1000), (64, 32000), (2000, 2000), (4096, 4096)])
+@pytest.mark.parametrize("k", [1, 15, 16, 32, 48, 63, 65, 127])
+def test_matmul_of_less_than_a_block_of_k_is_exact(m, n, k):
+    """The first half block is the last one, and its end is filled with zeros (several tiles to a workgroup too)."""
+    g = rng(21, m, n, k)
+    (a, sa), (b, sb) = operands(g, m, n, k, True)
+    ta, tsa = filled(m, k, a, sa, 0)
+    tb, tsb = filled(n, k, b, sb, 16)
+    want = torch.from_numpy(L.values(a, sa)).cuda() @ torch.from_numpy(L.values(b, sb, 128)).cuda().t()
+    for dtype in (torch.bfloat16, torch.float32):
+        c = torch.full((m, n), 99.0, dtype=dtype, device="cuda")
+        B.a2sf_matmul_scaled(ta, tsa, tb, tsb, c)
+        assert torch.equal(c, want.to(dtype)), (c.double() - want).abs().max()
+
+
 @pytest.mark.parametrize("m,n,k", [(1, 300, 1000), (7, 777, 4096), (40, 200, 333), (150, 700, 2000), (300, 300, 8000), (1030, 600, 500)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_matmul(m, n, k, dtype):

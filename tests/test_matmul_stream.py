@@ -62,3 +62,13 @@ def test_strips(assembly):
         per_step = 4 + 2 * int(re.search(r"Li(\d+)E", name)[1])
         ahead = [int(n) for ln in lines for n in re.findall(r"s_waitcnt vmcnt\((\d+)\)$", ln)]
         assert any(n > 0 and n % per_step == 0 for n in ahead), (name, ahead)
+
+
+def test_first_stages_are_written_before_the_first_barrier(kernels):
+    """A half block that k ends in is written to LDS by way of registers, also when it is the first (k < 64): those writes have
+    arrived before the barrier behind which other waves read them."""
+    for name, lines in kernels.items():
+        barrier = lines.index("s_barrier")
+        writes = [i for i, ln in enumerate(lines[:barrier]) if ln.startswith("ds_write")]
+        assert writes, name
+        assert any(ln.startswith("s_waitcnt") and "lgkmcnt(0)" in ln for ln in lines[writes[-1]: barrier]), name
