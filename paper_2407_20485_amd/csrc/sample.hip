@@ -589,7 +589,8 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
     listed = zone.bin >= 0 && zone.above + zone.in <= kSampleWaves * kListed;
   }
   if (!TOP_IS_INF && min_p > 0.f && (zoned ? f.k == 0 || !(f.p < 1.f) : !cuts)) {
-    const float share = fminf(sc.top, sc.top - (0.01f - __builtin_amdgcn_logf(min_p)) / sc.per);
+    // (no -infinity here either, where the distance is infinite: it would list what stands for logits behind the end of the row)
+    const float share = fmaxf(fminf(sc.top, sc.top - (0.01f - __builtin_amdgcn_logf(min_p)) / sc.per), -3.402823466e38f);
     if (!cuts || (zone.bin > 1 && share > sc.top - (float)(zone.bin - 1) / (kBinsPerOctave * sc.per))) {
       least = share;
       listed = true;

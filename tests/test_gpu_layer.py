@@ -598,6 +598,20 @@ def test_sample_infinities_and_nan():
     check_tokens(logits, None, top_k=[2] * 6)
 
 
+@pytest.mark.parametrize("n", [1, 5, 100, 511, 1000, 5003])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sample_min_p_that_keeps_every_token(n, dtype):
+    """Shares and temperatures that put the last logit kept at -infinity: what is kept ends with the row all the same, also where the
+    next row's logits are larger."""
+    g = rng(22, n)
+    l = g.normal(size=(6, n)) + 3 * np.arange(6)[:, None]
+    l[:, n // 2:][g.random((6, n - n // 2)) < 0.2] = -math.inf
+    l[:, 0] = 0.0
+    logits, noise = on_gpu(l, DT[dtype]), on_gpu(g.exponential(size=(6, n)) + 1e-9, torch.float32)
+    check_tokens(logits, noise, min_p=[1e-40, 1e-38, 1e-30, 1e-45, 1e-20, 1e-40])
+    check_tokens(logits, noise, min_p=[1e-40, 0.5, 1e-30, 0.1, 1e-6, 1.0], temperature=[1e38, math.inf, 1e38, 3e38, math.inf, math.inf])
+
+
 def test_sample_without_prob_and_with_numbers_that_are_zero():
     logits = torch.zeros(1, 10, device="cuda")
     noise = torch.ones(1, 10, device="cuda")
