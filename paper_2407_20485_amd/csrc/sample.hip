@@ -214,7 +214,7 @@ struct Scale {
   float top, per;         // largest logit; octaves per unit of logit (log2(e) / temperature)
   float first, bins_per;  // the bins: from this logit down, so many per unit of logit
   __device__ __forceinline__ float below(float l) const { return (top - l) * per; }
-  // (of -infinity: the last; of NaN: some)
+  // (of finite numbers)
   __device__ __forceinline__ int bin(float l) const {
     return (int)fminf(fmaxf((first - l) * bins_per, 0.f), (float)(kBins - 1));
   }
@@ -315,12 +315,13 @@ __device__ __forceinline__ void fill_bins(const R& row, const Scale& sc, SampleS
   uint32_t far_count = 0;
   unsigned long long far_mass = 0;
   row.each([&](float l, int) {
+    if (!(l > -kInf)) return;  // (a NaN, or -infinity at a temperature of infinity, would have some bin)
     const int bin = sc.bin(l);
     const uint32_t m = mass_of(sc.below(l));
     if (bin < kBins - 1) {
       atomicAdd(&s.count[bin], 1u);
       atomicAdd(&s.mass[bin], (unsigned long long)m);
-    } else if (l > -kInf) {
+    } else {
       ++far_count;
       far_mass += m;
     }

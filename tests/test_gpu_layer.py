@@ -612,6 +612,31 @@ def test_sample_min_p_that_keeps_every_token(n, dtype):
     check_tokens(logits, noise, min_p=[1e-40, 0.5, 1e-30, 0.1, 1e-6, 1.0], temperature=[1e38, math.inf, 1e38, 3e38, math.inf, math.inf])
 
 
+@pytest.mark.parametrize("live,nans", [(1000, 1000), (600, 1400), (599, 50), (800, 3000), (2000, 2000), (30, 5000)])
+@pytest.mark.parametrize("values", ["different", "few", "one and ties", "close"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sample_long_rows_with_nan(live, nans, values, dtype):
+    """NaN and -infinity among the logits count for nothing, whatever way the cut is found: k below and above the number of finite
+    ones, and below and above that of all but the -infinities."""
+    g = rng(23, live, nans, len(values))
+    n = live + nans + 500
+    l = np.full((7, n), -math.inf)
+    for r in range(7):
+        at = g.permutation(n)
+        l[r, at[:live]] = {"different": g.normal(size=live) * 3, "few": np.round(g.normal(size=live)), "close": 1 + 1e-3 * g.random(live),
+                           "one and ties": np.where(np.arange(live) < 10, 5 + 0.1 * np.arange(live), 1.0)}[values]
+        l[r, at[live: live + nans]] = math.nan
+    logits = on_gpu(l, DT[dtype])
+    noise = on_gpu(g.exponential(size=(7, n)) + 1e-9, torch.float32)
+    k = [513, min(live + 1, n - 1), live + nans // 2, live + nans, n - 1, 100, max(1, live - 1)]
+    check_tokens(logits, noise, top_k=k)
+    check_tokens(logits, None, top_k=k)
+    check_tokens(logits, noise, top_k=k, top_p=[0.5, 0.9, 0.99, 0.999, 0.3, 0.9, 0.7])
+    check_tokens(logits, noise, top_p=[0.5, 0.9, 0.99, 0.999, 0.3, 0.9, 0.7], min_p=[0.0, 0.1, 0.0, 0.5, 0.0, 0.0, 0.01])
+    check_tokens(logits, noise, top_k=k, temperature=[math.inf, 1e30, 100.0, 0.01, 1e-30, math.inf, 1.0])
+    check_tokens(logits, noise, min_p=[0.5, 1e-40, 0.01, 0.1, 1.0, 1e-9, 0.3], temperature=[math.inf, 1.0, 100.0, 0.01, 1e-30, math.inf, 1.0])
+
+
 def test_sample_without_prob_and_with_numbers_that_are_zero():
     logits = torch.zeros(1, 10, device="cuda")
     noise = torch.ones(1, 10, device="cuda")
