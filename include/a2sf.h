@@ -326,7 +326,8 @@ a2sf_status a2sf_decode_plan(int32_t G, int32_t capacity, int32_t d, int32_t* ns
  *    16 bytes.
  *  - Where an input and an output are the same rows, every element is read before it is written.  Other overlaps are
  *    not allowed.
- *  - Sums, norms and products are formed in 32 bits or more whatever the type; results are rounded once. */
+ *  - Sums, norms and products are formed in 32 bits or more whatever the type (a2sf_matmul_scaled: where the caller does not leave that
+ *    to the 8-bit matrix instruction); results are rounded once. */
 typedef struct {
   void* data;
   int64_t stride; /* elements from row to row */
@@ -371,9 +372,14 @@ a2sf_status a2sf_quantize_weight(const a2sf_rows* w, int32_t n, int32_t k, int32
  *   a          [m, k] as a2sf_rms_norm and a2sf_quantize write them.
  *   b          [n, k] as a2sf_quantize_weight writes them.
  *   c          out [m, n], c_dtype (A2SF_F32 or A2SF_BF16).
+ *   c_dtype    A2SF_F32, and A2SF_BF16 | A2SF_WIDE_SUMS: sums in 32 bits (within k * 2^-24 * sum |a b|).  A2SF_BF16 alone: by the 8-bit matrix
+ *              instruction, at about twice the rate where the rate counts; it cuts each of eight neighbouring products of k under 2^-13
+ *              of the largest of them, so a sum is within 8 * 2^-13 * sum |a b| of the exact one before it is rounded to bf16 (for data
+ *              like a model's 1.5e-5 of the result's size; a sum that cancels may lose all of it).
  *   workspace  may be NULL; with a2sf_matmul_workspace_bytes(m, n, k) bytes (0: none is of use) products that have too few
  *              tiles for the whole chip split their sums over k.  The same sizes with the same choice give the same bits.
  * Bytes of the rows past k are not used.  k <= 2^20, rows of a and b and rows of scales at most 2^23 bytes apart. */
+#define A2SF_WIDE_SUMS 0x100 /* or'ed to c_dtype */
 size_t a2sf_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
 a2sf_status a2sf_matmul_scaled(const a2sf_rows8* a, const a2sf_rows8* b, int32_t m, int32_t n, int32_t k,
                                const a2sf_rows* c, int32_t c_dtype, void* workspace, size_t workspace_bytes,

@@ -25,6 +25,7 @@ A2SF_EVICT_FAST, A2SF_EVICT_STABLE = 0, 1
 A2SF_MAX_CAPACITY = 36864
 A2SF_STATIC_WS_BYTES = 16 << 20
 A2SF_MAX_ROW, A2SF_MAX_VOCABULARY, A2SF_MAX_ROTARY_PARTS = 65536, 4194304, 4
+A2SF_WIDE_SUMS = 0x100
 
 EXPORTS = ("a2sf_workspace_bytes", "a2sf_prefill", "a2sf_decode_step", "a2sf_select",
            "a2sf_compact", "a2sf_status_string", "a2sf_prefill_alpha_per_head",
@@ -485,9 +486,10 @@ def a2sf_matmul_workspace_bytes(m, n, k) -> int:
     return int(lib().a2sf_matmul_workspace_bytes(m, n, k))
 
 
-def a2sf_matmul_scaled(a, a_scales, b, b_scales, c, workspace=None, workspace_bytes=None, stream=None):
+def a2sf_matmul_scaled(a, a_scales, b, b_scales, c, workspace=None, workspace_bytes=None, stream=None, wide_sums=False):
+    """wide_sums: a bfloat16 c too is summed in 32 bits (A2SF_WIDE_SUMS)."""
     at = _entry("a2sf_matmul_scaled")
-    status = _call.matmul_scaled(at, a, a_scales, b, b_scales, c, workspace, workspace_bytes, stream)
+    status = _call.matmul_scaled(at, a, a_scales, b, b_scales, c, workspace, workspace_bytes, stream, wide_sums)
     if status >= 0:
         return _check(status)
     _need(a.dim() == 2 and b.dim() == 2 and c.dim() == 2)
@@ -497,7 +499,8 @@ def a2sf_matmul_scaled(a, a_scales, b, b_scales, c, workspace=None, workspace_by
     if workspace_bytes is None:
         workspace_bytes = workspace.nbytes if workspace is not None else 0
     _check(lib().a2sf_matmul_scaled(_rows8(a, a_scales, m, k), _rows8(b, b_scales, n, k, -(-n // 128)), m, n, k, _rows(c, c),
-                                    dtype_code(c.dtype), _ptr(workspace), workspace_bytes, _stream(stream)))
+                                    dtype_code(c.dtype) | (A2SF_WIDE_SUMS if wide_sums else 0), _ptr(workspace), workspace_bytes,
+                                    _stream(stream)))
 
 
 def a2sf_rotary(parts, pos, table, interleaved=False, inverse=False, stream=None):

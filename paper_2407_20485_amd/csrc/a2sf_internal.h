@@ -168,7 +168,8 @@ struct MatmulArgs {
   int m, n, k;
 };
 size_t matmul_workspace(int m, int n, int k);
-void launch_matmul(const MatmulArgs& a, int dtype, void* workspace, size_t workspace_bytes, hipStream_t st);
+// wide_sums: a bf16 C too is summed in 32 bits
+void launch_matmul(const MatmulArgs& a, int dtype, bool wide_sums, void* workspace, size_t workspace_bytes, hipStream_t st);
 
 // rotary.hip
 struct RotaryPart {

@@ -140,6 +140,8 @@ size_t a2sf_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k) {
 a2sf_status a2sf_matmul_scaled(const a2sf_rows8* a, const a2sf_rows8* b, int32_t m, int32_t n, int32_t k,
                                const a2sf_rows* c, int32_t c_dtype, void* workspace, size_t workspace_bytes,
                                void* hip_stream) {
+  const bool wide_sums = (c_dtype & A2SF_WIDE_SUMS) != 0;
+  c_dtype &= ~A2SF_WIDE_SUMS;
   A2SF_TRY(check_sizes(m, n, c_dtype));
   if (k < 1 || k > (1 << 20) || m > 0x7FFFFFFF - 256 || n > 0x7FFFFFFF - 256) return A2SF_ESHAPE;
   // tiles are counted in 32 bits, and a tile's 256 rows are addressed by 32-bit offsets
@@ -166,7 +168,7 @@ a2sf_status a2sf_matmul_scaled(const a2sf_rows8* a, const a2sf_rows8* b, int32_t
   g.m = m;
   g.n = n;
   g.k = k;
-  return launched([&] { launch_matmul(g, c_dtype, workspace, workspace ? workspace_bytes : 0, (hipStream_t)hip_stream); });
+  return launched([&] { launch_matmul(g, c_dtype, wide_sums, workspace, workspace ? workspace_bytes : 0, (hipStream_t)hip_stream); });
 }
 
 a2sf_status a2sf_rotary(const a2sf_rotary_part* parts, int32_t n_parts, int32_t batch, int32_t length, int32_t d,

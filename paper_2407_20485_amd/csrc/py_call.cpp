@@ -276,9 +276,9 @@ PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (entry point, a, a_scales, b, b_scales, c, workspace, workspace_bytes, stream)
+// (entry point, a, a_scales, b, b_scales, c, workspace, workspace_bytes, stream[, wide_sums])
 PyObject* matmul_scaled(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!expects(n, 9)) return nullptr;
+  if (n != 10 && !expects(n, 9)) return nullptr;
   return guarded([&] {
     void *ws, *st, *fn = PyLong_AsVoidPtr(a[0]);
     const at::Tensor *c, *b;
@@ -293,8 +293,9 @@ PyObject* matmul_scaled(PyObject*, PyObject* const* a, Py_ssize_t n) {
           tensor(a[3], &b) && ta->size(1) <= INT32_MAX &&
           rows8(a[1], a[2], c->size(0), c->size(0), ta->size(1), s8, &ra) &&
           rows8(a[3], a[4], c->size(1), c->size(1) / 128 + (c->size(1) % 128 != 0), ta->size(1), s8 + 1, &rb) &&
-          workspace(a[6], a[7], &ws, &bytes) && stream(a[8], a[1], &st)))
+          workspace(a[6], a[7], &ws, &bytes) && stream(a[8], a[1], &st) && (n == 9 || PyBool_Check(a[9]))))
       return -1;
+    if (n == 10 && a[9] == Py_True) dtype |= A2SF_WIDE_SUMS;
     return without_gil([&]() -> int {
       return ((decltype(&a2sf_matmul_scaled))fn)(ra, rb, (int32_t)c->size(0), (int32_t)c->size(1), (int32_t)ta->size(1), rc, dtype,
                                                  ws, bytes, st);

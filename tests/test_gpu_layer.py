@@ -351,6 +351,39 @@ def test_matmul(m, n, k, dtype):
     assert torch.equal(c, again)
 
 
+@pytest.mark.parametrize("m,n,k", [(1, 300, 1000), (7, 777, 4096), (20, 5003, 640), (40, 200, 333), (60, 4200, 513), (150, 700, 2000), (300, 300, 8000),
+                                   (700, 1500, 640), (1030, 600, 500), (2100, 2000, 384)])
+@pytest.mark.parametrize("workspace", [True, False])
+def test_matmul_with_wide_sums(m, n, k, workspace):
+    """A bf16 C whose sums are fp32's: the fp32 C, rounded once."""
+    g = rng(24, m, n, k)
+    (a, sa), (b, sb) = operands(g, m, n, k, False)
+    ta, tsa = filled(m, k, a, sa, 16)
+    tb, tsb = filled(n, k, b, sb, 0)
+    c = on_gpu(np.zeros((m, n)), torch.bfloat16, stride=n + 3, offset=1)
+    f = torch.empty(m, n, device="cuda")
+    ws = torch.empty(B.a2sf_matmul_workspace_bytes(m, n, k), dtype=torch.uint8, device="cuda") if workspace else None
+    B.a2sf_matmul_scaled(ta, tsa, tb, tsb, c, workspace=ws, wide_sums=True)
+    B.a2sf_matmul_scaled(ta, tsa, tb, tsb, f, workspace=ws)
+    assert torch.equal(c, f.bfloat16())
+    va, vb = torch.from_numpy(L.values(a, sa)).cuda(), torch.from_numpy(L.values(b, sb, 128)).cuda().t()
+    want = va @ vb
+    assert bool(((c.double() - want).abs() <= max(k, 16) * 2.0 ** -24 * (va.abs() @ vb.abs()) + BF16 * want.abs()).all())
+
+
+@pytest.mark.parametrize("m", [1, 17, 40, 64, 130, 700, 2100])
+def test_matmul_wide_sums_keep_what_cancels(m):
+    """Products of 2^8 and -2^8 with seven of 2^-6 beside each: 7 * 2^-5 is left, exactly."""
+    n, k = 1100, 512
+    a, b = np.zeros((m, k)), np.ones((n, k))
+    a[:, :8], a[:, 64:72] = 2.0 ** -6, 2.0 ** -6
+    a[:, 3], a[:, 68] = 256.0, -256.0
+    ones = lambda r: np.full((r, 4), 127, np.uint8)
+    c = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    B.a2sf_matmul_scaled(*filled(m, k, L.to_e4m3(a), ones(m), 0), *filled(n, k, L.to_e4m3(b), ones(9), 0), c, wide_sums=True)
+    assert bool((c == 14 * 2.0 ** -6).all())
+
+
 @pytest.mark.parametrize("m", [1, 20, 200, 600])
 def test_matmul_scales_that_are_no_numbers_reach_their_rows_only(m):
     g = rng(7, m)

@@ -1,5 +1,7 @@
 """Refusals of the operators around the attention: found on the host, before any launch."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -186,3 +188,12 @@ def test_extension_leaves_unusual_arguments_to_ctypes():
     assert B._call.matmul_scaled(B._entry("a2sf_matmul_scaled"), x, x, x, x, x, None, None, None) == -1
     with pytest.raises(TypeError):
         B._call.sample(x)
+
+
+def test_matmul_choice_of_sums_is_checked_with_the_type():
+    f = lambda dtype, k=200: B.lib().a2sf_matmul_scaled(rows8(), rows8(), 4, 200, k, rows(), dtype, None, 0, None)
+    assert f(9 | B.A2SF_WIDE_SUMS) == B.A2SF_EDTYPE
+    assert f(B.A2SF_BF16 | 0x200) == B.A2SF_EDTYPE
+    assert f(B.A2SF_BF16 | B.A2SF_WIDE_SUMS, k=0) == B.A2SF_ESHAPE
+    header = open(os.path.join(os.path.dirname(B.__file__), "..", "include", "a2sf.h")).read()
+    assert int(re.search(r"#define A2SF_WIDE_SUMS (0x[0-9a-f]+)", header)[1], 16) == B.A2SF_WIDE_SUMS
