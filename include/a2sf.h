@@ -358,7 +358,8 @@ a2sf_status a2sf_rms_norm(const a2sf_rows* x, const a2sf_rows* residual, const v
                           int32_t n, int32_t dtype, const a2sf_rows* total, const a2sf_rows* out,
                           const a2sf_rows8* out8, void* hip_stream);
 
-/* Rows to 8 bits: y = x, or with a gate y = gate / (1 + exp(-gate)) * x.
+/* Rows to 8 bits: y = x, or with a gate y = gate / (1 + exp(-gate)) * x (before its rounding within 12 * 2^-24 of its size; 0 for gates
+ * below -87, where exp(-gate) leaves the range of 32 bits).
  *   x, gate    [rows, n] dtype; gate may be NULL.
  *   out, out8  out: y in dtype, y in 8 bits; either may be NULL, not both. */
 a2sf_status a2sf_quantize(const a2sf_rows* x, const a2sf_rows* gate, int32_t rows, int32_t n, int32_t dtype,

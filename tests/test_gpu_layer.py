@@ -227,6 +227,26 @@ def test_gate_far_from_zero():
     assert np.allclose(host(out), L.gated(np.ones((1, 8)), host(g)), rtol=1e-5, atol=1e-30)
 
 
+def test_gate_is_good_to_a_few_units_wherever_it_is():
+    """fp32: exp 2 u and its correction u, that twice (above and below the line), the sum u, the reciprocal 2 u, three products: 12 u."""
+    g = rng(25)
+    gate = on_gpu(np.concatenate([np.linspace(-86, 88, 30000), g.normal(size=30000) * 8])[None].clip(-86, 88), torch.float32)
+    x, out = on_gpu(g.normal(size=gate.shape), torch.float32), torch.empty_like(gate)
+    B.a2sf_quantize(x, None, None, gate=gate, out=out)
+    y = L.gated(host(x), host(gate))
+    assert (np.abs(host(out) - y) / np.abs(y).clip(1e-300)).max() <= 12 * 2.0 ** -24
+
+
+def test_gate_of_what_is_not_finite():
+    inf, nan = math.inf, math.nan
+    gate = torch.tensor([[inf, -inf, nan, inf, 3e38, -3e38, 1.0, 1.0, 0.0]], device="cuda")
+    x = torch.tensor([[1.0, 1.0, 1.0, -2.0, 0.5, 1.0, inf, nan, inf]], device="cuda")
+    out = torch.empty_like(x)
+    B.a2sf_quantize(x, None, None, gate=gate, out=out)
+    want = torch.tensor([[inf, nan, nan, -inf, 1.5e38, -0.0, inf, nan, nan]], device="cuda")
+    assert torch.allclose(out, want, rtol=1e-6, equal_nan=True)
+
+
 @pytest.mark.parametrize("n,k", [(1, 1), (128, 128), (129, 127), (300, 513), (77, 4100)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_quantize_weight_is_exact(n, k, dtype):
