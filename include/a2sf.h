@@ -429,7 +429,8 @@ a2sf_status a2sf_rotary_table(float* table, int32_t table_rows, int32_t rotary_d
  *   noise        [rows, n] fp32, positive; NULL: the first token is taken.
  *   temperature  [rows] fp32, may be NULL (1); <= 0: the first token, whatever the filters.
  *   top_k        [rows] int32, may be NULL; <= 0 or >= n: all.
- *   top_p        [rows] fp32, may be NULL; >= 1: all.
+ *   top_p        [rows] fp32, may be NULL; >= 1: all.  Its sums are of whole numbers of 2^-41 of the first token's probability (for probabilities
+ *                above 2^-10 of it: 2^-31), in 64 bits.
  *   min_p        [rows] fp32, may be NULL; <= 0: all.
  *   token        out [rows] int32.
  *   prob         out [rows] fp32, may be NULL: the token's probability among those that were left.

@@ -15,12 +15,13 @@
 // overflows or misses the cut (rows of few different values) is replaced by the row itself, whose bins are split until one
 // can be ranked, or holds one value only.
 //
-// Masses are whole numbers of 2^-31 of the largest token's weight, summed in 64 bits: their sums do not depend on the order in which
-// the lanes add, so the same inputs give the same cut, whichever way it was found.
+// Masses are whole numbers of 2^-41 of the largest token's weight, summed in 64 bits (2^22 tokens at most): their sums do not depend on the order
+// in which the lanes add, so the same inputs give the same cut, whichever way it was found.  A mass has 21 bits or all of its weight's, down to
+// weights of 2^-31, and what all tokens below 2^-42 lose is under 2^-20 of the largest one's.
 //
 // A workgroup of 1024 lanes takes a row.  Few rows are a chain of passes and barriers whose instructions are mostly fetched for the first
 // time: what counts is little code, so passes are loops that read the row again (from the caches) instead of unrolled ones over
-// registers (32 000 logits in fp32, all filters: 13.4 us, 24 with the row in registers; 256 rows of 50 272 in bf16, top-p and min-p: 21.5 us, 43 with
+// registers (32 000 logits in fp32, all filters: 13.4 us, 24 with the row in registers; 256 rows of 50 272 in bf16, top-p and min-p: 23.3 us, 43 with
 // a second pass for exact masses and a race over the whole row), and one function serves counts and masses.
 #include "a2sf_internal.h"
 #include "rows_dev.h"
@@ -43,7 +44,7 @@ struct SampleShared {
   int list_index[kSampleWaves][kListed];
   float rank[kRanked];
   int rank_index[kRanked];
-  uint32_t rank_mass[kRanked];
+  unsigned long long rank_mass[kRanked];
   unsigned long long wave64[kSampleWaves], wave64b[kSampleWaves];
   uint32_t wave32[kSampleWaves], wave32b[kSampleWaves];
   float wavef[kSampleWaves], wavef2[kSampleWaves];
@@ -233,7 +234,13 @@ __device__ __forceinline__ float next_above(float l) {
   return bits << 1 == 0 ? __int_as_float(1) : __int_as_float(bits + (bits < 0 ? -1 : 1));
 }
 __device__ __forceinline__ float weight(float below) { return __builtin_amdgcn_exp2f(-below); }
-__device__ __forceinline__ uint32_t mass_of(float below) { return (uint32_t)fmaf(weight(below), 2147483648.f, 0.5f); }
+// Its mass: of the ten octaves below the largest a whole number of 2^-31, under them one of 2^-41; 32 bits either way
+__device__ __forceinline__ unsigned long long mass_of(float below) {
+  const bool near = below < 10.f;
+  const uint32_t m = (uint32_t)fmaf(weight(below), near ? 0x1p31f : 0x1p41f, 0.5f);
+  return near ? (unsigned long long)m << 10 : m;
+}
+constexpr float kMassUnit = 0x1p-41f;
 
 // What is looked for: the token at which the count (by_mass: the mass) reaches a number
 struct Target {
@@ -317,10 +324,10 @@ __device__ __forceinline__ void fill_bins(const R& row, const Scale& sc, SampleS
   row.each([&](float l, int) {
     if (!(l > -kInf)) return;  // (a NaN, or -infinity at a temperature of infinity, would have some bin)
     const int bin = sc.bin(l);
-    const uint32_t m = mass_of(sc.below(l));
+    const unsigned long long m = mass_of(sc.below(l));
     if (bin < kBins - 1) {
       atomicAdd(&s.count[bin], 1u);
-      atomicAdd(&s.mass[bin], (unsigned long long)m);
+      atomicAdd(&s.mass[bin], m);
     } else {
       ++far_count;
       far_mass += m;
@@ -368,7 +375,7 @@ __device__ __forceinline__ bool cut_in_bin(const R& row, const Scale& sc, Sample
         const uint32_t key = ordered_key(l);
         if (l > -kInf && key >= low && key <= high) {
           atomicAdd(&s.count[(high - key) >> shift], 1u);
-          atomicAdd(&s.mass[(high - key) >> shift], (unsigned long long)mass_of(sc.below(l)));
+          atomicAdd(&s.mass[(high - key) >> shift], mass_of(sc.below(l)));
         }
       });
       scan_bins(s, to, before_count, before_mass);
@@ -382,7 +389,7 @@ __device__ __forceinline__ bool cut_in_bin(const R& row, const Scale& sc, Sample
     if (members > kRanked) {
       // all of one value: the cut is the r-th of them by index, found by halving the range of indices
       const float value = __uint_as_float((high & 0x80000000u) ? high ^ 0x80000000u : ~high);
-      const uint32_t each = mass_of(sc.below(value));
+      const unsigned long long each = mass_of(sc.below(value));
       uint32_t r = to.tokens - before_count;
       if (to.by_mass) r = each ? (uint32_t)((to.mass - before_mass + each - 1) / each) : members;
       int first = 0, last = row.n - 1;
@@ -397,7 +404,7 @@ __device__ __forceinline__ bool cut_in_bin(const R& row, const Scale& sc, Sample
       if (t == 0) {
         s.cut = value;
         s.cut_index = first;
-        s.kept_mass = before_mass + (unsigned long long)r * each;
+        s.kept_mass = before_mass + r * each;
       }
       __syncthreads();
       return split;
@@ -430,7 +437,7 @@ __device__ __forceinline__ bool cut_in_bin(const R& row, const Scale& sc, Sample
       const float o = s.rank[j];
       const bool ahead = o > l || (o == l && s.rank_index[j] < at);
       c += ahead;
-      m += ahead ? s.rank_mass[j] : 0u;
+      m += ahead ? s.rank_mass[j] : 0ull;
     }
   }
   for (int by = 1; by < share; by *= 2) {
@@ -441,7 +448,7 @@ __device__ __forceinline__ bool cut_in_bin(const R& row, const Scale& sc, Sample
   if (mine < (int)members && (t & (share - 1)) == 0) {
     c += before_count;
     m += before_mass;
-    const uint32_t own = s.rank_mass[mine];
+    const unsigned long long own = s.rank_mass[mine];
     if (to.by_mass ? (m < to.mass && m + own >= to.mass) : c + 1 == to.tokens) {
       s.cut = s.rank[mine];
       s.cut_index = s.rank_index[mine];
@@ -493,17 +500,23 @@ template <typename R>
 __device__ __forceinline__ Zone find_zone(const R& row, const Scale& sc, const Filters& f, bool by_mass, unsigned long long inside,
                                           SampleShared& s) {
   clear_bins(s);
-  // In the last bin lies, mostly, what has no mass, and may be most of a row: nobody adds it there.
+  // In the last bin lies what has next to no mass, and may be most of a row: in registers first (under 2^10 a token, 2^12 tokens a lane).
+  uint32_t far = 0;
   row.each([&](float l, int) {
     const float below = sc.below(l);
-    const uint32_t m = mass_of(below);
+    const unsigned long long m = mass_of(below);
     const uint32_t bin = (uint32_t)fminf(below * kBinsPerOctave, (float)(kBins - 1));
-    if (m) atomicAdd(&s.mass[bin], (unsigned long long)m);
-    if (!by_mass && bin < kBins - 1) atomicAdd(&s.count[bin], 1u);
+    far += bin < kBins - 1 ? 0u : (uint32_t)m;
+    if (bin < kBins - 1) {
+      atomicAdd(&s.mass[bin], m);
+      if (!by_mass) atomicAdd(&s.count[bin], 1u);
+    }
   });
+  far = (uint32_t)wave_sum_i((int)far);  // (under 2^28; a thousand lanes at one address of LDS would take 2.5 us)
+  if ((threadIdx.x & 63) == 0) atomicAdd(&s.mass[kBins - 1], (unsigned long long)far);
   __syncthreads();
-  // (a token of octave o has between 2^(30 - o) and 2^(31 - o))
-  if (by_mass) s.count[threadIdx.x] = (uint32_t)(s.mass[threadIdx.x] >> (30u - min(threadIdx.x / 32u, 30u)));
+  // (a token of octave o has between 2^(40 - o) and 2^(41 - o))
+  if (by_mass) s.count[threadIdx.x] = (uint32_t)(s.mass[threadIdx.x] >> (40u - threadIdx.x / 32u));
   Zone zone;
   zone.all = scan_bins(s, Target{by_mass, (uint32_t)f.k, inside ? mass_for(f.p, inside) : 0}, 0, 0, by_mass && !inside ? f.p : 1.f);
   zone.bin = s.bin < kBins - 1 ? s.bin : -1;
@@ -676,7 +689,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const Row<T, TOP
         run.at = most > run.best ? first : run.at;
         run.best = fmaxf(run.best, most);
       });
-      if (t == 0) run.z = (float)s.kept_mass * 4.656612873077393e-10f;
+      if (t == 0) run.z = (float)s.kept_mass * kMassUnit;
       unit_cut = cut_index;
     } else {
       row.each_unit([&](const RawUnit<T>& u, int first) {

@@ -651,6 +651,44 @@ def test_sample_infinities_and_nan():
     check_tokens(logits, None, top_k=[2] * 6)
 
 
+@pytest.mark.parametrize("octaves", [20.0, 30.0, 31.9, 32.1, 33.0, 36.0])
+def test_sample_long_tails_have_their_mass(octaves):
+    """One token and 150 000 that many octaves below it: a share p of the whole is reached so far along the tail.  Without random numbers the
+    first token is drawn, and its probability says how much was left (a sum in 32 bits)."""
+    n = 150000
+    l = np.full((1, n), -octaves * math.log(2.0), np.float32)
+    l[0, 70000] = 0.0
+    w = float(np.exp(float(l[0, 0])))
+    logits, total = torch.from_numpy(l).cuda(), 1 + (n - 1) * w
+    for share in (0.0, 0.25, 0.5, 0.9, 1.0):    # of the tail
+        p = float(np.float32((1 + share * (n - 1) * w) / total))
+        if p >= 1:
+            continue
+        token, prob = draw_tokens(logits, None, top_p=[p])
+        kept = min(max(p * total, 1.0), total)
+        # what is left is p of the whole and not more than one token of the tail beyond it.  Roundings: a mass 2^-42 and the exponent of its weight
+        # 2^-18 of it; of the sum the 150 tokens beside the first in its lane and ten additions across the lanes, the quotient, its inverse
+        assert token[0] == 70000
+        assert abs(1 / prob[0] - kept) <= 151 * w + 14 * 2.0 ** -24 + (n - 1) * (w * 2.0 ** -18 + 2.0 ** -42)
+
+
+def test_sample_deep_tails_are_in_reach_of_top_p():
+    """Half of the mass of a tail 32.5 octaves down: its tokens can be drawn, and the last ones cannot."""
+    n, octaves = 150000, 32.5
+    l = np.full((1, n), -octaves * math.log(2.0), np.float32)
+    l[0, 0] = 0.0
+    w = math.exp(float(l[0, 1]))
+    whole = 1 + (n - 1) * w
+    p = np.float32(1 - 0.5 * (n - 1) * w / whole)
+    assert p < 1
+    last = int(math.ceil((float(p) * whole - 1) / w))   # tokens 0 .. last are left, give or take the rounding of a mass: 2^-42 of 2^-32.5
+    for at, drawn in ((1, True), (last // 2, True), (last - last // 500, True), (last + last // 500, False), (n - 1, False)):
+        noise = torch.ones(1, n, device="cuda")
+        noise[0, at] = 1e-30
+        token, _ = draw_tokens(torch.from_numpy(l).cuda(), noise, top_p=[float(p)])
+        assert (token[0] == at) == drawn, (at, last, token)
+
+
 @pytest.mark.parametrize("n", [1, 5, 100, 511, 1000, 5003])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_sample_min_p_that_keeps_every_token(n, dtype):
