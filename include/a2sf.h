@@ -351,7 +351,7 @@ typedef struct {
  *   x, residual  [rows, n] dtype; residual may be NULL (h = x).
  *   weight       [n] dtype.
  *   total        out [rows, n] dtype; may be NULL, and may be the rows of x or residual.  The norm is of h before its
- *                rounding to dtype.
+ *                rounding to dtype, h being formed in 32 bits; its squares may leave their range at either end.
  *   out, out8    out: y in dtype, y in 8 bits; either may be NULL, not both.
  * n <= A2SF_MAX_ROW, eps >= 0 and finite. */
 a2sf_status a2sf_rms_norm(const a2sf_rows* x, const a2sf_rows* residual, const void* weight, float eps, int32_t rows,

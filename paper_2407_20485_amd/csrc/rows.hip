@@ -34,6 +34,7 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
 // rounding, which costs nothing here and is nearer to the definition).  The squares of a unit are added in fp32, the units in 64 bits, and
 // h is multiplied with what the roundings of its products cut off: then y is off by about one rounding to 32 bits, and
 // next to none of its 8-bit values is another than the definition's.
+// Rows whose squares leave the range of fp32 are summed once more in 64 bits (+0.4 us of 113 for the question).
 // THREADS = 64: a wave per row, four rows per workgroup, no barrier.
 // 16384 x 5120 in bf16 with a residual, its sum and 8-bit rows (588 MB): 113 us = 5.2 TB/s (a copy of 1 GiB: 5.2); 109 without the products' remainders,
 // but then one 8-bit value in 1 500 000 goes the other way, now one in 12 000 000.
@@ -65,16 +66,42 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel
     for (int j = 0; j < kUnit; ++j) s = fmaf(h[i][j], h[i][j], s);
     sum += s;
   }
-  sum = wave_sum_f64(sum);
-  if constexpr (THREADS > 64) {
-    __shared__ double part[THREADS / 64];
-    if ((t & 63) == 0) part[t >> 6] = sum;
-    __syncthreads();
+  const auto row_sum = [&](double v) {
+    v = wave_sum_f64(v);
+    if constexpr (THREADS > 64) {
+      __shared__ double part[THREADS / 64];
+      if ((t & 63) == 0) part[t >> 6] = v;
+      __syncthreads();
+      v = 0.0;
+#pragma unroll
+      for (int w = 0; w < THREADS / 64; ++w) v += part[w];
+    }
+    return v;
+  };
+  double mean = row_sum(sum) / a.n + a.eps;
+  T* total = a.total ? (T*)a.total + row * a.total_stride : nullptr;
+  double by = 1.0;  // what h was multiplied with
+  if (!(mean < 0x1p128) || mean < 0x1p-100) {
+    // Squares above the range of 32 bits, or so many under its normal numbers that their sum counts (the whole row sees the same mean): again in
+    // 64 bits, and h by a power of two into the middle of the range, where the factor is a normal number too.
     sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) sum += part[w];
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) sum += (double)h[i][j] * h[i][j];
+    if constexpr (THREADS > 64) __syncthreads();  // (the first sum's parts are read)
+    mean = row_sum(sum) / a.n + a.eps;
+    by = mean < 1.0 ? 0x1p100 : 0x1p-64;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = (i * THREADS + t) * kUnit;
+      if (total && c < a.n) store_unit(total + c, a.n - c, h[i]);
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) h[i][j] *= (float)by;
+    }
+    total = nullptr;
   }
-  const double factor = 1.0 / sqrt(sum / a.n + a.eps);
+  const double factor = 1.0 / sqrt(mean) / by;
   const float scale = (float)factor, rest = (float)(factor - scale);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -82,7 +109,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel
     const int have = a.n - c;
     // the 16 lanes of a block that ends inside it stay together: the exchange below reads all of them
     if ((c & ~(kBlock - 1)) >= a.n) break;
-    if (a.total && have > 0) store_unit((T*)a.total + row * a.total_stride + c, have, h[i]);
+    if (total && have > 0) store_unit(total + c, have, h[i]);
     float w[kUnit];
     load_unit((const T*)a.weight + c, have, w);
 #pragma unroll

@@ -147,6 +147,43 @@ def test_rms_norm_in_place(dtype):
     assert torch.equal(tr, total) and torch.equal(tx, out)
 
 
+@pytest.mark.parametrize("rows,n", [(3, 200), (5, 1000), (520, 2500), (2, 4096), (515, 9000), (2, 12000), (3, 40000)])
+@pytest.mark.parametrize("size", [3e38, 1e30, 4e19, 1e19, 1e17, 1e-15, 1e-18, 1e-25, 1e-36])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rms_norm_at_the_ends_of_the_range(rows, n, size, dtype):
+    """Finite rows whose squares are no finite or no normal numbers of 32 bits, without eps where it would be all of the mean.  The same
+    tolerance as in the middle of the range."""
+    g = rng(26, rows, n)
+    dt = DT[dtype]
+    x, r = (g.uniform(-0.49, 0.49, size=(rows, n)) * size for _ in range(2))
+    x[:, n // 3] = 0.5 * size                      # all of a row, or one element of it, is that large
+    x[1, : n // 2], r[1] = x[1, : n // 2] * 1e-3, 0.0
+    x, r = on_gpu(x, dt, stride=n + 1), on_gpu(r, dt)
+    w = on_gpu(1 + 0.1 * g.normal(size=(1, n)), dt)[0]
+    total, out = (on_gpu(np.zeros((rows, n)), dt, stride=n + s) for s in (2, 8))
+    q, s = eight(rows, n)
+    eps = 0.0 if size < 1 else 1e-5
+    B.a2sf_rms_norm(x, w, eps, residual=r, total=total, out=out, q=q, scales=s)
+    few = slice(0, rows, max(1, rows // 4))
+    h, y = L.rms_norm(host(x[few]), host(r[few]), host(w), eps)
+    half = BF16 if dtype == "bf16" else 0.0
+    # (bf16's subnormal numbers are 2^-133 apart)
+    assert (np.abs(host(total[few]) - h) <= (half + 2.0 ** -24) * np.abs(h) + (2.0 ** -134 if half else 0.0)).all()
+    slack = 3e-6 * np.abs(y) + 2.0 ** -24 * np.abs(y / np.where(h == 0, 1, h)) * (np.abs(host(x[few])) + np.abs(host(r[few])))
+    assert (np.abs(host(out[few]) - y) <= half * np.abs(y) + slack).all()
+    check_eight(q[few], s[few], y, 5e-6)
+    check_marks(q, s)
+
+
+def test_rms_norm_of_subnormal_numbers_without_eps():
+    x = torch.zeros(3, 300, device="cuda")
+    x[0, 7], x[1] = 1e-45, 3e-42
+    out = torch.empty_like(x)
+    B.a2sf_rms_norm(x, torch.ones(300, device="cuda"), 0.0, out=out)
+    assert abs(float(out[0, 7]) - math.sqrt(300)) < 1e-4 and float(out[0].abs().sum()) == float(out[0, 7])
+    assert bool(((out[1] - 1).abs() < 1e-6).all()) and bool(torch.isnan(out[2]).all())   # a row of zeros: 0 / 0
+
+
 def test_rms_norm_rows_that_are_not_numbers():
     x = torch.randn(6, 300, device="cuda")
     x[1, 5], x[2, 299] = math.nan, math.inf
