@@ -377,8 +377,9 @@ a2sf_status a2sf_quantize_weight(const a2sf_rows* w, int32_t n, int32_t k, int32
  *              instruction, at about twice the rate where the rate counts; it cuts each of eight neighbouring products of k under 2^-13
  *              of the largest of them, so a sum is within 8 * 2^-13 * sum |a b| of the exact one before it is rounded to bf16 (for data
  *              like a model's 1.5e-5 of the result's size; a sum that cancels may lose all of it).
- *   workspace  may be NULL; with a2sf_matmul_workspace_bytes(m, n, k) bytes (0: none is of use) products that have too few
- *              tiles for the whole chip split their sums over k.  The same sizes with the same choice give the same bits.
+ *   workspace  may be NULL; with a2sf_matmul_workspace_bytes(m, n, k) bytes (0: none is of use; enough for either kind of sums) products
+ *              that have too few tiles for the whole chip split their sums over k; with less, if their own parts fit.  The same sizes with
+ *              the same choices give the same bits.
  * Bytes of the rows past k are not used.  k <= 2^20, rows of a and b and rows of scales at most 2^23 bytes apart. */
 #define A2SF_WIDE_SUMS 0x100 /* or'ed to c_dtype */
 size_t a2sf_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);

@@ -729,8 +729,8 @@ template <typename S, typename T>
 void matmul(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t st) {
   constexpr bool kExact = sizeof(S) == 4;
   Choice c = choose(g.m, g.n, g.k, kExact, kMostScratch);
-  // (without the room that was asked for: no parts)
-  if (c.splits > 1 && (!workspace || workspace_bytes < matmul_workspace(g.m, g.n, g.k))) c = choose(g.m, g.n, g.k, kExact, 0);
+  // (without room for its parts: none)
+  if (c.splits > 1 && (!workspace || workspace_bytes < (size_t)c.splits * g.m * g.n * 4)) c = choose(g.m, g.n, g.k, kExact, 0);
   if (c.form == kStrip) {
     // Several workgroups to a compute unit where there are columns for them, eight waves else (1 x 5120 x 5120: three workgroups 6.4 us, two
     // 7.6, one 8.9; 1 x 4096 x 4096: eight waves 4.7, four 5.2; 32 x 12288 x 4096: two workgroups 10.4, one 12.0).

@@ -441,6 +441,26 @@ def test_matmul_wide_sums_keep_what_cancels(m):
     assert bool((c == 14 * 2.0 ** -6).all())
 
 
+@pytest.mark.parametrize("m,n,k,parts", [(300, 1000, 11008, 4), (500, 2048, 8192, 2)])
+def test_matmul_takes_a_workspace_that_its_own_parts_fit(m, n, k, parts):
+    """32-bit sums would be split in more parts than the 8-bit instruction's: a workspace for the fewer is enough for those."""
+    g = rng(27, m, n, k)
+    (a, sa), (b, sb) = operands(g, m, n, k, False)
+    args = (*filled(m, k, a, sa, 16), *filled(n, k, b, sb, 0))
+
+    def product(size):
+        c = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+        B.a2sf_matmul_scaled(*args, c, workspace=torch.empty(size, dtype=torch.uint8, device="cuda") if size else None)
+        return c
+
+    own = parts * m * n * 4
+    whole = B.a2sf_matmul_workspace_bytes(m, n, k)
+    assert own < whole
+    with_parts, without = product(whole), product(0)
+    assert not torch.equal(with_parts, without)
+    assert torch.equal(product(own), with_parts) and torch.equal(product(own - 16), without)
+
+
 @pytest.mark.parametrize("m", [1, 20, 200, 600])
 def test_matmul_scales_that_are_no_numbers_reach_their_rows_only(m):
     g = rng(7, m)
