@@ -326,6 +326,8 @@ a2sf_status a2sf_decode_plan(int32_t G, int32_t capacity, int32_t d, int32_t* ns
  *    16 bytes.
  *  - Where an input and an output are the same rows, every element is read before it is written.  Other overlaps are
  *    not allowed.
+ *  - A launch takes less than 2^32 lanes, and what needs more is refused with A2SF_ESHAPE: a row of a2sf_rms_norm takes 64 to 1024 by its
+ *    length, a row of a2sf_sample 1024, 128 columns of a2sf_quantize 16, 128 x 128 weights 256, 64 bytes of a token's heads in a2sf_rotary 1.
  *  - Sums, norms and products are formed in 32 bits or more whatever the type (a2sf_matmul_scaled: where the caller does not leave that
  *    to the 8-bit matrix instruction); results are rounded once. */
 typedef struct {

@@ -140,6 +140,8 @@ void launch_scores_bf16(const void* q, const void* k, const float* lse2, int G, 
 int first_contributing_row(int n, float alpha, float* log2_alpha);
 
 // ---- the operators around the attention ------------------------------------------------------------------------------------
+// A launch's lanes are counted in 32 bits: false, and nothing launched, where a call would take more.
+inline bool grid_fits(unsigned long long groups, unsigned lanes) { return groups * lanes <= 0xFFFFFFFFull; }
 // rows.hip.  Strides in elements (8-bit rows and scales: bytes); absent tensors are null.
 struct NormArgs {
   const void *x, *residual, *weight;
@@ -149,7 +151,7 @@ struct NormArgs {
   float eps;
   int rows, n;
 };
-void launch_rms_norm(const NormArgs& a, int dtype, hipStream_t st);
+bool launch_rms_norm(const NormArgs& a, int dtype, hipStream_t st);
 struct QuantArgs {
   const void *x, *gate;
   void* out;
@@ -157,8 +159,8 @@ struct QuantArgs {
   long long x_stride, gate_stride, out_stride, q_stride, scale_stride;
   int rows, n, blocks_per_row;
 };
-void launch_quantize(const QuantArgs& a, int dtype, hipStream_t st);
-void launch_quantize_weight(const QuantArgs& a, int dtype, hipStream_t st);
+bool launch_quantize(const QuantArgs& a, int dtype, hipStream_t st);
+bool launch_quantize_weight(const QuantArgs& a, int dtype, hipStream_t st);
 
 // matmul.hip: C[m, n] = A[m, k] B[n, k]^T
 struct MatmulArgs {
@@ -190,7 +192,7 @@ struct RotaryArgs {
   int turning, items;
   uint32_t first_block[A2SF_MAX_ROTARY_PARTS];
 };
-void launch_rotary(RotaryArgs a, int dtype, bool neighbours, hipStream_t st);
+bool launch_rotary(RotaryArgs a, int dtype, bool neighbours, hipStream_t st);
 struct RotaryTableArgs {
   float* table;
   int rows, rot, original_length;
@@ -209,6 +211,6 @@ struct SampleArgs {
   long long stride, noise_stride;
   int rows, n;
 };
-void launch_sample(const SampleArgs& a, int dtype, hipStream_t st);
+bool launch_sample(const SampleArgs& a, int dtype, hipStream_t st);
 
 }  // namespace a2sf

@@ -48,7 +48,7 @@ long long stride(const R* r) { return r ? (long long)r->stride : 0; }
 template <typename F>
 a2sf_status launched(F launch) {
   (void)hipGetLastError();
-  launch();
+  if (!launch()) return A2SF_ESHAPE;
   return hipGetLastError() == hipSuccess ? A2SF_OK : A2SF_EHIP;
 }
 
@@ -84,7 +84,7 @@ a2sf_status a2sf_rms_norm(const a2sf_rows* x, const a2sf_rows* residual, const v
   a.eps = eps;
   a.rows = rows;
   a.n = n;
-  return launched([&] { launch_rms_norm(a, dtype, (hipStream_t)hip_stream); });
+  return launched([&] { return launch_rms_norm(a, dtype, (hipStream_t)hip_stream); });
 }
 
 a2sf_status a2sf_quantize(const a2sf_rows* x, const a2sf_rows* gate, int32_t rows, int32_t n, int32_t dtype,
@@ -108,7 +108,7 @@ a2sf_status a2sf_quantize(const a2sf_rows* x, const a2sf_rows* gate, int32_t row
   a.rows = rows;
   a.n = n;
   a.blocks_per_row = blocks(n);
-  return launched([&] { launch_quantize(a, dtype, (hipStream_t)hip_stream); });
+  return launched([&] { return launch_quantize(a, dtype, (hipStream_t)hip_stream); });
 }
 
 a2sf_status a2sf_quantize_weight(const a2sf_rows* w, int32_t n, int32_t k, int32_t dtype, const a2sf_rows8* out8,
@@ -130,7 +130,7 @@ a2sf_status a2sf_quantize_weight(const a2sf_rows* w, int32_t n, int32_t k, int32
   a.rows = n;
   a.n = k;
   a.blocks_per_row = blocks(k);
-  return launched([&] { launch_quantize_weight(a, dtype, (hipStream_t)hip_stream); });
+  return launched([&] { return launch_quantize_weight(a, dtype, (hipStream_t)hip_stream); });
 }
 
 size_t a2sf_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k) {
@@ -168,7 +168,7 @@ a2sf_status a2sf_matmul_scaled(const a2sf_rows8* a, const a2sf_rows8* b, int32_t
   g.m = m;
   g.n = n;
   g.k = k;
-  return launched([&] { launch_matmul(g, c_dtype, wide_sums, workspace, workspace ? workspace_bytes : 0, (hipStream_t)hip_stream); });
+  return launched([&] { return launch_matmul(g, c_dtype, wide_sums, workspace, workspace ? workspace_bytes : 0, (hipStream_t)hip_stream), true; });
 }
 
 a2sf_status a2sf_rotary(const a2sf_rotary_part* parts, int32_t n_parts, int32_t batch, int32_t length, int32_t d,
@@ -212,7 +212,7 @@ a2sf_status a2sf_rotary(const a2sf_rotary_part* parts, int32_t n_parts, int32_t 
   a.pos_stride = pos_stride;
   a.table = table;
   a.table_rows = table_rows;
-  return launched([&] { launch_rotary(a, dtype, pairs == A2SF_ROTARY_NEIGHBOURS, (hipStream_t)hip_stream); });
+  return launched([&] { return launch_rotary(a, dtype, pairs == A2SF_ROTARY_NEIGHBOURS, (hipStream_t)hip_stream); });
 }
 
 a2sf_status a2sf_rotary_table(float* table, int32_t table_rows, int32_t rotary_dims, double base, double factor,
@@ -224,7 +224,7 @@ a2sf_status a2sf_rotary_table(float* table, int32_t table_rows, int32_t rotary_d
       original_length < 0 || !isfinite(low) || !isfinite(high) || low > high)
     return A2SF_EINVAL;
   const RotaryTableArgs a = {table, table_rows, rotary_dims, original_length, base, factor, low, high, magnitude};
-  return launched([&] { launch_rotary_table(a, (hipStream_t)hip_stream); });
+  return launched([&] { return launch_rotary_table(a, (hipStream_t)hip_stream), true; });
 }
 
 a2sf_status a2sf_sample(const a2sf_rows* logits, const a2sf_rows* noise, int32_t rows, int32_t n, int32_t dtype,
@@ -250,7 +250,7 @@ a2sf_status a2sf_sample(const a2sf_rows* logits, const a2sf_rows* noise, int32_t
   a.noise_stride = stride(noise);
   a.rows = rows;
   a.n = n;
-  return launched([&] { launch_sample(a, dtype, (hipStream_t)hip_stream); });
+  return launched([&] { return launch_sample(a, dtype, (hipStream_t)hip_stream); });
 }
 
 }  // extern "C"

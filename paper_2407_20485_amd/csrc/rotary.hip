@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256) void rotary_table_kernel(RotaryTableArgs a) {
 }
 
 template <typename T>
-void rotary(RotaryArgs a, bool neighbours, hipStream_t st) {
+bool rotary(RotaryArgs a, bool neighbours, hipStream_t st) {
   constexpr int W = Chunk<T>::kCount;
   const int turned = neighbours ? a.rot : a.rot / 2;
   a.turning = (turned + W - 1) / W;
@@ -197,6 +197,7 @@ void rotary(RotaryArgs a, bool neighbours, hipStream_t st) {
     P.tokens_per_block = 256 / P.lanes;
     grid += (uint32_t)((tokens + P.tokens_per_block - 1) / P.tokens_per_block);
   }
+  if (!grid_fits(grid, 256)) return false;
   if (neighbours) {
     if (whole) rotary_kernel<T, true, true><<<grid, 256, 0, st>>>(a);
     else rotary_kernel<T, true, false><<<grid, 256, 0, st>>>(a);
@@ -204,13 +205,13 @@ void rotary(RotaryArgs a, bool neighbours, hipStream_t st) {
     if (whole) rotary_kernel<T, false, true><<<grid, 256, 0, st>>>(a);
     else rotary_kernel<T, false, false><<<grid, 256, 0, st>>>(a);
   }
+  return true;
 }
 
 }  // namespace
 
-void launch_rotary(RotaryArgs a, int dtype, bool neighbours, hipStream_t st) {
-  if (dtype == A2SF_F32) rotary<float>(a, neighbours, st);
-  else rotary<bf16_t>(a, neighbours, st);
+bool launch_rotary(RotaryArgs a, int dtype, bool neighbours, hipStream_t st) {
+  return dtype == A2SF_F32 ? rotary<float>(a, neighbours, st) : rotary<bf16_t>(a, neighbours, st);
 }
 
 void launch_rotary_table(const RotaryTableArgs& a, hipStream_t st) {

@@ -143,23 +143,28 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel
 }
 
 template <typename T, int THREADS, int V>
-void norm(const NormArgs& a, hipStream_t st) {
-  constexpr int kRows = THREADS == 64 ? 4 : 1;
-  rms_norm_kernel<T, THREADS, V><<<dim3((a.rows + kRows - 1) / kRows), dim3(THREADS == 64 ? 256 : THREADS), 0, st>>>(a);
+bool norm(const NormArgs& a, hipStream_t st) {
+  constexpr int kRows = THREADS == 64 ? 4 : 1, kLanes = THREADS == 64 ? 256 : THREADS;
+  const uint32_t groups = ((uint32_t)a.rows + kRows - 1) / kRows;
+  if (!grid_fits(groups, kLanes)) return false;
+  rms_norm_kernel<T, THREADS, V><<<dim3(groups), dim3(kLanes), 0, st>>>(a);
+  return true;
 }
 template <typename T, int THREADS>
-void norm_units(const NormArgs& a, hipStream_t st) {
+bool norm_units(const NormArgs& a, hipStream_t st) {
   const int v = (a.n + THREADS * kUnit - 1) / (THREADS * kUnit);
   if (v <= 1) return norm<T, THREADS, 1>(a, st);
   if (v <= 2) return norm<T, THREADS, 2>(a, st);
-  if (v <= 3) return norm<T, THREADS, 3>(a, st);
-  if constexpr (THREADS != 256) {
-    if (v <= 4) return norm<T, THREADS, 4>(a, st);
+  if constexpr (THREADS == 256 || THREADS == 512) {  // (no more units than three)
+    return norm<T, THREADS, 3>(a, st);
+  } else {
+    if (v <= 3) return norm<T, THREADS, 3>(a, st);
+    if (v <= 4 || THREADS == 64) return norm<T, THREADS, 4>(a, st);
+    if constexpr (THREADS == 1024) return norm<T, THREADS, 8>(a, st);
   }
-  if constexpr (THREADS == 1024) return norm<T, THREADS, 8>(a, st);
 }
 template <typename T>
-void norm_type(const NormArgs& a, hipStream_t st) {
+bool norm_type(const NormArgs& a, hipStream_t st) {
   // A wave per row needs no barrier; of 16 bits also where it has four units (16384 x 1280: 31 us, by 256 lanes 40; fp32 47 and 44)
   if (a.n <= 2 * 64 * kUnit || (sizeof(T) == 2 && a.rows >= 4096 && a.n <= 4 * 64 * kUnit)) return norm_units<T, 64>(a, st);
   if (a.rows < 512 && a.n > 256 * kUnit) {
@@ -249,13 +254,13 @@ __global__ __launch_bounds__(256) void quantize_weight_kernel(QuantArgs a) {
 
 }  // namespace
 
-void launch_rms_norm(const NormArgs& a, int dtype, hipStream_t st) {
-  if (dtype == A2SF_F32) norm_type<float>(a, st);
-  else norm_type<bf16_t>(a, st);
+bool launch_rms_norm(const NormArgs& a, int dtype, hipStream_t st) {
+  return dtype == A2SF_F32 ? norm_type<float>(a, st) : norm_type<bf16_t>(a, st);
 }
 
-void launch_quantize(const QuantArgs& a, int dtype, hipStream_t st) {
+bool launch_quantize(const QuantArgs& a, int dtype, hipStream_t st) {
   const dim3 grid((uint32_t)(((long long)a.rows * a.blocks_per_row + 15) / 16));
+  if (!grid_fits(grid.x, 256)) return false;
   if (dtype == A2SF_F32) {
     if (a.gate) quantize_kernel<float, true><<<grid, 256, 0, st>>>(a);
     else quantize_kernel<float, false><<<grid, 256, 0, st>>>(a);
@@ -263,12 +268,15 @@ void launch_quantize(const QuantArgs& a, int dtype, hipStream_t st) {
     if (a.gate) quantize_kernel<bf16_t, true><<<grid, 256, 0, st>>>(a);
     else quantize_kernel<bf16_t, false><<<grid, 256, 0, st>>>(a);
   }
+  return true;
 }
 
-void launch_quantize_weight(const QuantArgs& a, int dtype, hipStream_t st) {
+bool launch_quantize_weight(const QuantArgs& a, int dtype, hipStream_t st) {
   const dim3 grid((uint32_t)((a.rows + kBlock - 1) / kBlock) * (uint32_t)a.blocks_per_row);
+  if (!grid_fits(grid.x, 256)) return false;
   if (dtype == A2SF_F32) quantize_weight_kernel<float><<<grid, 256, 0, st>>>(a);
   else quantize_weight_kernel<bf16_t><<<grid, 256, 0, st>>>(a);
+  return true;
 }
 
 }  // namespace a2sf

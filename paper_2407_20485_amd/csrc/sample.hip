@@ -809,18 +809,19 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
 }
 
 template <typename T>
-void sample(const SampleArgs& a, hipStream_t st) {
+bool sample(const SampleArgs& a, hipStream_t st) {
   static const hipError_t raised =
       hipFuncSetAttribute((const void*)sample_kernel<T>, hipFuncAttributeMaxDynamicSharedMemorySize, kSampleLds);
   (void)raised;
+  if (!grid_fits(a.rows, kSampleThreads)) return false;
   sample_kernel<T><<<a.rows, kSampleThreads, kSampleLds, st>>>(a);
+  return true;
 }
 
 }  // namespace
 
-void launch_sample(const SampleArgs& a, int dtype, hipStream_t st) {
-  if (dtype == A2SF_F32) sample<float>(a, st);
-  else sample<bf16_t>(a, st);
+bool launch_sample(const SampleArgs& a, int dtype, hipStream_t st) {
+  return dtype == A2SF_F32 ? sample<float>(a, st) : sample<bf16_t>(a, st);
 }
 
 }  // namespace a2sf

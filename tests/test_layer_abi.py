@@ -197,3 +197,18 @@ def test_matmul_choice_of_sums_is_checked_with_the_type():
     assert f(B.A2SF_BF16 | B.A2SF_WIDE_SUMS, k=0) == B.A2SF_ESHAPE
     header = open(os.path.join(os.path.dirname(B.__file__), "..", "include", "a2sf.h")).read()
     assert int(re.search(r"#define A2SF_WIDE_SUMS (0x[0-9a-f]+)", header)[1], 16) == B.A2SF_WIDE_SUMS
+
+
+def test_calls_of_more_lanes_than_a_launch_takes_are_refused():
+    """Found on the host: no launch is tried."""
+    L, far = B.lib(), 1 << 17
+    for n, m in ((1025, 2 ** 24), (5000, 2 ** 24), (10000, 2 ** 23), (40000, 2 ** 22), (128, 2 ** 26 + 4)):
+        assert L.a2sf_rms_norm(rows(stride=far), None, FAKE, 1e-5, m, n, B.A2SF_F32, None, rows(stride=far), None, None) == B.A2SF_ESHAPE, n
+    for gate in (None, rows(stride=far)):
+        assert L.a2sf_quantize(rows(stride=far), gate, 2 ** 28, 100, B.A2SF_BF16, rows(stride=far), None, None) == B.A2SF_ESHAPE
+        assert L.a2sf_quantize(rows(stride=far), gate, 2 ** 27, 200, B.A2SF_F32, rows(stride=far), None, None) == B.A2SF_ESHAPE
+    out8 = rows8(stride=far, scale_stride=1024)
+    assert L.a2sf_quantize_weight(rows(stride=far), 2 ** 24, 2 ** 14, B.A2SF_BF16, out8, None) == B.A2SF_ESHAPE
+    assert L.a2sf_sample(rows(stride=far), None, 2 ** 22, 100, B.A2SF_F32, None, None, None, None, FAKE, None, None) == B.A2SF_ESHAPE
+    made = (B.RotaryPart * 1)(part(xs=(far, far, 512), ys=(far, far, 512), heads=64))
+    assert L.a2sf_rotary(made, 1, 2 ** 24, 4, 512, B.A2SF_F32, FAKE, 4, FAKE, 32, 64, 0, 0, None) == B.A2SF_ESHAPE
