@@ -424,30 +424,46 @@ def _need(ok, status=A2SF_ESHAPE):
         raise A2SFError(status)
 
 
+def _reach(x, like):
+    """x is memory that the GPU of `like` can read: its own, or pinned memory of the host."""
+    if x.device != like.device:
+        _need(not like.is_cuda if x.is_cuda else x.device.type == "cpu" and x.is_pinned(), A2SF_EINVAL)
+
+
+def _stream_of(first, stream):
+    """The stream of a call that takes its sizes from `first`, which has to be such memory too."""
+    _need(first.is_cuda or not torch.cuda.is_available() or first.is_pinned(), A2SF_EINVAL)
+    return _stream(stream)
+
+
 def _rows(x, like, dtype=None):
     """The C struct of [rows, n] (None of None); `like`: the tensor whose sizes (and type, unless one is named) it has to have."""
     if x is None:
         return None
+    _reach(x, like)
     _need(x.dim() == 2 and x.shape == like.shape and (x.stride(1) == 1 or x.shape[1] == 1))
     _need(x.dtype == (dtype or like.dtype), A2SF_EDTYPE)
     return Rows(x.data_ptr(), x.stride(0))
 
 
-def _rows8(q, scales, rows, n, scale_rows=None):
+def _rows8(q, scales, rows, n, like, scale_rows=None):
     """... of 8-bit rows [rows, n] (torch.float8_e4m3fn, or uint8 for their bytes) and scales [scale_rows, ceil(n / 128)] uint8."""
     if q is None and scales is None:
         return None
     _need(q is not None and scales is not None, A2SF_EINVAL)
+    _reach(q, like)
+    _reach(scales, like)
     _need(q.dtype in _EIGHT_BIT and scales.dtype == torch.uint8, A2SF_EDTYPE)
     _need(tuple(q.shape) == (rows, n) and (q.stride(1) == 1 or n == 1))
     _need(tuple(scales.shape) == (scale_rows or rows, -(-n // 128)) and (scales.stride(1) == 1 or n <= 128))
     return Rows8(q.data_ptr(), scales.data_ptr(), q.stride(0), scales.stride(0))
 
 
-def _column(x, rows, dtype):
+def _column(x, rows, dtype, like):
     """The address of [rows] (None of None)."""
     if x is None:
         return None
+    _reach(x, like)
     _need(x.dim() == 1 and x.shape[0] == rows and (x.stride(0) == 1 or rows == 1))
     _need(x.dtype == dtype, A2SF_EDTYPE)
     return x.data_ptr()
@@ -460,8 +476,8 @@ def a2sf_rms_norm(x, weight, eps, residual=None, total=None, out=None, q=None, s
         return _check(status)
     _need(x.dim() == 2)
     rows, n = x.shape
-    _check(lib().a2sf_rms_norm(_rows(x, x), _rows(residual, x), _column(weight, n, x.dtype), eps, rows, n, dtype_code(x.dtype),
-                               _rows(total, x), _rows(out, x), _rows8(q, scales, rows, n), _stream(stream)))
+    _check(lib().a2sf_rms_norm(_rows(x, x), _rows(residual, x), _column(weight, n, x.dtype, x), eps, rows, n, dtype_code(x.dtype),
+                               _rows(total, x), _rows(out, x), _rows8(q, scales, rows, n, x), _stream_of(x, stream)))
 
 
 def a2sf_quantize(x, q, scales, gate=None, out=None, stream=None):
@@ -472,14 +488,14 @@ def a2sf_quantize(x, q, scales, gate=None, out=None, stream=None):
     _need(x.dim() == 2)
     rows, n = x.shape
     _check(lib().a2sf_quantize(_rows(x, x), _rows(gate, x), rows, n, dtype_code(x.dtype), _rows(out, x),
-                               _rows8(q, scales, rows, n), _stream(stream)))
+                               _rows8(q, scales, rows, n, x), _stream_of(x, stream)))
 
 
 def a2sf_quantize_weight(w, q, scales, stream=None):
     _need(w.dim() == 2)
     n, k = w.shape
-    _check(lib().a2sf_quantize_weight(_rows(w, w), n, k, dtype_code(w.dtype), _rows8(q, scales, n, k, -(-n // 128)),
-                                      _stream(stream)))
+    _check(lib().a2sf_quantize_weight(_rows(w, w), n, k, dtype_code(w.dtype), _rows8(q, scales, n, k, w, -(-n // 128)),
+                                      _stream_of(w, stream)))
 
 
 def a2sf_matmul_workspace_bytes(m, n, k) -> int:
@@ -498,9 +514,11 @@ def a2sf_matmul_scaled(a, a_scales, b, b_scales, c, workspace=None, workspace_by
     _need(tuple(c.shape) == (m, n))
     if workspace_bytes is None:
         workspace_bytes = workspace.nbytes if workspace is not None else 0
-    _check(lib().a2sf_matmul_scaled(_rows8(a, a_scales, m, k), _rows8(b, b_scales, n, k, -(-n // 128)), m, n, k, _rows(c, c),
+    if isinstance(workspace, torch.Tensor):
+        _reach(workspace, c)
+    _check(lib().a2sf_matmul_scaled(_rows8(a, a_scales, m, k, c), _rows8(b, b_scales, n, k, c, -(-n // 128)), m, n, k, _rows(c, c),
                                     dtype_code(c.dtype) | (A2SF_WIDE_SUMS if wide_sums else 0), _ptr(workspace), workspace_bytes,
-                                    _stream(stream)))
+                                    _stream_of(c, stream)))
 
 
 def a2sf_rotary(parts, pos, table, interleaved=False, inverse=False, stream=None):
@@ -519,21 +537,26 @@ def a2sf_rotary(parts, pos, table, interleaved=False, inverse=False, stream=None
         _need(x.dim() == 4 and x.shape == y.shape and x.shape[:2] == (batch, length) and x.shape[3] == d)
         _need((x.stride(3) == 1 and y.stride(3) == 1) or d == 1)
         _need(x.dtype == first.dtype and y.dtype == first.dtype, A2SF_EDTYPE)
+        _reach(x, first)
+        _reach(y, first)
         to.x, to.y, to.heads, to.rotate = x.data_ptr(), y.data_ptr(), x.shape[2], int(rotate[0]) if rotate else 1
         to.x_stride[:], to.y_stride[:] = x.stride()[:3], y.stride()[:3]
     _need(tuple(pos.shape) == (batch, length) and (pos.stride(1) == 1 or length == 1))
     _need(table.dim() == 2 and table.is_contiguous())
     _need(pos.dtype == torch.int32 and table.dtype == torch.float32, A2SF_EDTYPE)
+    _reach(pos, first)
+    _reach(table, first)
+    _need(table.shape[1] <= d)
     _check(lib().a2sf_rotary(made, len(parts), batch, length, d, dtype_code(first.dtype), pos.data_ptr(), pos.stride(0),
                              table.data_ptr(), table.shape[0], table.shape[1], int(bool(interleaved)), int(bool(inverse)),
-                             _stream(stream)))
+                             _stream_of(first, stream)))
 
 
 def a2sf_rotary_table(table, base=10000.0, factor=1.0, original_length=0, low=0.0, high=0.0, magnitude=1.0, stream=None):
     _need(table.dim() == 2 and table.is_contiguous())
     _need(table.dtype == torch.float32, A2SF_EDTYPE)
     _check(lib().a2sf_rotary_table(table.data_ptr(), table.shape[0], table.shape[1], base, factor, original_length, low,
-                                   high, magnitude, _stream(stream)))
+                                   high, magnitude, _stream_of(table, stream)))
 
 
 def a2sf_sample(logits, noise, token, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, stream=None):
@@ -545,6 +568,7 @@ def a2sf_sample(logits, noise, token, temperature=None, top_k=None, top_p=None, 
     rows, n = logits.shape
     f = torch.float32
     _check(lib().a2sf_sample(_rows(logits, logits), _rows(noise, logits, f), rows, n, dtype_code(logits.dtype),
-                             _column(temperature, rows, f), _column(top_k, rows, torch.int32), _column(top_p, rows, f),
-                             _column(min_p, rows, f), _column(token, rows, torch.int32), _column(prob, rows, f),
-                             _stream(stream)))
+                             _column(temperature, rows, f, logits), _column(top_k, rows, torch.int32, logits),
+                             _column(top_p, rows, f, logits), _column(min_p, rows, f, logits),
+                             _column(token, rows, torch.int32, logits), _column(prob, rows, f, logits),
+                             _stream_of(logits, stream)))

@@ -184,7 +184,7 @@ PyObject* prefill_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // ---- the operators around the attention: [rows, n] tensors, whose sizes, strides and types the C arguments come from.  What
-// does not fit together (or is no plain tensor) is left to binding.py, which names the error.
+// does not fit together, lies on another device (or is no plain tensor) is left to binding.py, which names the error.
 bool type_of(const at::Tensor& t, int32_t* dtype) {
   const auto k = t.scalar_type();
   *dtype = k == at::kFloat ? A2SF_F32 : A2SF_BF16;
@@ -198,16 +198,18 @@ bool rows_like(PyObject* x, const at::Tensor& like, at::ScalarType type, a2sf_ro
   const at::Tensor* t;
   *to = nullptr;
   if (x == Py_None) return true;
-  if (!tensor(x, &t) || t->scalar_type() != type || !matrix(*t, like.size(0), like.size(1))) return false;
+  if (!tensor(x, &t) || t->scalar_type() != type || !matrix(*t, like.size(0), like.size(1)) || t->device() != like.device()) return false;
   *s = {t->data_ptr(), t->stride(0)};
   *to = s;
   return true;
 }
-bool rows8(PyObject* q, PyObject* scales, int64_t rows, int64_t scale_rows, int64_t n, a2sf_rows8* s, const a2sf_rows8** to) {
+bool rows8(PyObject* q, PyObject* scales, const at::Tensor& like, int64_t rows, int64_t scale_rows, int64_t n, a2sf_rows8* s,
+           const a2sf_rows8** to) {
   const at::Tensor *t, *u;
   *to = nullptr;
   if (q == Py_None && scales == Py_None) return true;
-  if (!tensor(q, &t) || !tensor(scales, &u) || u->scalar_type() != at::kByte) return false;
+  if (!tensor(q, &t) || !tensor(scales, &u) || u->scalar_type() != at::kByte || t->device() != like.device() || u->device() != like.device())
+    return false;
   if (t->scalar_type() != at::kFloat8_e4m3fn && t->scalar_type() != at::kByte) return false;
   const int64_t nb = n / 128 + (n % 128 != 0);
   if (!matrix(*t, rows, n) || !matrix(*u, scale_rows, nb)) return false;
@@ -215,11 +217,12 @@ bool rows8(PyObject* q, PyObject* scales, int64_t rows, int64_t scale_rows, int6
   *to = s;
   return true;
 }
-bool column(PyObject* x, int64_t rows, at::ScalarType type, const void** p) {
+bool column(PyObject* x, const at::Tensor& like, int64_t rows, at::ScalarType type, const void** p) {
   const at::Tensor* t;
   *p = nullptr;
   if (x == Py_None) return true;
-  if (!tensor(x, &t) || t->scalar_type() != type || t->dim() != 1 || t->size(0) != rows || (rows != 1 && t->stride(0) != 1))
+  if (!tensor(x, &t) || t->scalar_type() != type || t->dim() != 1 || t->size(0) != rows || (rows != 1 && t->stride(0) != 1) ||
+      t->device() != like.device())
     return false;
   *p = t->data_ptr();
   return true;
@@ -242,9 +245,9 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t dtype;
     float eps;
     if (!(fn && first(a[1], &x, &dtype) && rows_like(a[1], *x, x->scalar_type(), s, &rx) &&
-          column(a[2], x->size(1), x->scalar_type(), &w) && number(a[3], &eps) &&
+          column(a[2], *x, x->size(1), x->scalar_type(), &w) && number(a[3], &eps) &&
           rows_like(a[4], *x, x->scalar_type(), s + 1, &residual) && rows_like(a[5], *x, x->scalar_type(), s + 2, &total) &&
-          rows_like(a[6], *x, x->scalar_type(), s + 3, &out) && rows8(a[7], a[8], x->size(0), x->size(0), x->size(1), &s8, &out8) &&
+          rows_like(a[6], *x, x->scalar_type(), s + 3, &out) && rows8(a[7], a[8], *x, x->size(0), x->size(0), x->size(1), &s8, &out8) &&
           stream(a[9], a[1], &st)))
       return -1;
     return without_gil([&]() -> int {
@@ -266,7 +269,7 @@ PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const a2sf_rows8* out8;
     int32_t dtype;
     if (!(fn && first(a[1], &x, &dtype) && rows_like(a[1], *x, x->scalar_type(), s, &rx) &&
-          rows8(a[2], a[3], x->size(0), x->size(0), x->size(1), &s8, &out8) &&
+          rows8(a[2], a[3], *x, x->size(0), x->size(0), x->size(1), &s8, &out8) &&
           rows_like(a[4], *x, x->scalar_type(), s + 1, &gate) && rows_like(a[5], *x, x->scalar_type(), s + 2, &out) &&
           stream(a[6], a[1], &st)))
       return -1;
@@ -286,14 +289,14 @@ PyObject* matmul_scaled(PyObject*, PyObject* const* a, Py_ssize_t n) {
     a2sf_rows8 s8[2];
     const a2sf_rows* rc;
     const a2sf_rows8 *ra, *rb;
-    const at::Tensor* ta;
+    const at::Tensor *ta, *room;
     size_t bytes;
     int32_t dtype;
     if (!(fn && first(a[5], &c, &dtype) && rows_like(a[5], *c, c->scalar_type(), &s, &rc) && tensor(a[1], &ta) && ta->dim() == 2 &&
           tensor(a[3], &b) && ta->size(1) <= INT32_MAX &&
-          rows8(a[1], a[2], c->size(0), c->size(0), ta->size(1), s8, &ra) &&
-          rows8(a[3], a[4], c->size(1), c->size(1) / 128 + (c->size(1) % 128 != 0), ta->size(1), s8 + 1, &rb) &&
-          workspace(a[6], a[7], &ws, &bytes) && stream(a[8], a[1], &st) && (n == 9 || PyBool_Check(a[9]))))
+          rows8(a[1], a[2], *c, c->size(0), c->size(0), ta->size(1), s8, &ra) &&
+          rows8(a[3], a[4], *c, c->size(1), c->size(1) / 128 + (c->size(1) % 128 != 0), ta->size(1), s8 + 1, &rb) &&
+          workspace(a[6], a[7], &ws, &bytes) && (!tensor(a[6], &room) || room->device() == c->device()) && stream(a[8], a[1], &st) && (n == 9 || PyBool_Check(a[9]))))
       return -1;
     if (n == 10 && a[9] == Py_True) dtype |= A2SF_WIDE_SUMS;
     return without_gil([&]() -> int {
@@ -326,7 +329,8 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
           if (x->size(j) > INT32_MAX) return -1;
       }
       if (x->size(0) != head->size(0) || x->size(1) != head->size(1) || x->size(3) != head->size(3) || x->size(2) > INT32_MAX ||
-          x->scalar_type() != head->scalar_type() || y->scalar_type() != head->scalar_type() ||
+          x->scalar_type() != head->scalar_type() || y->scalar_type() != head->scalar_type() || x->device() != head->device() ||
+          y->device() != head->device() ||
           (x->size(3) != 1 && (x->stride(3) != 1 || y->stride(3) != 1)))
         return -1;
       parts[i].x = x->data_ptr();
@@ -340,7 +344,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (!tensor(a[2], &pos) || pos->scalar_type() != at::kInt || !matrix(*pos, head->size(0), head->size(1)) || !tensor(a[3], &table) ||
         table->scalar_type() != at::kFloat || table->dim() != 2 || !table->is_contiguous() || table->size(0) > INT32_MAX ||
-        table->size(1) > INT32_MAX || !PyBool_Check(a[4]) || !PyBool_Check(a[5]) || !stream(a[6], a[2], &st))
+        table->size(1) > INT32_MAX || pos->device() != head->device() || table->device() != head->device() || !PyBool_Check(a[4]) || !PyBool_Check(a[5]) || !stream(a[6], a[2], &st))
       return -1;
     return without_gil([&]() -> int {
       return ((decltype(&a2sf_rotary))fn)(parts, count, (int32_t)head->size(0), (int32_t)head->size(1), (int32_t)head->size(3), dtype,
@@ -361,10 +365,10 @@ PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const void *token, *temperature, *top_k, *top_p, *min_p, *prob;
     int32_t dtype;
     if (!(fn && first(a[1], &x, &dtype) && rows_like(a[1], *x, x->scalar_type(), s, &logits) &&
-          rows_like(a[2], *x, at::kFloat, s + 1, &noise) && column(a[3], x->size(0), at::kInt, &token) &&
-          column(a[4], x->size(0), at::kFloat, &temperature) && column(a[5], x->size(0), at::kInt, &top_k) &&
-          column(a[6], x->size(0), at::kFloat, &top_p) && column(a[7], x->size(0), at::kFloat, &min_p) &&
-          column(a[8], x->size(0), at::kFloat, &prob) && stream(a[9], a[1], &st)))
+          rows_like(a[2], *x, at::kFloat, s + 1, &noise) && column(a[3], *x, x->size(0), at::kInt, &token) &&
+          column(a[4], *x, x->size(0), at::kFloat, &temperature) && column(a[5], *x, x->size(0), at::kInt, &top_k) &&
+          column(a[6], *x, x->size(0), at::kFloat, &top_p) && column(a[7], *x, x->size(0), at::kFloat, &min_p) &&
+          column(a[8], *x, x->size(0), at::kFloat, &prob) && stream(a[9], a[1], &st)))
       return -1;
     return without_gil([&]() -> int {
       return ((decltype(&a2sf_sample))fn)(logits, noise, (int32_t)x->size(0), (int32_t)x->size(1), dtype, (const float*)temperature,

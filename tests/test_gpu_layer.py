@@ -873,3 +873,25 @@ def test_calls_on_another_stream_and_through_ctypes(monkeypatch):
             calls()
         torch.cuda.synchronize()
         assert all(torch.equal(t, e) for t, e in zip(outs, eager)), way
+
+
+def test_tensors_of_the_host_are_refused_and_pinned_ones_taken():
+    logits = torch.randn(4, 50, device="cuda")
+    token, k = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.tensor([1, 2, 3, 4], dtype=torch.int32)
+    for at in (dict(top_k=k), dict(top_p=torch.ones(4)), dict(prob=torch.ones(4))):
+        with pytest.raises(B.A2SFError) as e:
+            B.a2sf_sample(logits, None, token, **at)
+        assert e.value.status == B.A2SF_EINVAL
+    for args in ((logits.cpu(), None, token), (logits.cpu(), None, token.cpu()), (logits, None, token.cpu()), (logits, logits.cpu(), token)):
+        with pytest.raises(B.A2SFError) as e:
+            B.a2sf_sample(*args)
+        assert e.value.status == B.A2SF_EINVAL
+    x, w = torch.randn(3, 256, device="cuda"), torch.ones(256)
+    with pytest.raises(B.A2SFError):
+        B.a2sf_rms_norm(x, w, 1e-5, out=torch.empty_like(x))
+    with pytest.raises(B.A2SFError):
+        B.a2sf_rotary_table(torch.empty(8, 64))
+    out = torch.empty(4, dtype=torch.int32, pin_memory=True)
+    B.a2sf_sample(logits, None, out, top_k=k.pin_memory())
+    torch.cuda.synchronize()
+    assert torch.equal(out, logits.argmax(1).int().cpu())

@@ -212,3 +212,31 @@ def test_calls_of_more_lanes_than_a_launch_takes_are_refused():
     assert L.a2sf_sample(rows(stride=far), None, 2 ** 22, 100, B.A2SF_F32, None, None, None, None, FAKE, None, None) == B.A2SF_ESHAPE
     made = (B.RotaryPart * 1)(part(xs=(far, far, 512), ys=(far, far, 512), heads=64))
     assert L.a2sf_rotary(made, 1, 2 ** 24, 4, 512, B.A2SF_F32, FAKE, 4, FAKE, 32, 64, 0, 0, None) == B.A2SF_ESHAPE
+
+
+def test_tensors_of_another_device_are_refused():
+    """Not handed on as addresses; here "meta" stands for the other device."""
+    x = torch.zeros(4, 200, dtype=torch.bfloat16)
+    q, s = torch.zeros(4, 208, dtype=torch.uint8)[:, :200], torch.zeros(4, 4, dtype=torch.uint8)[:, :2]
+    w, b, bs = torch.ones(200, dtype=torch.bfloat16), torch.zeros(9, 208, dtype=torch.uint8)[:, :200], torch.zeros(1, 4, dtype=torch.uint8)[:, :2]
+    c, ws = torch.zeros(4, 9), torch.zeros(64, dtype=torch.uint8)
+    h, pos, table = torch.zeros(2, 3, 4, 64), torch.zeros(2, 3, dtype=torch.int32), torch.zeros(9, 64)
+    logits, token, k, f = torch.zeros(4, 50), torch.zeros(4, dtype=torch.int32), torch.ones(4, dtype=torch.int32), torch.ones(4)
+
+    def away(t):  # the same sizes and strides elsewhere
+        return torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device="meta")
+
+    calls = [(B.a2sf_rms_norm, (x, w, 1e-5), dict(residual=x, total=x, out=x, q=q, scales=s)), (B.a2sf_quantize, (x, q, s), dict(gate=x, out=x)),
+             (B.a2sf_quantize_weight, (x, q, torch.zeros(1, 4, dtype=torch.uint8)[:, :2]), {}), (B.a2sf_matmul_scaled, (q, s, b, bs, c), dict(workspace=ws)),
+             (lambda y, pos, table, v: B.a2sf_rotary([(h, y), (v, v, False)], pos, table), (h, pos, table, h), {}),
+             (B.a2sf_sample, (logits, logits, token), dict(temperature=f, top_k=k, top_p=f, min_p=f, prob=f))]
+    for call, args, named in calls:
+        for i, t in enumerate(args):
+            if isinstance(t, torch.Tensor):
+                with pytest.raises(B.A2SFError) as e:
+                    call(*args[:i], away(t), *args[i + 1:], **named)
+                assert e.value.status == B.A2SF_EINVAL, (call, i)
+        for name, t in named.items():
+            with pytest.raises(B.A2SFError) as e:
+                call(*args, **{**named, name: away(t)})
+            assert e.value.status == B.A2SF_EINVAL, (call, name)
