@@ -424,6 +424,11 @@ def _need(ok, status=A2SF_ESHAPE):
         raise A2SFError(status)
 
 
+def _int32(*sizes):
+    """The C arguments are of 32 bits, and ctypes would cut larger ones off."""
+    _need(max(sizes) <= 0x7FFFFFFF)
+
+
 def _reach(x, like):
     """x is memory that the GPU of `like` can read: its own, or pinned memory of the host."""
     if x.device != like.device:
@@ -476,6 +481,7 @@ def a2sf_rms_norm(x, weight, eps, residual=None, total=None, out=None, q=None, s
         return _check(status)
     _need(x.dim() == 2)
     rows, n = x.shape
+    _int32(rows, n)
     _check(lib().a2sf_rms_norm(_rows(x, x), _rows(residual, x), _column(weight, n, x.dtype, x), eps, rows, n, dtype_code(x.dtype),
                                _rows(total, x), _rows(out, x), _rows8(q, scales, rows, n, x), _stream_of(x, stream)))
 
@@ -487,6 +493,7 @@ def a2sf_quantize(x, q, scales, gate=None, out=None, stream=None):
         return _check(status)
     _need(x.dim() == 2)
     rows, n = x.shape
+    _int32(rows, n)
     _check(lib().a2sf_quantize(_rows(x, x), _rows(gate, x), rows, n, dtype_code(x.dtype), _rows(out, x),
                                _rows8(q, scales, rows, n, x), _stream_of(x, stream)))
 
@@ -494,12 +501,13 @@ def a2sf_quantize(x, q, scales, gate=None, out=None, stream=None):
 def a2sf_quantize_weight(w, q, scales, stream=None):
     _need(w.dim() == 2)
     n, k = w.shape
+    _int32(n, k)
     _check(lib().a2sf_quantize_weight(_rows(w, w), n, k, dtype_code(w.dtype), _rows8(q, scales, n, k, w, -(-n // 128)),
                                       _stream_of(w, stream)))
 
 
 def a2sf_matmul_workspace_bytes(m, n, k) -> int:
-    return int(lib().a2sf_matmul_workspace_bytes(m, n, k))
+    return int(lib().a2sf_matmul_workspace_bytes(m, n, k)) if max(m, n, k) <= 0x7FFFFFFF else 0
 
 
 def a2sf_matmul_scaled(a, a_scales, b, b_scales, c, workspace=None, workspace_bytes=None, stream=None, wide_sums=False):
@@ -512,6 +520,7 @@ def a2sf_matmul_scaled(a, a_scales, b, b_scales, c, workspace=None, workspace_by
     m, k = a.shape
     n = b.shape[0]
     _need(tuple(c.shape) == (m, n))
+    _int32(m, n, k)
     if workspace_bytes is None:
         workspace_bytes = workspace.nbytes if workspace is not None else 0
     if isinstance(workspace, torch.Tensor):
@@ -539,6 +548,7 @@ def a2sf_rotary(parts, pos, table, interleaved=False, inverse=False, stream=None
         _need(x.dtype == first.dtype and y.dtype == first.dtype, A2SF_EDTYPE)
         _reach(x, first)
         _reach(y, first)
+        _int32(*x.shape)
         to.x, to.y, to.heads, to.rotate = x.data_ptr(), y.data_ptr(), x.shape[2], int(rotate[0]) if rotate else 1
         to.x_stride[:], to.y_stride[:] = x.stride()[:3], y.stride()[:3]
     _need(tuple(pos.shape) == (batch, length) and (pos.stride(1) == 1 or length == 1))
@@ -547,6 +557,7 @@ def a2sf_rotary(parts, pos, table, interleaved=False, inverse=False, stream=None
     _reach(pos, first)
     _reach(table, first)
     _need(table.shape[1] <= d)
+    _int32(table.shape[0])
     _check(lib().a2sf_rotary(made, len(parts), batch, length, d, dtype_code(first.dtype), pos.data_ptr(), pos.stride(0),
                              table.data_ptr(), table.shape[0], table.shape[1], int(bool(interleaved)), int(bool(inverse)),
                              _stream_of(first, stream)))
@@ -555,6 +566,7 @@ def a2sf_rotary(parts, pos, table, interleaved=False, inverse=False, stream=None
 def a2sf_rotary_table(table, base=10000.0, factor=1.0, original_length=0, low=0.0, high=0.0, magnitude=1.0, stream=None):
     _need(table.dim() == 2 and table.is_contiguous())
     _need(table.dtype == torch.float32, A2SF_EDTYPE)
+    _int32(*table.shape)
     _check(lib().a2sf_rotary_table(table.data_ptr(), table.shape[0], table.shape[1], base, factor, original_length, low,
                                    high, magnitude, _stream_of(table, stream)))
 
@@ -566,6 +578,7 @@ def a2sf_sample(logits, noise, token, temperature=None, top_k=None, top_p=None, 
         return _check(status)
     _need(logits.dim() == 2)
     rows, n = logits.shape
+    _int32(rows, n)
     f = torch.float32
     _check(lib().a2sf_sample(_rows(logits, logits), _rows(noise, logits, f), rows, n, dtype_code(logits.dtype),
                              _column(temperature, rows, f, logits), _column(top_k, rows, torch.int32, logits),

@@ -240,3 +240,20 @@ def test_tensors_of_another_device_are_refused():
             with pytest.raises(B.A2SFError) as e:
                 call(*args, **{**named, name: away(t)})
             assert e.value.status == B.A2SF_EINVAL, (call, name)
+
+
+def test_sizes_above_32_bits_are_refused():
+    """Rows repeated in place (no memory behind them): 2^32 + 1 of them are not 1."""
+    many = lambda n, dtype: torch.zeros(1, n, dtype=dtype).expand(2 ** 32 + 1, n)  # noqa: E731
+    x, q, s = many(128, torch.bfloat16), many(128, torch.uint8), many(1, torch.uint8)
+    h, pos = torch.zeros(1, 1, 1, 64).expand(2 ** 32 + 1, 1, 1, 64), torch.zeros(1, 1, dtype=torch.int32).expand(2 ** 32 + 1, 1)
+    for call in (lambda: B.a2sf_quantize(x, q, s), lambda: B.a2sf_rms_norm(x, x[0], 1e-5, out=x),
+                 lambda: B.a2sf_quantize_weight(x, q, torch.zeros(1, 1, dtype=torch.uint8).expand(2 ** 25 + 1, 1)),
+                 lambda: B.a2sf_matmul_scaled(q, s, q[:1], s[:1], torch.zeros(1, 1).expand(2 ** 32 + 1, 1)),
+                 lambda: B.a2sf_rotary([(h, h)], pos, torch.zeros(4, 64)),
+                 lambda: B.a2sf_rotary_table(torch.zeros(1, 0).expand(2 ** 32 + 1, 0)),
+                 lambda: B.a2sf_sample(x, None, torch.zeros(1, dtype=torch.int32).expand(2 ** 32 + 1))):
+        with pytest.raises(B.A2SFError) as e:
+            call()
+        assert e.value.status == B.A2SF_ESHAPE
+    assert B.a2sf_matmul_workspace_bytes(2 ** 32 + 100, 4096, 11008) == 0
