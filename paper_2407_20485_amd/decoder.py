@@ -158,7 +158,8 @@ class Decoder:
             B.a2sf_decode_step(m["q"], m["k"], m["v"], self.position, cache, self.alpha, *kept, m["o"], workspace=ws)
 
     def generate(self, prompt, steps, temperature=0.8, top_k=50, top_p=0.95, min_p=0.0, seed=0):
-        """`steps` tokens behind the prompts [batch, n]: [batch, steps] int32."""
+        """`steps` tokens behind the prompts [batch, n]: [batch, steps] int32.  A sequence with an infinity or a NaN in its activations has
+        no token to take: -1 from there on."""
         b = prompt.shape[0]
         gen = torch.Generator(device="cuda").manual_seed(seed)
         row = lambda v, t: torch.full((b,), v, dtype=t, device="cuda")  # noqa: E731
@@ -170,7 +171,7 @@ class Decoder:
         for i in range(steps):
             logits = self.forward(tokens)
             B.a2sf_sample(logits, noise.exponential_(generator=gen), out[i], **filters)
-            tokens = out[i].view(b, 1)
+            tokens = out[i].view(b, 1).clamp_min(0)
         return out.t()
 
 

@@ -76,3 +76,15 @@ def test_generation_under_a_budget_repeats():
     greedy = model.generate(prompt, 4, temperature=0.0)
     model.start(4, 0.5, 10, 10)
     assert torch.equal(greedy[:, 0], model.forward(prompt).argmax(1).int())
+
+
+def test_a_sequence_that_is_not_finite_gives_no_tokens_and_leaves_the_others():
+    model = D.Decoder(SMALL[0], positions=128)
+    prompt = torch.randint(10, 1003, (3, 50), device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    model.start(3, 0.5, 10, 10)
+    want = model.generate(prompt, 6, seed=4)
+    model.embedding[5] = math.inf
+    prompt[1, -1] = 5
+    model.start(3, 0.5, 10, 10)
+    got = model.generate(prompt, 6, seed=4)
+    assert bool((got[1] == -1).all()) and torch.equal(got[::2], want[::2])
