@@ -109,6 +109,8 @@ class Decoder:
         """tokens [batch, n] behind what the caches hold (n > 1 only as the prompt): logits [batch, vocabulary] of the last one."""
         c = self.config
         b, n = tokens.shape
+        if n > 1 and self.position > 0:
+            raise ValueError(f"{n} tokens behind {self.position} that are cached: a prompt goes into empty caches (start), then one token a call")
         m = self._memory(b * n, n)
         group = c.heads // c.kv_heads
         m["pos"].copy_(torch.arange(self.position, self.position + n, dtype=torch.int32, device="cuda").expand(b, n))

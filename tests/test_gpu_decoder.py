@@ -88,3 +88,15 @@ def test_a_sequence_that_is_not_finite_gives_no_tokens_and_leaves_the_others():
     model.start(3, 0.5, 10, 10)
     got = model.generate(prompt, 6, seed=4)
     assert bool((got[1] == -1).all()) and torch.equal(got[::2], want[::2])
+
+
+def test_a_prompt_goes_into_empty_caches_only():
+    model = D.Decoder(SMALL[1], positions=64)
+    tokens = torch.randint(0, 777, (2, 9), device="cuda")
+    model.start(2, 0.5, 10, 10)
+    first = model.forward(tokens).clone()
+    with pytest.raises(ValueError):
+        model.forward(tokens)
+    assert model.position == 9
+    model.start(2, 0.5, 10, 10)
+    assert torch.equal(model.forward(tokens), first)
