@@ -375,7 +375,8 @@ a2sf_status a2sf_quantize_weight(const a2sf_rows* w, int32_t n, int32_t k, int32
  *   a          [m, k] as a2sf_rms_norm and a2sf_quantize write them.
  *   b          [n, k] as a2sf_quantize_weight writes them.
  *   c          out [m, n], c_dtype (A2SF_F32 or A2SF_BF16).
- *   c_dtype    A2SF_F32, and A2SF_BF16 | A2SF_WIDE_SUMS: sums in 32 bits (within k * 2^-24 * sum |a b|).  A2SF_BF16 alone: by the 8-bit matrix
+ *   c_dtype    A2SF_F32, and A2SF_BF16 | A2SF_WIDE_SUMS: sums in 32 bits (within k * 2^-24 * sum |a b|, for scale bytes of 10 to 246: values are
+ *              taken as bf16, whose subnormal numbers have fewer bits than those of smaller scales, and whose range ends before larger ones).  A2SF_BF16 alone: by the 8-bit matrix
  *              instruction, at about twice the rate where the rate counts; it cuts each of eight neighbouring products of k under 2^-13
  *              of the largest of them, so a sum is within 8 * 2^-13 * sum |a b| of the exact one before it is rounded to bf16 (for data
  *              like a model's 1.5e-5 of the result's size; a sum that cancels may lose all of it).

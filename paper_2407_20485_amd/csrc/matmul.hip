@@ -8,8 +8,8 @@
 //    fp32: the sum is off by 8 * 2^-13 of the sum of magnitudes at most, for Gaussian data by 1.5e-5 of the result's size, a hundred times less than
 //    the rounding to bf16 (2^-9 on the average).  The 8-bit values themselves are roundings of 2^-4, so what is cut is under 2^-8 of what the largest of
 //    the eight products may be off; but for data that 8 bits hold exactly a sum that cancels keeps only 13 bits under its largest term.
-//  * An fp32 C, where that cut would be the largest error by far, and a bf16 C with A2SF_WIDE_SUMS: the 8-bit values are made bf16 (which holds them,
-//    times a power of two, exactly) and multiplied by v_mfma_f32_16x16x32_bf16 or 32x32x16, whose sums are fp32's, at half the rate.
+//  * An fp32 C, where that cut would be the largest error by far, and a bf16 C with A2SF_WIDE_SUMS: the 8-bit values are made bf16 (which holds them
+//    times their scale exactly for scale bytes of 10 to 246: from 2^-9 of the smallest scale, its last normal bit, to 448 of the largest) and multiplied by v_mfma_f32_16x16x32_bf16 or 32x32x16, whose sums are fp32's, at half the rate.
 //
 // In both the instruction's first operand is B, its second A: its result then has, per lane, four neighbouring columns of C of the
 // row lane % 16.  An operand fragment is 16 rows x 128 bytes, 32 bytes per lane, of row lane % 16; which of the 128 they are is the same

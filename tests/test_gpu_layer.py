@@ -441,6 +441,19 @@ def test_matmul_wide_sums_keep_what_cancels(m):
     assert bool((c == 14 * 2.0 ** -6).all())
 
 
+@pytest.mark.parametrize("m,n,k", [(3, 100, 256), (40, 4200, 384), (200, 300, 1000), (2100, 600, 640)])
+@pytest.mark.parametrize("of_a,of_b", [((10, 13), (220, 240)), ((241, 247), (10, 14)), ((10, 14), (241, 247)), ((60, 80), (120, 180))])
+def test_matmul_in_32_bits_at_the_ends_of_the_scales(m, n, k, of_a, of_b):
+    """All 8-bit values under scale bytes from 10 to 246."""
+    g = rng(28, m, of_a[0])
+    (a, sa), (b, sb) = operands(g, m, n, k, False)
+    sa, sb = (g.integers(*r, size=s.shape).astype(np.uint8) for r, s in ((of_a, sa), (of_b, sb)))
+    c = torch.empty(m, n, device="cuda")
+    B.a2sf_matmul_scaled(*filled(m, k, a, sa, 0), *filled(n, k, b, sb, 0), c)
+    va, vb = torch.from_numpy(L.values(a, sa)).cuda(), torch.from_numpy(L.values(b, sb, 128)).cuda().t()
+    assert bool(((c.double() - va @ vb).abs() <= max(k, 16) * 2.0 ** -24 * (va.abs() @ vb.abs())).all())
+
+
 @pytest.mark.parametrize("m,n,k,parts", [(300, 1000, 11008, 4), (500, 2048, 8192, 2)])
 def test_matmul_takes_a_workspace_that_its_own_parts_fit(m, n, k, parts):
     """32-bit sums would be split in more parts than the 8-bit instruction's: a workspace for the fewer is enough for those."""
