@@ -772,6 +772,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
   f.p = a.top_p ? a.top_p[r] : 1.f;
   f.min_p = a.min_p ? a.min_p[r] : 0.f;
   f.min_p = f.min_p > 0.f ? f.min_p : 0.f;  // (not a number: no filter)
+  if (f.min_p > 1.f) f = {a.n > 1 ? 1 : 0, 1.f, 0.f};  // (nothing but the first, not even what equals it)
   if (greedy) f = {0, 1.f, 0.f};
 
   // The largest logit; and the smallest of the largest ones of `groups` groups of lanes: so many tokens at least are not below

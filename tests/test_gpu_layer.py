@@ -798,6 +798,17 @@ def test_sample_long_rows_with_nan(live, nans, values, dtype):
     check_tokens(logits, noise, min_p=[0.5, 1e-40, 0.01, 0.1, 1.0, 1e-9, 0.3], temperature=[math.inf, 1.0, 100.0, 0.01, 1e-30, math.inf, 1.0])
 
 
+@pytest.mark.parametrize("n", [1, 2, 700, 9000])
+def test_sample_min_p_above_one_leaves_the_first_alone(n):
+    """Equal logits too stand behind it."""
+    g = rng(29, n)
+    l = np.where(g.random((5, n)) < 0.3, 2.0, g.normal(size=(5, n)) - 3)
+    l[:, n // 2] = 2.0
+    noise = on_gpu(g.exponential(size=(5, n)) + 1e-9, torch.float32)
+    check_tokens(on_gpu(l, torch.bfloat16), noise, min_p=[1.5, 2.0, 1.0, 3e38, math.inf])
+    check_tokens(on_gpu(l, torch.float32), noise, min_p=[1.5, 2.0, 1.0, 1e10, math.inf], top_p=[0.9] * 5, top_k=[0, 5, 3, 600, 1])
+
+
 def test_sample_without_prob_and_with_numbers_that_are_zero():
     logits = torch.zeros(1, 10, device="cuda")
     noise = torch.ones(1, 10, device="cuda")
