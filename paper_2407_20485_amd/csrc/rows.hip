@@ -1,5 +1,7 @@
 // Row operators of a decoder layer: residual sum with root-mean-square norm, and conversion to 8-bit rows (of rows, of
 // silu(gate) * rows, of weights).  All read and write each element once and are bound by memory.
+#include <type_traits>
+
 #include "a2sf_internal.h"
 #include "rows_dev.h"
 
@@ -66,31 +68,37 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void rms_norm_kernel
     for (int j = 0; j < kUnit; ++j) s = fmaf(h[i][j], h[i][j], s);
     sum += s;
   }
-  const auto row_sum = [&](double v) {
+  const auto row_sum = [&](double v, auto once_more) {
     v = wave_sum_f64(v);
     if constexpr (THREADS > 64) {
       __shared__ double part[THREADS / 64];
       if ((t & 63) == 0) part[t >> 6] = v;
       __syncthreads();
       v = 0.0;
+      if constexpr (once_more) {
+#pragma unroll 1
+        for (int w = 0; w < THREADS / 64; ++w) v += part[w];
+      } else {
 #pragma unroll
-      for (int w = 0; w < THREADS / 64; ++w) v += part[w];
+        for (int w = 0; w < THREADS / 64; ++w) v += part[w];
+      }
     }
     return v;
   };
-  double mean = row_sum(sum) / a.n + a.eps;
+  double mean = row_sum(sum, std::false_type()) / a.n + a.eps;
   T* total = a.total ? (T*)a.total + row * a.total_stride : nullptr;
   double by = 1.0;  // what h was multiplied with
   if (!(mean < 0x1p128) || mean < 0x1p-100) {
     // Squares above the range of 32 bits, or so many under its normal numbers that their sum counts (the whole row sees the same mean): again in
-    // 64 bits, and h by a power of two into the middle of the range, where the factor is a normal number too.
+    // 64 bits, and h by a power of two into the middle of the range, where the factor is a normal number too.  (The parts one by one: the
+    // registers for all at once would cost every row a wave in eight: 7000 x 10000 bf16 107 us, so 99.)
     sum = 0.0;
 #pragma unroll
     for (int i = 0; i < V; ++i)
 #pragma unroll
       for (int j = 0; j < kUnit; ++j) sum += (double)h[i][j] * h[i][j];
     if constexpr (THREADS > 64) __syncthreads();  // (the first sum's parts are read)
-    mean = row_sum(sum) / a.n + a.eps;
+    mean = row_sum(sum, std::true_type()) / a.n + a.eps;
     by = mean < 1.0 ? 0x1p100 : 0x1p-64;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
