@@ -154,7 +154,8 @@ __device__ __forceinline__ void store_bytes(T* p, int have, u32x4_t v) {
 // row, ask for 16 bytes at a time of 64 places: 48 x 4096 x 11008 33 us, so 12.5; 1 x 4096 x 11008 10.5, so 8.7.
 // Where rows of B lie a multiple of 4096 bytes apart, workgroups that all began at the same place of k would all ask the same few of the
 // caches' channels: each begins at another one (1 x 12288 x 4096 straight into registers 12.8 us, so 10.3).
-// 1 x 12288 x 4096 9.0 us = 5.6 TB/s; 1 x 8192 x 8192 11.4 = 5.9; 32 x 12288 x 4096 10.4 = 4.9; 48 x 4096 x 11008 12.5 = 3.7.
+// 1 x 12288 x 4096 9.2 us = 5.5 TB/s; 1 x 8192 x 8192 11.4 = 5.9; 32 x 12288 x 4096 10.2 = 4.9; 48 x 4096 x 11008 12.5 = 3.7 (weights that the last-level cache
+// holds; from memory 1 x 12288 x 4096 11.2, 48 x 4096 x 11008 17.8).
 template <int MT, int WAVES, int ROOM>
 struct StripLds {
   static constexpr int kPart = WAVES * MT * 1024;
@@ -294,9 +295,9 @@ __global__ __launch_bounds__(WAVES * 64) void matmul_strip_kernel(MatmulArgs g) 
 //
 // Eight waves: the two of a SIMD are half an iteration apart, with a barrier at each half: while one has the matrix pipe, the other
 // reads the fragments of its next half block and fetches.  (8192 x 8192 x 8192: all waves in step 490 us, so 461; with a group's half blocks
-// written out, which takes the questions about the end of the stream out of them, 440 = 2500 TFLOP/s, the chip at its power
-// limit.)  Four waves: the next half block's fragments are read while this one's are multiplied, and workgroups share a
-// compute unit.
+// written out, which takes the questions about the end of the stream out of them, 440 = 2500 TFLOP/s.  8192 x 22016 x 4096 662 us: matrix pipe busy 54 %
+// of the cycles, at 1.96 of 2.4 GHz, which its operands leave; on zeros 2.395 GHz and 599 us.)  Four waves: the next half block's
+// fragments are read while this one's are multiplied, and workgroups share a compute unit.
 //
 // A row of a stage is 64 bytes, four chunks of 16; chunk c of row r lies at c ^ (r / 4 % 4): 16 lanes that read the same chunk of 16
 // rows then meet all 64 banks once.  The scales of four blocks of the tile's rows come the same way, a group ahead.  Results go through
@@ -666,7 +667,7 @@ void tile_form(const MatmulArgs& g, TilePlan plan, hipStream_t st) {
 // ---- which form ------------------------------------------------------------------------------------------------------------------
 // Up to 16 rows: strips.  Else the form that a model of its time says is the fastest.  A tile's time is its half blocks' times what an
 // iteration takes, from measurements (k = 4096, us an iteration; few compute units at work / all / each of two or three workgroups on one):
-//   256 x 256  0.57 / 0.84 (power)   128 x 128  0.26 / 0.30 / 0.34   64 x 128  0.175 / 0.21 / 0.25   64 x 64  0.147 / 0.17 (rate of L2)
+//   256 x 256  0.57 / 0.84 (at a lower clock)   128 x 128  0.26 / 0.30 / 0.34   64 x 128  0.175 / 0.21 / 0.25   64 x 64  0.147 / 0.17 (rate of L2)
 //   fp32: 128 x 128  0.30 / 0.44 / 0.44   64 x 128  0.26 / 0.30 / 0.30
 // but no less than B takes from memory (5.2 TB/s).  A tile's start and end cost 1.6 to 3.4 us; parts of k cost a second launch and the traffic of the
 // parts; strips take 0.36, 0.38 or 0.62 us for a step of each of a compute unit's four waves, with up to 32, 48 and 64 rows (more rows:

