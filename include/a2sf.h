@@ -59,7 +59,7 @@ typedef enum {
   A2SF_EHIP = 6        /* the HIP runtime reported an error at launch */
 } a2sf_status;
 
-typedef enum { A2SF_F32 = 0, A2SF_BF16 = 1 } a2sf_dtype;
+typedef enum { A2SF_F32 = 0, A2SF_BF16 = 1, A2SF_E4M3 = 2 /* pages only */ } a2sf_dtype;
 
 /* How a generation step makes the cache dense again after an eviction. */
 typedef enum {
@@ -443,6 +443,93 @@ a2sf_status a2sf_rotary_table(float* table, int32_t table_rows, int32_t rotary_d
 a2sf_status a2sf_sample(const a2sf_rows* logits, const a2sf_rows* noise, int32_t rows, int32_t n, int32_t dtype,
                         const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                         int32_t* token, float* prob, void* hip_stream);
+
+/* ---- Keys and values in pages -----------------------------------------------------------------------------------------
+ * A cache that keeps every token (or, under a window, the newest and a few first ones) of sequences of different lengths that come and
+ * go: the baseline without eviction, and the local one.  Keys and values lie in pages of page_size tokens; a table says which
+ * page holds a sequence's tokens 0 .. page_size - 1, page_size .. 2 page_size - 1, and so on.  The conventions of the operators around
+ * the attention hold. */
+typedef struct {
+  void* k;                    /* page p, head h, token t of the page: d elements from p * stride[0] + h * stride[1] + t * stride[2] on */
+  void* v;                    /* laid out as k */
+  uint8_t* k_scales;          /* A2SF_E4M3: the scale of each token and head, a byte at p * scale_stride[0] + h * scale_stride[1] + t * */
+  uint8_t* v_scales;          /*            scale_stride[2], as for a2sf_rows8.  Other types: NULL */
+  int64_t stride[3];          /* elements; rows start at multiples of 16 bytes */
+  int64_t scale_stride[3];    /* bytes */
+  int32_t pages;
+  int32_t page_size;          /* tokens, a power of two, at most 65536 */
+  int32_t kv_heads;
+  int32_t d;                  /* 64 or 128 */
+  int32_t dtype;              /* that of the call's tensors, or A2SF_E4M3 */
+} a2sf_pages;
+
+/* Which sequences a call is about, and which of its tokens are theirs. */
+typedef struct {
+  const int32_t* table;       /* [sequences, table_pages]: pages; an entry that no token of the call needs may be anything (-1) */
+  const int32_t* len;         /* [sequences]: tokens of each sequence, the call's new ones among them */
+  const int32_t* starts;      /* [sequences + 1]: sequence s has the call's tokens starts[s] .. starts[s + 1] - 1, its newest ones, in
+                                 order.  NULL: token s is the newest of sequence s, and a sequence of length 0 is a place without one */
+  int64_t table_stride;       /* entries from row to row */
+  int32_t sequences;
+  int32_t table_pages;
+} a2sf_sequences;
+
+typedef struct {
+  void* data;                 /* [tokens, heads, d]; a head's elements are next to each other */
+  int64_t stride[2];          /* elements from token to token, head to head */
+} a2sf_heads;
+
+/* A sequence is bad if its length is negative or more than table_pages * page_size, or if it has a negative number of new tokens or more
+ * of them than tokens.  Starts do not fall and lie in 0 .. the call's tokens; where two of them do, their sequence is bad, and rows of others
+ * may be left alone.  Tokens of the call that no sequence has are left alone: nothing is written for them. */
+
+/* New tokens: their keys and values go to their sequences' pages, k and q turned by their positions (a token's place in its sequence) on
+ * the way, as a2sf_rotary turns them.
+ *   q, q_out    [tokens, heads, d] dtype, both or neither; q_out may be q with the same strides.
+ *   k, v        [tokens, cache->kv_heads, d] dtype.  What turning gives is rounded once, to the pages' type.
+ *   dtype       A2SF_F32 or A2SF_BF16.
+ *   table       [table_rows, rotary_dims] fp32 as a2sf_rotary takes it; NULL: nothing is turned.  A token whose position is no row of
+ *               the table has NaN in the rotary_dims of q and k (pages of 8 bits: in all of k).
+ * A token of a bad sequence, or one whose page is none of the cache's, leaves the cache alone and has NaN for its row of q_out.
+ * starts NULL: a place without a sequence (length 0) leaves q_out as it is.  A page that two sequences share is not
+ * written by both in one call. */
+a2sf_status a2sf_paged_append(const a2sf_heads* q, const a2sf_heads* k, const a2sf_heads* v, int32_t tokens, int32_t heads,
+                              int32_t dtype, const a2sf_sequences* sequences, const a2sf_pages* cache, const float* table,
+                              int32_t table_rows, int32_t rotary_dims, int32_t pairs, const a2sf_heads* q_out,
+                              void* hip_stream);
+
+/* Attention of each sequence's newest tokens (already appended) over its pages: o_i = sum_j softmax_j(q_i . k_j / sqrt(d)) v_j over the
+ * tokens j that token i sees: j <= i, and j > i - window or j < sinks (the window counts the token itself).
+ *   q          [tokens, heads, d] dtype, heads a multiple of cache->kv_heads: query head h reads K/V head h / (heads / kv_heads).
+ *   window     >= 1; A2SF_NO_WINDOW: every earlier token.
+ *   sinks      >= 0: first tokens that stay visible.
+ *   o          out [tokens, heads, d] dtype.  NaN for a bad sequence, and for a token that sees one whose page is none of the cache's;
+ *              0 for a place without a sequence.  An infinity or NaN in a row of v reaches the tokens that see it alone, as one or the other.
+ *   workspace  may be NULL; with a2sf_paged_workspace_bytes() bytes calls of few rows split their tokens over more of the chip, with less into
+ *              fewer parts.  The same sizes with the same workspace give the same bits.
+ * Only pages with a token that some token of the call sees are looked up in the table and read. */
+#define A2SF_NO_WINDOW 0x7FFFFFFF
+a2sf_status a2sf_paged_attention(const a2sf_heads* q, int32_t tokens, int32_t heads, int32_t dtype, const a2sf_sequences* sequences,
+                                 const a2sf_pages* cache, int32_t window, int32_t sinks, const a2sf_heads* o, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream);
+/* The most that a call of these sizes makes use of, whatever its window (0: nothing, or the sizes are wrong).
+ *   table_tokens  table_pages * page_size. */
+size_t a2sf_paged_workspace_bytes(int32_t tokens, int32_t heads, int32_t kv_heads, int32_t d, int32_t sequences, int64_t table_tokens);
+
+/* What a row of logits says of given tokens, with y = logit - max, Z = sum exp(y): log p = y - log(Z), the entropy
+ * log(Z) - sum(exp(y) y) / Z, and the tokens of the largest logits (equal ones: the lower index first).
+ *   logits      [rows, n] dtype.  -infinity has probability 0.  A row with a NaN or +infinity, or of -infinity alone, has NaN for all
+ *               its values; among its alternatives a NaN counts as -infinity.
+ *   tokens      [rows, given] int32; NULL with given = 0.  A token outside 0 .. n - 1 has NaN.
+ *   logp        out [rows, given] fp32.
+ *   entropy     out [rows] fp32, may be NULL.
+ *   top         out [rows, alternatives] fp32: their log p, falling; may be NULL.
+ *   top_tokens  out [rows, alternatives] int32; may be NULL.
+ * n <= A2SF_MAX_VOCABULARY, alternatives <= n and <= A2SF_MAX_ALTERNATIVES, 0 without top and top_tokens. */
+#define A2SF_MAX_ALTERNATIVES 64
+a2sf_status a2sf_log_probs(const a2sf_rows* logits, int32_t rows, int32_t n, int32_t dtype, const a2sf_rows* tokens, int32_t given,
+                           const a2sf_rows* logp, float* entropy, const a2sf_rows* top, const a2sf_rows* top_tokens,
+                           int32_t alternatives, void* hip_stream);
 
 const char* a2sf_status_string(int32_t status);
 

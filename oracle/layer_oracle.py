@@ -127,3 +127,52 @@ def sample(logits, noise, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         if best is None or key > best[0] or (key == best[0] and order[i] < order[best[1]]):
             best = (key, i)
     return order[best[1]], w[best[1]] / sum(w[i] for i in keep)
+
+
+# ---- keys and values in pages, log probabilities ----
+
+def seen(past, new, window, sinks):
+    """[new, past + new]: whether the i-th new token, at position past + i, sees token j."""
+    m = np.zeros((new, past + new), bool)
+    for i in range(new):
+        p = past + i
+        for j in range(p + 1):
+            m[i, j] = j < sinks or p - j < window
+    return m
+
+
+def gather(pages, row, n):
+    """pages [pages, heads, page_size, d] -> the sequence's [heads, n, d]; row: its entries of the table."""
+    size = pages.shape[2]
+    return np.stack([pages[row[j // size], :, j % size] for j in range(n)], 1)
+
+
+def attend(q, k, v, mask):
+    """q [new, heads, d], k, v [kv_heads, n, d], mask [new, n]: (o, sum of p |v|, largest sum of |q k| / sqrt(d) that a row sees)."""
+    new, heads, d = q.shape
+    group = heads // k.shape[0]
+    o, size, reach = (np.zeros((new, heads, d)), np.zeros((new, heads, d)), np.zeros((new, heads, 1)))
+    for h in range(heads):
+        kh, vh = k[h // group], v[h // group]
+        for i in range(new):
+            at = mask[i]
+            s = kh[at] @ q[i, h] / math.sqrt(d)
+            with np.errstate(invalid="ignore"):
+                p = np.exp(s - s.max())
+                p /= p.sum()
+            o[i, h], size[i, h] = p @ vh[at], p @ np.abs(vh[at])
+            reach[i, h] = (np.abs(kh[at]) @ np.abs(q[i, h])).max() / math.sqrt(d)
+    return o, size, reach
+
+
+def log_probs(logits):
+    """(log p of every token, entropy, tokens by falling logit, equal ones by index) of one row."""
+    x = logits.astype(np.float64)
+    order = sorted(range(len(x)), key=lambda i: (math.inf if np.isnan(x[i]) else -x[i], i))
+    if np.isnan(x).any() or x.max() in (math.inf, -math.inf):
+        return np.full(len(x), math.nan), math.nan, order
+    y = x - x.max()
+    w = np.exp(y)
+    z = w.sum()
+    with np.errstate(invalid="ignore"):
+        return y - math.log(z), math.log(z) - np.where(w > 0, w * y, 0.0).sum() / z, order

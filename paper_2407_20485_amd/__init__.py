@@ -11,7 +11,9 @@ from .binding import (A2SF_BF16, A2SF_EVICT_FAST, A2SF_EVICT_STABLE, A2SF_F32, A
                       a2sf_prefill_gqa, a2sf_decode_step_gqa, a2sf_prefill_chunk_gqa,
                       A2SF_MAX_ROTARY_PARTS, A2SF_MAX_ROW, A2SF_MAX_VOCABULARY, A2SF_WIDE_SUMS, a2sf_matmul_scaled,
                       a2sf_matmul_workspace_bytes, a2sf_quantize, a2sf_quantize_weight, a2sf_rms_norm, a2sf_rotary,
-                      a2sf_rotary_table, a2sf_sample)
+                      a2sf_rotary_table, a2sf_sample,
+                      A2SF_E4M3, A2SF_MAX_ALTERNATIVES, A2SF_NO_WINDOW, Pages, a2sf_log_probs, a2sf_paged_append,
+                      a2sf_paged_attention, a2sf_paged_workspace_bytes)
 
 __all__ = ["A2SF_BF16", "A2SF_F32", "A2SF_EVICT_FAST", "A2SF_EVICT_STABLE", "A2SF_MAX_CAPACITY",
            "A2SFError", "Cache", "a2sf_compact", "a2sf_decode_step", "a2sf_prefill", "a2sf_select",
@@ -21,4 +23,5 @@ __all__ = ["A2SF_BF16", "A2SF_F32", "A2SF_EVICT_FAST", "A2SF_EVICT_STABLE", "A2S
            "a2sf_prefill_gqa", "a2sf_decode_step_gqa", "a2sf_prefill_chunk_gqa",
            "A2SF_MAX_ROTARY_PARTS", "A2SF_MAX_ROW", "A2SF_MAX_VOCABULARY", "A2SF_WIDE_SUMS", "a2sf_matmul_scaled",
            "a2sf_matmul_workspace_bytes", "a2sf_quantize", "a2sf_quantize_weight", "a2sf_rms_norm", "a2sf_rotary",
-           "a2sf_rotary_table", "a2sf_sample"]
+           "a2sf_rotary_table", "a2sf_sample", "A2SF_E4M3", "A2SF_MAX_ALTERNATIVES", "A2SF_NO_WINDOW", "Pages", "a2sf_log_probs",
+           "a2sf_paged_append", "a2sf_paged_attention", "a2sf_paged_workspace_bytes"]

@@ -20,12 +20,13 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liba2sf.so")
 
 A2SF_OK, A2SF_EINVAL, A2SF_ESHAPE, A2SF_EDTYPE, A2SF_ECAPACITY, A2SF_EWORKSPACE, A2SF_EHIP = range(7)
-A2SF_F32, A2SF_BF16 = 0, 1
+A2SF_F32, A2SF_BF16, A2SF_E4M3 = 0, 1, 2
 A2SF_EVICT_FAST, A2SF_EVICT_STABLE = 0, 1
 A2SF_MAX_CAPACITY = 36864
 A2SF_STATIC_WS_BYTES = 16 << 20
 A2SF_MAX_ROW, A2SF_MAX_VOCABULARY, A2SF_MAX_ROTARY_PARTS = 65536, 4194304, 4
 A2SF_WIDE_SUMS = 0x100
+A2SF_NO_WINDOW, A2SF_MAX_ALTERNATIVES = 0x7FFFFFFF, 64
 
 EXPORTS = ("a2sf_workspace_bytes", "a2sf_prefill", "a2sf_decode_step", "a2sf_select",
            "a2sf_compact", "a2sf_status_string", "a2sf_prefill_alpha_per_head",
@@ -33,7 +34,8 @@ EXPORTS = ("a2sf_workspace_bytes", "a2sf_prefill", "a2sf_decode_step", "a2sf_sel
            "a2sf_similarity_mean", "a2sf_decode_plan", "a2sf_prefill_windowed",
            "a2sf_prefill_chunk", "a2sf_prefill_gqa", "a2sf_decode_step_gqa", "a2sf_prefill_chunk_gqa",
            "a2sf_rms_norm", "a2sf_quantize", "a2sf_quantize_weight", "a2sf_matmul_workspace_bytes", "a2sf_matmul_scaled",
-           "a2sf_rotary", "a2sf_rotary_table", "a2sf_sample")
+           "a2sf_rotary", "a2sf_rotary_table", "a2sf_sample",
+           "a2sf_paged_append", "a2sf_paged_attention", "a2sf_paged_workspace_bytes", "a2sf_log_probs")
 
 
 class Budget(ctypes.Structure):
@@ -58,6 +60,21 @@ class Rows8(ctypes.Structure):
 class RotaryPart(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_stride", ctypes.c_int64 * 3),
                 ("y_stride", ctypes.c_int64 * 3), ("heads", ctypes.c_int32), ("rotate", ctypes.c_int32)]
+
+
+class PagesStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("stride", ctypes.c_int64 * 3), ("scale_stride", ctypes.c_int64 * 3), ("pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class Sequences(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("len", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("sequences", ctypes.c_int32), ("table_pages", ctypes.c_int32)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64 * 2)]
 
 
 _lib = None
@@ -135,6 +152,15 @@ def lib() -> ctypes.CDLL:
         L.a2sf_rotary_table.argtypes = [vp, i32, i32, f64, f64, i32, f64, f64, f64, vp]
         L.a2sf_sample.restype = i32
         L.a2sf_sample.argtypes = [rows, rows, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        heads, pages, seqs = ctypes.POINTER(Heads), ctypes.POINTER(PagesStruct), ctypes.POINTER(Sequences)
+        L.a2sf_paged_append.restype = i32
+        L.a2sf_paged_append.argtypes = [heads, heads, heads, i32, i32, i32, seqs, pages, vp, i32, i32, i32, heads, vp]
+        L.a2sf_paged_attention.restype = i32
+        L.a2sf_paged_attention.argtypes = [heads, i32, i32, i32, seqs, pages, i32, i32, heads, vp, sz, vp]
+        L.a2sf_paged_workspace_bytes.restype = sz
+        L.a2sf_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int64]
+        L.a2sf_log_probs.restype = i32
+        L.a2sf_log_probs.argtypes = [rows, i32, i32, i32, rows, i32, rows, vp, rows, rows, i32, vp]
         L.a2sf_status_string.restype = ctypes.c_char_p
         L.a2sf_status_string.argtypes = [i32]
         if _call is None:
@@ -209,6 +235,9 @@ def _check(status: int):
 _DTYPE_CODES = {torch.float32: A2SF_F32, torch.bfloat16: A2SF_BF16}
 
 
+_PAGE_CODES = {**_DTYPE_CODES, torch.float8_e4m3fn: A2SF_E4M3}
+
+
 def dtype_code(t: torch.dtype) -> int:
     code = _DTYPE_CODES.get(t)
     if code is None:
@@ -241,6 +270,47 @@ class Cache:
     def restore(self, snap):
         for t, s in zip(self.tensors(), snap):
             t.copy_(s)
+
+
+class Pages:
+    """Device buffers of a paged KV cache: k, v [pages, kv_heads, page_size, d], and for 8 bits (torch.float8_e4m3fn) the bytes of
+    their scales [pages, kv_heads, page_size]."""
+
+    def __init__(self, pages: int, page_size: int, kv_heads: int, d: int, dtype: torch.dtype, device="cuda"):
+        shape, eight = (pages, kv_heads, page_size, d), dtype == torch.float8_e4m3fn
+        k, v = (torch.zeros(shape, dtype=dtype, device=device) for _ in range(2))
+        ks, vs = (torch.zeros(shape[:3], dtype=torch.uint8, device=device) if eight else None for _ in range(2))
+        self._take(k, v, ks, vs)
+
+    @classmethod
+    def of(cls, k, v, k_scales=None, v_scales=None) -> "Pages":
+        """Pages in tensors that are there already: views of any strides with a row's elements next to each other, k and v alike."""
+        self = cls.__new__(cls)
+        self._take(k, v, k_scales, v_scales)
+        return self
+
+    def _take(self, k, v, k_scales, v_scales):
+        _need(k.dim() == 4 and v.shape == k.shape and v.stride() == k.stride() and k.stride(3) == 1)
+        _need(k.dtype in _PAGE_CODES and v.dtype == k.dtype, A2SF_EDTYPE)
+        _need((k.dtype == torch.float8_e4m3fn) == (k_scales is not None) == (v_scales is not None), A2SF_EINVAL)
+        _reach(v, k)
+        scale_stride = (0, 0, 0)
+        if k_scales is not None:
+            _need(k_scales.shape == k.shape[:3] and v_scales.shape == k.shape[:3] and k_scales.stride() == v_scales.stride())
+            _need(k_scales.dtype == torch.uint8 and v_scales.dtype == torch.uint8, A2SF_EDTYPE)
+            _reach(k_scales, k)
+            _reach(v_scales, k)
+            scale_stride = k_scales.stride()
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.pages, self.kv_heads, self.page_size, self.d = k.shape
+        _int32(*k.shape)
+        self.dtype = k.dtype
+        three = ctypes.c_int64 * 3
+        self.struct = PagesStruct(k.data_ptr(), v.data_ptr(), _ptr(k_scales), _ptr(v_scales), three(*k.stride()[:3]), three(*scale_stride),
+                                  self.pages, self.page_size, self.kv_heads, self.d, _PAGE_CODES[k.dtype])
+
+    def tensors(self):
+        return tuple(t for t in (self.k, self.v, self.k_scales, self.v_scales) if t is not None)
 
 
 def _cache_struct(cache):
@@ -585,3 +655,95 @@ def a2sf_sample(logits, noise, token, temperature=None, top_k=None, top_p=None, 
                              _column(top_p, rows, f, logits), _column(min_p, rows, f, logits),
                              _column(token, rows, torch.int32, logits), _column(prob, rows, f, logits),
                              _stream_of(logits, stream)))
+
+
+# ---- keys and values in pages ----
+
+def _heads(x, like, heads=None):
+    """The C struct of [tokens, heads, d]; `like`: the tensor whose tokens, d and type it has to have."""
+    _reach(x, like)
+    _need(x.dim() == 3 and x.shape[0] == like.shape[0] and x.shape[2] == like.shape[2] and (heads is None or x.shape[1] == heads))
+    _need(x.stride(2) == 1 or x.shape[2] == 1)
+    _need(x.dtype == like.dtype, A2SF_EDTYPE)
+    return Heads(x.data_ptr(), (ctypes.c_int64 * 2)(x.stride(0), x.stride(1)))
+
+
+def _sequences(table, lens, starts, like):
+    """... of table [sequences, table_pages], lens [sequences] and starts [sequences + 1] (or None), all int32."""
+    _need(table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1))
+    _need(table.dtype == torch.int32, A2SF_EDTYPE)
+    _reach(table, like)
+    n = table.shape[0]
+    _int32(*table.shape)
+    return Sequences(table.data_ptr(), _column(lens, n, torch.int32, like), _column(starts, n + 1, torch.int32, like), table.stride(0), n,
+                     table.shape[1])
+
+
+def a2sf_paged_append(q, k, v, cache, table, lens, starts=None, q_out=None, rotary=None, interleaved=False, stream=None):
+    """q [tokens, heads, d] (with q_out; both may be None), k, v [tokens, kv_heads, d] into the pages of `cache` (Pages); table, lens and
+    starts as in a2sf_sequences; rotary: the table [rows, rotary_dims] of a2sf_rotary_table, None: nothing is turned."""
+    _need(k.dim() == 3 and k.shape[2] == cache.d)
+    _need((q is None) == (q_out is None), A2SF_EINVAL)
+    _reach(cache.k, k)
+    tokens, heads = k.shape[0], 0 if q is None else q.shape[1]
+    _int32(tokens, heads)
+    rows = dims = 0
+    if rotary is not None:
+        _need(rotary.dim() == 2 and rotary.is_contiguous())
+        _need(rotary.dtype == torch.float32, A2SF_EDTYPE)
+        _reach(rotary, k)
+        rows, dims = rotary.shape
+        _int32(rows, dims)
+    _check(lib().a2sf_paged_append(None if q is None else _heads(q, k), _heads(k, k, cache.kv_heads), _heads(v, k, cache.kv_heads), tokens,
+                                   heads, dtype_code(k.dtype), _sequences(table, lens, starts, k), ctypes.byref(cache.struct),
+                                   _ptr(rotary), rows, dims, int(bool(interleaved)), None if q is None else _heads(q_out, k, heads),
+                                   _stream_of(k, stream)))
+
+
+def a2sf_paged_attention(q, cache, table, lens, o, starts=None, window=None, sinks=0, workspace=None, workspace_bytes=None, stream=None):
+    """window: tokens that a token sees, itself among them (None: all)."""
+    _need(q.dim() == 3 and q.shape[2] == cache.d)
+    _reach(cache.k, q)
+    tokens, heads = q.shape[:2]
+    window = A2SF_NO_WINDOW if window is None else window
+    _int32(tokens, heads, window, sinks)
+    if workspace_bytes is None:
+        workspace_bytes = workspace.nbytes if workspace is not None else 0
+    if isinstance(workspace, torch.Tensor):
+        _reach(workspace, q)
+    _check(lib().a2sf_paged_attention(_heads(q, q), tokens, heads, dtype_code(q.dtype), _sequences(table, lens, starts, q),
+                                      ctypes.byref(cache.struct), window, sinks, _heads(o, q, heads), _ptr(workspace), workspace_bytes,
+                                      _stream_of(q, stream)))
+
+
+def a2sf_paged_workspace_bytes(tokens, heads, kv_heads, d, sequences, table_tokens) -> int:
+    if max(tokens, heads, kv_heads, d, sequences) > 0x7FFFFFFF:
+        return 0
+    return int(lib().a2sf_paged_workspace_bytes(tokens, heads, kv_heads, d, sequences, table_tokens))
+
+
+def _rows_of(x, rows, dtype, like):
+    """The C struct of [rows, any] and its columns (None, 0 of None)."""
+    if x is None:
+        return None, 0
+    _reach(x, like)
+    _need(x.dim() == 2 and x.shape[0] == rows and (x.stride(1) == 1 or x.shape[1] == 1))
+    _need(x.dtype == dtype, A2SF_EDTYPE)
+    _int32(x.shape[1])
+    return Rows(x.data_ptr(), x.stride(0)), x.shape[1]
+
+
+def a2sf_log_probs(logits, tokens=None, logp=None, entropy=None, top=None, top_tokens=None, stream=None):
+    """tokens [rows, given] int32 with logp [rows, given], entropy [rows], top [rows, alternatives] and top_tokens int32: all but the
+    logits may be None."""
+    _need(logits.dim() == 2)
+    rows, n = logits.shape
+    _int32(rows, n)
+    f = torch.float32
+    t, given = _rows_of(tokens, rows, torch.int32, logits)
+    l, values = _rows_of(logp, rows, f, logits)
+    a, alternatives = _rows_of(top, rows, f, logits)
+    i, indices = _rows_of(top_tokens, rows, torch.int32, logits)
+    _need(given == values and (top is None or top_tokens is None or alternatives == indices))
+    _check(lib().a2sf_log_probs(_rows(logits, logits), rows, n, dtype_code(logits.dtype), t, given, l, _column(entropy, rows, f, logits),
+                                a, i, max(alternatives, indices), _stream_of(logits, stream)))

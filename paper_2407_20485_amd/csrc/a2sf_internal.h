@@ -213,4 +213,52 @@ struct SampleArgs {
 };
 bool launch_sample(const SampleArgs& a, int dtype, hipStream_t st);
 
+// logprobs.hip
+struct LogProbsArgs {
+  const void* logits;
+  const int32_t* tokens;
+  float *logp, *entropy, *top;
+  int32_t* top_tokens;
+  long long stride, token_stride, logp_stride, top_stride, top_token_stride;
+  int rows, n, given, alternatives;
+};
+bool launch_log_probs(const LogProbsArgs& a, int dtype, hipStream_t st);
+
+// ---- keys and values in pages ----------------------------------------------------------------------------------------------
+// The cache and the sequences of a call as the kernels take them: strides in bytes, page_size = 2^shift.
+struct PagedCache {
+  char *k, *v;
+  uint8_t *k_scales, *v_scales;
+  long long stride[3], scale_stride[3];
+  const int32_t *table, *len, *starts;
+  long long table_stride;
+  int sequences, table_pages, pages, shift, kv_heads, d, dtype;
+  int tokens;  // of the call
+};
+// paged_append.hip
+struct AppendArgs {
+  PagedCache c;
+  const void *q, *k, *v;
+  void* q_out;
+  long long q_stride[2], k_stride[2], v_stride[2], q_out_stride[2];
+  const float* table;
+  int heads, table_rows, rot;
+  int per_lane, groups;  // set by the launcher
+};
+bool launch_paged_append(AppendArgs a, int dtype, bool neighbours, hipStream_t st);
+// paged_attention.hip
+struct PagedArgs {
+  PagedCache c;
+  const void* q;
+  void* o;
+  long long q_stride[2], o_stride[2];
+  int heads, group, window, sinks;
+  float scale_log2e;
+  // set by the launcher
+  float *part, *part_ml;  // [rows][splits][d], [rows][splits][2]: a row is a (token, head)
+  int splits, blocks;
+};
+size_t paged_workspace(int tokens, int heads, int kv_heads, int d, int sequences, long long table_tokens);
+bool launch_paged_attention(PagedArgs a, int dtype, void* workspace, size_t workspace_bytes, hipStream_t st);
+
 }  // namespace a2sf

@@ -1,0 +1,709 @@
+"""Keys and values in pages and log probabilities on the GPU against the float64 oracle.
+
+Tolerances, from the arithmetic (u = 2^-24 is fp32's unit of rounding):
+  * a logit of d products in fp32 is within (d + 4) u of the sum of their magnitudes / sqrt(d), `reach`; the exponential of it to
+    base 2 takes its argument with two more roundings (of at most `reach` and the maximum) and is within 2 u itself: a probability is
+    within e = (d + 8) u reach + 4 u of its value, and so is each in the sum that it is divided by;
+  * sums over tokens: matrix instructions of up to 32 tokens each, one after the other, then waves and shares: a term goes through
+    fewer than n / 16 + 128 additions;
+  * so a result is within (2 e + 2 (n / 16 + 128) u) sum p |v| of its value; where probabilities go into the product as bf16 numbers
+    2^-17 more for two of them, 2^-8 for one; then 2^-8 of itself where it is rounded to bf16;
+  * keys and values: a pair turns in two products and a sum, 3 u of |x0| + |x1|, and is rounded once;
+  * log probabilities: y of one rounding, its exponential within (|y| + 4) u, |y| < 104; sums of up to n terms in 1024 lanes:
+    (n / 1024 + 24) u; the logarithm 2 u of its value and what its argument's error comes to.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_oracle as L
+from paper_2407_20485_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+U = 2.0 ** -24
+EIGHT = torch.float8_e4m3fn
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def values(t, scales):
+    """What a cache's rows stand for."""
+    if scales is None:
+        return host(t)
+    s = scales.cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        return L.E4M3[t.view(torch.uint8).cpu().numpy()] * np.where(s == 255, math.nan, 2.0 ** (s.astype(float) - 127))[..., None]
+
+
+class Batch:
+    """Sequences of (past, new) tokens over pages in no order.  Rows of pages that no token fills, and entries of the table behind a
+    sequence's pages, are rubbish: NaN and numbers that are no page."""
+
+    def __init__(self, seed, lengths, kv, d, page, dtype, eight=False, one_each=False, spare=3, extra=2, layout="heads"):
+        self.g = np.random.default_rng([11, seed])
+        self.lengths, self.kv, self.d, self.page, self.dt = lengths, kv, d, page, DT[dtype]
+        need = [-(-(p + n) // page) for p, n in lengths]
+        pages = sum(need) + spare
+        order = self.g.permutation(pages)
+        width = max(1, max(need))
+        self.rows, at = [], 0
+        table = np.full((len(lengths), width + extra), -7, np.int32)
+        for i, k in enumerate(need):
+            table[i, :k] = order[at: at + k]
+            table[i, k:] = self.g.choice([-1, pages, 2 ** 30, -2 ** 31], size=width + extra - k)
+            at += k
+        self.host_table = table
+        self.table = torch.from_numpy(table).cuda()[:, :width]
+        self.len = torch.tensor([p + n for p, n in lengths], dtype=torch.int32).cuda()
+        starts = np.concatenate([[0], np.cumsum([n for _, n in lengths])])
+        self.tokens = int(starts[-1]) if not one_each else len(lengths)
+        self.starts = None if one_each else torch.tensor(starts, dtype=torch.int32).cuda()
+        self.first = starts
+        kind = EIGHT if eight else self.dt
+        shape = (pages, kv, page, d)
+
+        def buffer(shape, dtype):
+            if layout == "heads":
+                return torch.empty(shape, dtype=dtype, device="cuda")
+            # a token's heads next to each other, and k and v of a page
+            return torch.empty((shape[0], 2, shape[2], shape[1]) + tuple(shape[3:]), dtype=dtype, device="cuda")[:, 0].transpose(1, 2)
+        self.k, self.v = buffer(shape, kind), buffer(shape, kind)
+        self.ks, self.vs = (buffer(shape[:3], torch.uint8) for _ in range(2)) if eight else (None, None)
+        self.cache = B.Pages.of(self.k, self.v, self.ks, self.vs)
+        self.rubbish()
+
+    def rubbish(self):
+        for t in (self.k, self.v):
+            if t.dtype == EIGHT:
+                t.view(torch.uint8).fill_(0x7F)
+            else:
+                t.fill_(math.nan)
+        for t in (self.ks, self.vs):
+            if t is not None:
+                t.fill_(255)
+
+    def slots(self):
+        """(page, place) of all tokens of all sequences."""
+        at = [(self.host_table[i, j // self.page], j % self.page) for i, (p, n) in enumerate(self.lengths) for j in range(p + n)]
+        return tuple(torch.tensor(x, dtype=torch.long, device="cuda") for x in zip(*at))
+
+    def fill(self, scale=1.0):
+        page, place = self.slots()
+        for t, s in ((self.k, self.ks), (self.v, self.vs)):
+            x = torch.from_numpy(self.g.normal(size=(len(page), self.kv, self.d)) * scale).cuda().float()
+            if s is None:
+                t[page, :, place] = x.to(t.dtype)
+            else:
+                q, b = L.quantize(host(x).reshape(-1, self.d)) if self.d == 128 else L.quantize(host(x).reshape(-1, self.d))
+                t.view(torch.uint8)[page, :, place] = torch.from_numpy(q).cuda().view(-1, self.kv, self.d)
+                s[page, :, place] = torch.from_numpy(b).cuda().view(-1, self.kv)
+        return self
+
+    def rows_of(self, i):
+        p, n = self.lengths[i]
+        return [L.gather(x, self.host_table[i], p + n) for x in self.seen_values]
+
+    def attention(self, q, window, sinks):
+        """Per sequence (o, sum of p |v|, reach)."""
+        self.seen_values = values(self.k, self.ks), values(self.v, self.vs)
+        for i, (p, n) in enumerate(self.lengths):
+            if p + n == 0 or n == 0:
+                yield i, None
+                continue
+            k, v = self.rows_of(i)
+            at = int(self.first[i]) if self.starts is not None else i
+            yield i, (at, n) + L.attend(host(q[at: at + n]), k, v, L.seen(p, n, window, sinks))
+
+
+def strided(tokens, heads, d, dtype, g, scale=1.0):
+    """Heads in the middle of wider rows that start at no multiple of 16 bytes."""
+    store = torch.full((tokens * (heads * d + 9) + 64,), 7.0, dtype=dtype, device="cuda")
+    x = torch.as_strided(store, (tokens, heads, d), (heads * d + 9, d, 1), 3)
+    x.copy_(torch.from_numpy(g.normal(size=(tokens, heads, d)) * scale))
+    return x, store
+
+
+def check_attention(b, q, o, window, sinks, one_product=False):
+    half = HALF["bf16" if q.dtype == torch.bfloat16 else "f32"]
+    lost = 0.0 if q.dtype == torch.float32 else 2.0 ** -8 if one_product else 2.0 ** -17
+    for i, want in b.attention(q, window, sinks):
+        if want is None:
+            continue
+        at, n, w, size, reach = want
+        count = sum(b.lengths[i])
+        e = (b.d + 8) * U * reach + 4 * U
+        slack = (2 * e + 2 * (count / 16 + 128) * U + lost) * size
+        off = np.abs(host(o[at: at + n]) - w)
+        assert (off <= half * np.abs(w) + slack * (1 + half)).all(), (i, b.lengths[i], float((off - half * np.abs(w) - slack).max()))
+
+
+def attend(b, heads, window=None, sinks=0, workspace="enough", scale=2.0, q=None, seed=1, one_product=False):
+    g = np.random.default_rng([12, seed])
+    if q is None:
+        q, _ = strided(b.tokens, heads, b.d, b.dt, g, scale)
+    o, store = strided(b.tokens, heads, b.d, b.dt, g)
+    before = store.clone()
+    n = B.a2sf_paged_workspace_bytes(b.tokens, heads, b.kv, b.d, len(b.lengths), b.table.shape[1] * b.page)
+    ws = None if workspace is None else torch.full((n + 16 if workspace == "enough" else n // 3 // 16 * 16,), 0xFF, dtype=torch.uint8, device="cuda")
+    B.a2sf_paged_attention(q, b.cache, b.table, b.len, o, starts=b.starts, window=window, sinks=sinks, workspace=ws,
+                           workspace_bytes=None if workspace != "enough" else n)
+    if workspace == "enough":
+        assert bool((ws[n:] == 0xFF).all())
+    check_attention(b, q, o, window or 1 << 30, sinks, one_product)
+    # nothing around the rows is written
+    inside = torch.zeros_like(store, dtype=torch.bool)
+    torch.as_strided(inside, o.shape, o.stride(), 3).fill_(True)
+    assert torch.equal(before[~inside].float(), store[~inside].float())
+    return q, o
+
+
+KINDS = [("bf16", False), ("f32", False), ("bf16", True), ("f32", True)]
+STEP = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 255, 257, 400, 1000]
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kv,group,page", [(1, 1, 1), (2, 4, 16), (3, 8, 64), (2, 7, 32), (1, 16, 128), (2, 17, 8), (1, 40, 256)])
+def test_single_tokens(dtype, eight, d, kv, group, page):
+    """Lengths around the tiles' edges, a place without a sequence among them, groups of up to 40 heads."""
+    b = Batch(1, [(n - 1, 1) if n else (0, 0) for n in STEP], kv, d, page, dtype, eight, one_each=True).fill()
+    _, o = attend(b, kv * group)
+    assert bool((o[0] == 0).all())
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+@pytest.mark.parametrize("workspace", ["enough", "less", None])
+def test_single_tokens_of_a_long_sequence(dtype, eight, workspace):
+    b = Batch(2, [(7000, 1), (299, 1)], 1, 128, 64, dtype, eight, one_each=True).fill()
+    q, o = attend(b, 4, workspace=workspace)
+    _, again = attend(b, 4, workspace=workspace, q=q)
+    assert torch.equal(o, again)
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 5), (2, 1), (33, 0), (64, 4), (100, 70), (128, 1), (400, 2), (5000, 4)])
+def test_single_tokens_under_a_window(dtype, eight, window, sinks):
+    """Pages that nothing sees any more are handed back: their entries are no pages."""
+    b = Batch(3, [(n - 1, 1) for n in (1, 2, 64, 100, 101, 170, 171, 399, 700)], 2, 128, 16, dtype, eight, one_each=True).fill()
+    table = b.table.clone()
+    for i, (p, _) in enumerate(b.lengths):
+        for k in range(table.shape[1]):
+            if k * 16 >= sinks and k * 16 + 15 <= p - window:
+                table[i, k] = 1 << 28
+    b.table = table
+    attend(b, 8, window, sinks)
+
+
+RAGGED = [[(0, 1)], [(0, 5), (3, 1), (0, 0), (9, 2)], [(0, 100)], [(50, 33), (0, 17), (200, 64)], [(300, 1), (10, 1), (0, 1)],
+          [(0, 129), (129, 129), (1000, 3)], [(0, 260)], [(0, 0), (40, 0), (5, 7)]]
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+@pytest.mark.parametrize("lengths", RAGGED)
+@pytest.mark.parametrize("kv,group,d,page", [(2, 4, 128, 16), (1, 1, 64, 32), (2, 3, 64, 1), (1, 20, 128, 64)])
+def test_ragged_tokens(dtype, eight, lengths, kv, group, d, page):
+    b = Batch(4, lengths, kv, d, page, dtype, eight).fill()
+    attend(b, kv * group, one_product=True)
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 3), (7, 2), (64, 0), (100, 4), (130, 90), (1000, 1)])
+def test_ragged_tokens_under_a_window(dtype, eight, window, sinks):
+    b = Batch(5, [(0, 200), (333, 70), (500, 1), (90, 150)], 2, 128, 16, dtype, eight).fill()
+    table = b.table.clone()
+    for i, (p, _) in enumerate(b.lengths):
+        for k in range(table.shape[1]):
+            if k * 16 >= sinks and k * 16 + 15 <= p - window:
+                table[i, k] = -1
+    b.table = table
+    attend(b, 8, window, sinks, one_product=True)
+
+
+@pytest.mark.parametrize("dtype,eight", [("bf16", False), ("f32", True)])
+@pytest.mark.parametrize("one_each", [True, False])
+def test_pages_of_another_layout(dtype, eight, one_each):
+    """A token's heads next to each other, k and v of a page in one tensor."""
+    lengths = [(n - 1, 1) for n in (1, 40, 333)] if one_each else [(0, 40), (100, 90)]
+    b = Batch(6, lengths, 3, 128, 16, dtype, eight, one_each=one_each, layout="tokens").fill()
+    attend(b, 6, one_product=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("one_each", [True, False])
+def test_large_logits(dtype, one_each):
+    """Logits of some thousands, and rows whose logits are all very negative: the maximum moves."""
+    b = Batch(7, [(400, 1), (70, 1)] if one_each else [(100, 40), (0, 150)], 1, 128, 16, dtype, one_each=one_each).fill(scale=30.0)
+    q, _ = strided(b.tokens, 4, 128, b.dt, b.g, 30.0)
+    attend(b, 4, q=q, one_product=True)
+    page, place = b.slots()
+    b.k[page, :, place] = (-b.k[page, :, place].abs())
+    q.copy_(q.abs())
+    attend(b, 4, q=q, one_product=True)
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+@pytest.mark.parametrize("one_each", [True, False])
+def test_bad_sequences_and_pages(dtype, eight, one_each):
+    """Lengths that do not fit the table, pages that are none of the cache's: NaN for what is concerned, the others as before."""
+    lengths = [(20, 1), (300, 1), (64, 1), (100, 1), (9, 1)] if one_each else [(20, 9), (300, 5), (64, 30), (100, 130), (9, 20)]
+    b = Batch(8, lengths, 2, 64, 16, dtype, eight, one_each=one_each).fill()
+    q, o = attend(b, 4, one_product=True)
+    keep_len, keep_table = b.len.clone(), b.table.clone()
+    at = [slice(i, i + 1) if one_each else slice(int(b.first[i]), int(b.first[i + 1])) for i in range(5)]
+
+    def run():
+        ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+        got = torch.full_like(o, 5.0)
+        B.a2sf_paged_attention(q, b.cache, b.table, b.len, got, starts=b.starts, workspace=ws)
+        return got
+
+    good = run()
+    for bad in (-1, -2 ** 31, b.table.shape[1] * 16 + 1, 2 ** 31 - 1):
+        b.len = keep_len.clone()
+        b.len[1] = bad
+        got = run()
+        assert bool(torch.isnan(got[at[1]]).all())
+        for i in (0, 2, 3, 4):
+            assert torch.equal(got[at[i]], good[at[i]]), (bad, i)
+    b.len = keep_len
+    for bad in (-1, b.cache.pages, 2 ** 31 - 1, -2 ** 31):
+        b.table = keep_table.clone()
+        b.table[2, 3] = bad
+        got = run()
+        assert bool(torch.isnan(got[at[2]]).all())   # tokens 48 .. 63 are seen by all of them
+        for i in (0, 1, 3, 4):
+            assert torch.equal(got[at[i]], good[at[i]])
+    if not one_each:  # a page that only the later tokens see
+        b.table = keep_table.clone()
+        b.table[3, 12] = -1
+        got = run()
+        assert torch.equal(got[at[3]][:92], good[at[3]][:92]) and bool(torch.isnan(got[at[3]][92:]).all())
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+@pytest.mark.parametrize("window,sinks", [(None, 0), (20, 3)])
+def test_values_that_are_not_numbers_reach_who_sees_them(dtype, eight, window, sinks):
+    """An infinity or NaN in a row of v: the tokens before it, and those whose window has left it behind, come out as without it."""
+    b = Batch(10, [(0, 150), (200, 70)], 2, 128, 16, dtype, eight).fill()
+    q, _ = attend(b, 4, window, sinks, one_product=True)
+
+    def run():
+        got = torch.empty_like(q)
+        B.a2sf_paged_attention(q, b.cache, b.table, b.len, got, starts=b.starts, window=window, sinks=sinks,
+                               workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+        return got
+
+    o = run()
+    odd = {0: (5, 61, 62, 64, 100, 131, 149), 1: (150, 201, 230, 269)}
+    for i, tokens in odd.items():
+        for n, j in enumerate(tokens):
+            page, place = int(b.host_table[i, j // 16]), j % 16
+            if eight:
+                b.v.view(torch.uint8)[page, 1, place] = 0x7F
+                b.vs[page, 1, place] = 255
+            else:
+                b.v[page, 1, place, 3 + n] = math.nan if n % 2 else math.inf
+                b.v[page, 1, place, 100] = -math.inf
+    got = run()
+    assert torch.equal(got[:, :2], o[:, :2])                       # the other K/V head's
+    for i, (p, n) in enumerate(b.lengths):
+        mask = L.seen(p, n, window or 1 << 30, sinks)
+        for r in range(n):
+            t = int(b.first[i]) + r
+            reached = torch.zeros(128, dtype=torch.bool, device="cuda")
+            for m, j in enumerate(odd[i]):
+                if j <= p + r and mask[r, j]:
+                    reached[list(range(128)) if eight else [3 + m, 100]] = True
+            assert not bool(torch.isfinite(got[t, 2:][:, reached]).any()), (i, r)
+            assert torch.equal(got[t, 2:][:, ~reached], o[t, 2:][:, ~reached]), (i, r)
+
+
+def test_starts_that_make_no_sense():
+    """Whatever the starts hold, nothing is written outside the rows, and tokens that no sequence has are left alone."""
+    b = Batch(9, [(20, 9), (300, 5), (64, 30), (10, 40)], 2, 64, 16, "bf16").fill()
+    q, o = attend(b, 4, one_product=True)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    B.a2sf_paged_attention(q, b.cache, b.table, b.len, o, starts=b.starts, workspace=ws)
+    for starts in ([0, 9, 14, 44, 2 ** 31 - 1], [-2 ** 31, 9, 14, 44, 84], [0, 9, 14, 8, 5], [0, 0, 0, 0, 0], [84, 84, 84, 84, 84],
+                   [5, 9, 14, 44, 60], [90, 91, 92, 93, 94]):
+        got, store = strided(84, 4, 64, torch.bfloat16, np.random.default_rng(1))
+        before = store.clone()
+        s = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        B.a2sf_paged_attention(q, b.cache, b.table, b.len, got, starts=s, workspace=ws)
+        inside = torch.zeros_like(store, dtype=torch.bool)
+        torch.as_strided(inside, got.shape, got.stride(), 3).fill_(True)
+        assert torch.equal(before[~inside].float(), store[~inside].float())
+        if starts[1:4] == [9, 14, 44]:        # (where starts fall, rows of other sequences may be left alone)
+            assert torch.equal(got[9:14], o[9:14])
+        if starts[0] == 5:  # tokens that no sequence has
+            was = torch.as_strided(before, got.shape, got.stride(), 3)
+            assert torch.equal(got[:5], was[:5]) and torch.equal(got[60:], was[60:])
+
+
+def test_long_offsets():
+    """Pages further than 2^32 bytes into the cache."""
+    k = torch.empty(5, 2, 65536, 128 * 32, dtype=torch.bfloat16, device="cuda")[..., :128]   # 5.4 GB, rows 8 KB apart
+    v = torch.empty(5, 2, 65536, 128 * 32, dtype=torch.bfloat16, device="cuda")[..., :128]
+    cache = B.Pages.of(k, v)
+    g = torch.Generator("cuda").manual_seed(3)
+    n = 65536 + 300
+    for t in (k, v):
+        t[4] = torch.randn(2, 65536, 128, device="cuda", generator=g).bfloat16()
+        t[3, :, :300] = torch.randn(2, 300, 128, device="cuda", generator=g).bfloat16()
+    q = torch.randn(1, 4, 128, device="cuda", generator=g).bfloat16()
+    table = torch.tensor([[4, 3]], dtype=torch.int32, device="cuda")
+    o = torch.empty_like(q)
+    B.a2sf_paged_attention(q, cache, table, torch.tensor([n], dtype=torch.int32, device="cuda"), o,
+                           workspace=torch.empty(8 << 20, dtype=torch.uint8, device="cuda"))
+    kk, vv = (torch.cat([t[4], t[3, :, :300]], 1).double() for t in (k, v))
+    s = torch.matmul(kk, q[0].double().view(2, 2, 128).transpose(1, 2).contiguous()) / math.sqrt(128)
+    p = torch.softmax(s, 1)
+    want = torch.matmul(p.transpose(1, 2).contiguous(), vv).reshape(1, 4, 128)
+    # 65836 terms: 4243 additions, of probabilities that add up to 1 and values of 0.8 on the average
+    assert bool(((o.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2 * 4243 * U + 2.0 ** -16).all())
+
+
+# ---- new keys and values -----------------------------------------------------------------------------------------------------------
+
+def check_append(b, x, heads, rot, neighbours, table, q_out):
+    """The cache and q_out hold what the oracle says, and the cache nothing else."""
+    k0, v0 = values(b.k, b.ks), values(b.v, b.vs)
+    fresh = np.zeros(k0.shape[:1] + k0.shape[2:3], bool)
+    half = HALF["bf16" if b.dt == torch.bfloat16 else "f32"]
+    for i, (p, n) in enumerate(b.lengths):
+        at = int(b.first[i]) if b.starts is not None else i
+        for j in range(n):
+            row = host(x[at + j]).reshape(-1, b.d)
+            q, k, v = row[:heads], row[heads: heads + b.kv], row[heads + b.kv:]
+            page, place = b.host_table[i, (p + j) // b.page], (p + j) % b.page
+            fresh[page, place] = True
+            slack = np.zeros((heads + b.kv, b.d))
+            if rot:
+                cs = host(table[p + j])
+                cos, sin = cs[: rot // 2], cs[rot // 2:]
+                both = L.rotate(np.concatenate([q, k]), cos, sin, rot, neighbours, False)
+                slack = 3 * U * L.rotate(np.abs(np.concatenate([q, k])), np.abs(cos), -np.abs(sin), rot, neighbours, False)
+                first = np.arange(rot // 2) * (2 if neighbours else 1)
+                second = first + (1 if neighbours else rot // 2)
+                slack[:, second] = 3 * U * (np.abs(np.concatenate([q, k]))[:, second] * np.abs(cos) + np.abs(np.concatenate([q, k]))[:, first] * np.abs(sin))
+                slack[:, rot:] = 0
+                q, k = both[:heads], both[heads:]
+            if heads:
+                assert (np.abs(host(q_out[at + j]) - q) <= half * np.abs(q) + 2 * slack[:heads]).all()
+            for got, s, want, e in ((k0, b.ks, k, slack[heads:]), (v0, b.vs, v, np.zeros_like(v))):
+                off = np.abs(got[page, :, place] - want)
+                if s is None:
+                    assert (off <= half * np.abs(want) + 2 * e).all()
+                else:
+                    byte = s[page, :, place].cpu().numpy().astype(float)
+                    unit, top = 2.0 ** (byte - 127)[:, None], np.abs(want).max(1, keepdims=True)
+                    assert (top <= 448 * unit + e.max()).all() and ((top >= 224 * unit - e.max()) | (byte[:, None] == 0)).all()
+                    assert (off <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * unit) + 2 * e).all()
+    assert np.isnan(k0.transpose(0, 2, 1, 3)[~fresh]).all() and np.isnan(v0.transpose(0, 2, 1, 3)[~fresh]).all()
+
+
+def new_rows(b, heads, seed=5):
+    """Rows of a QKV product whose heads start at no multiple of 16 bytes."""
+    g = np.random.default_rng([13, seed])
+    n = (heads + 2 * b.kv) * b.d
+    store = torch.zeros(b.tokens * (n + 5) + 32, dtype=b.dt, device="cuda")
+    x = torch.as_strided(store, (b.tokens, n), (n + 5, 1), 1)
+    x.copy_(torch.from_numpy(g.normal(size=(b.tokens, n))))
+    return x, x.unflatten(1, (-1, b.d)).split([heads, b.kv, b.kv], 1)
+
+
+def cos_sin(rows, rot):
+    t = torch.empty(rows, rot, device="cuda")
+    B.a2sf_rotary_table(t)
+    return t
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+@pytest.mark.parametrize("neighbours", [False, True])
+@pytest.mark.parametrize("d,rot", [(64, 64), (128, 128), (128, 32), (64, 22), (128, 100), (64, 2), (128, 0)])
+@pytest.mark.parametrize("lengths,heads,kv,page", [([(0, 1), (15, 1), (16, 1), (0, 0), (300, 1)], 6, 2, 16), ([(0, 40), (17, 3), (0, 0), (99, 1)], 5, 1, 1),
+                                                   ([(0, 300), (77, 220)], 0, 3, 32)])
+def test_append(dtype, eight, neighbours, d, rot, lengths, heads, kv, page):
+    one_each = len(lengths) == 5
+    b = Batch(20, lengths, kv, d, page, dtype, eight, one_each=one_each)
+    x, (q, k, v) = new_rows(b, heads)
+    table = cos_sin(400, rot) if rot else None
+    out, store = strided(b.tokens, heads, d, b.dt, b.g) if heads else (None, None)
+    before = store.clone() if heads else None
+    B.a2sf_paged_append(q if heads else None, k, v, b.cache, b.table, b.len, starts=b.starts, q_out=out, rotary=table, interleaved=neighbours)
+    check_append(b, x, heads, rot, neighbours, table, out)
+    if heads:
+        inside = torch.zeros_like(store, dtype=torch.bool)
+        torch.as_strided(inside, out.shape, out.stride(), 3).fill_(True)
+        assert torch.equal(before[~inside].float(), store[~inside].float())
+        if one_each:  # a place without a sequence
+            assert torch.equal(out[3], torch.as_strided(before, out.shape, out.stride(), 3)[3])
+        # q in its own place
+        B.a2sf_paged_append(q, k, v, b.cache, b.table, b.len, starts=b.starts, q_out=q, rotary=table, interleaved=neighbours)
+        live = [i for i in range(b.tokens) if not (one_each and i == 3)]
+        assert torch.equal(q[live], out[live])
+
+
+@pytest.mark.parametrize("dtype,eight", [("bf16", False), ("f32", True)])
+def test_append_many(dtype, eight):
+    """More rows than a launch's workgroups take one head each."""
+    b = Batch(21, [(p, 90 + p) for p in range(12)], 4, 128, 16, dtype, eight, layout="tokens")
+    x, (q, k, v) = new_rows(b, 9)
+    out = torch.empty(b.tokens, 9, 128, dtype=b.dt, device="cuda")
+    table = cos_sin(200, 128)
+    B.a2sf_paged_append(q, k, v, b.cache, b.table, b.len, starts=b.starts, q_out=out, rotary=table)
+    check_append(b, x, 9, 128, False, table, out)
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+def test_append_of_tokens_without_a_place(dtype, eight):
+    """Bad lengths and pages leave the cache alone and have NaN for their q; positions behind the table are NaN where they would turn."""
+    b = Batch(22, [(0, 20), (30, 9), (5, 3), (60, 8)], 2, 64, 16, dtype, eight)
+    x, (q, k, v) = new_rows(b, 3)
+    out = torch.full((b.tokens, 3, 64), 5.0, dtype=b.dt, device="cuda")
+    good = torch.empty_like(out)
+    table = cos_sin(66, 32)
+    B.a2sf_paged_append(q, k, v, b.cache, b.table, b.len, starts=b.starts, q_out=good, rotary=table)
+    kept = [t.clone() for t in b.cache.tensors()]
+    assert bool(torch.isnan(good[38:, :, :32]).all()) and bool(torch.isfinite(good[38:, :, 32:]).all()) and bool(torch.isfinite(good[:38]).all())
+    page, place = int(b.host_table[3, 4]), 3
+    late = values(b.k, b.ks)[page, :, place]
+    assert np.isnan(late[:, :32]).all() and (np.isnan(late[:, 32:]).all() if eight else np.isfinite(late[:, 32:]).all())
+    b.rubbish()
+    rubbish = [t.clone() for t in b.cache.tensors()]
+    lens, tab = b.len.clone(), b.table.clone()
+    lens[0], lens[2] = -3, 10 ** 9
+    tab[1, 2], tab[3, 4] = -1, b.cache.pages
+    B.a2sf_paged_append(q, k, v, b.cache, tab, lens, starts=b.starts, q_out=out, rotary=table)
+    assert bool(torch.isnan(out[:20]).all()) and bool(torch.isnan(out[29:32]).all())
+    assert torch.equal(out[20:22], good[20:22]) and bool(torch.isnan(out[22:29]).all())       # positions 30, 31 | 32 ..
+    assert torch.equal(out[32:36], good[32:36]) and bool(torch.isnan(out[36:]).all())         # 60 .. 63 | 64 ..
+    for t, r, w in zip(b.cache.tensors(), rubbish, kept):
+        t, r, w = (y.view(torch.uint8) if y.dtype == EIGHT else y for y in (t, r, w))
+        same = lambda a, c: torch.equal(torch.nan_to_num(a.float(), nan=1e30), torch.nan_to_num(c.float(), nan=1e30))  # noqa: E731
+        for i, j in ((1, 1), (3, 3)):
+            p = int(b.host_table[i, j])
+            assert same(t[p], w[p])
+        others = [p for p in range(b.cache.pages) if p not in (int(b.host_table[1, 1]), int(b.host_table[3, 3]))]
+        assert same(t[others], r[others])
+
+
+# ---- log probabilities --------------------------------------------------------------------------------------------------------------
+
+LARGEST = float(np.finfo(np.float32).max) * (1 + 2.0 ** -25)
+
+
+def check_log_probs(x, tokens, logp, entropy, top, ids):
+    rows, n = x.shape
+    for i in range(rows):
+        want, h, order = L.log_probs(host(x[i]))
+        l = host(x[i])
+        if ids is not None:
+            assert ids[i].tolist() == order[: ids.shape[1]], i
+        if math.isnan(h):
+            for t in (logp, entropy, top):
+                assert t is None or bool(torch.isnan(t[i]).all())
+            continue
+        reach = min(104.0, float(np.ptp(l[np.isfinite(l)])))
+        e = (2 * reach + n / 1024 + 40) * U       # of the logarithm of the sum
+        got = lambda t: host(t[i])  # noqa: E731
+        if logp is not None:
+            t = tokens[i].tolist()
+            for j, token in enumerate(t):
+                g = float(logp[i, j])
+                if not 0 <= token < n:
+                    assert math.isnan(g)
+                elif want[token] < -LARGEST:       # no number of 32 bits, nor is what rounds to one
+                    assert g == -math.inf
+                else:
+                    assert abs(g - want[token]) <= e + 2 * U * (abs(want[token]) + math.log(n)), (i, j)
+        if top is not None:
+            w = want[order[: top.shape[1]]]
+            w = np.where(w < -LARGEST, -math.inf, w)
+            g = got(top)
+            assert ((g == w) | (np.abs(g - w) <= e + 2 * U * (np.abs(np.where(np.isfinite(w), w, 0)) + math.log(n)))).all()
+        if entropy is not None:
+            assert abs(float(entropy[i]) - h) <= (e + 4 * U) * (1 + h + math.log(n))
+
+
+def log_probs(x, given=2, k=0, extra=(), seed=0):
+    rows, n = x.shape
+    g = np.random.default_rng([14, seed])
+    tokens = torch.from_numpy(g.integers(0, n, (rows, given)).astype(np.int32)).cuda() if given else None
+    for i, t in enumerate(extra):
+        tokens[i % rows, i % given] = t
+    new = lambda c, t=torch.float32: torch.full((rows, c + 2), 7, dtype=t, device="cuda")[:, :c]  # noqa: E731
+    logp = new(given) if given else None
+    top, ids = (new(k), new(k, torch.int32)) if k else (None, None)
+    entropy = torch.full((rows,), 7.0, device="cuda")
+    B.a2sf_log_probs(x, tokens, logp, entropy, top, ids)
+    for t, c in ((logp, given), (top, k), (ids, k)):
+        assert t is None or bool((t._base[:, c:] == 7).all())
+    check_log_probs(x, tokens, logp, entropy, top, ids)
+    return logp, entropy, top, ids
+
+
+SIZES = [1, 2, 3, 7, 8, 9, 63, 64, 65, 100, 511, 1000, 1023, 1024, 1025, 4096, 8191, 8192, 8193, 20000, 32003, 65537]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", SIZES)
+def test_log_probs(dtype, n):
+    g = np.random.default_rng([15, n])
+    rows = 5
+    store = torch.full((rows * (n + 3) + 40,), 90.0, dtype=DT[dtype], device="cuda")     # what lies between the rows would be the largest
+    x = torch.as_strided(store, (rows, n), (n + 3, 1), 1)
+    x.copy_(torch.from_numpy(g.normal(size=(rows, n)) * np.array([[0.1], [1], [3], [10], [30]])))
+    for k in sorted({0, 1, min(5, n), min(20, n), min(64, n)}):
+        log_probs(x, 1 + k % 3, k, extra=(-1, n, 2 ** 31 - 1) if k == 1 else ())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [70, 1500, 9000, 50272])
+def test_log_probs_of_rows_with_ties(dtype, n):
+    """Equal logits go by their index: rows of one value, of few, of rising and falling ones, of one large value."""
+    x = torch.empty(7, n, dtype=DT[dtype], device="cuda")
+    i = torch.arange(n, device="cuda")
+    x[0] = 1.5
+    x[1] = (i % 3).to(x.dtype)
+    x[2] = (i // 5).float().to(x.dtype)
+    x[3] = -(i // 5).float().to(x.dtype)
+    x[4] = -40.0
+    x[4, n // 2] = 40.0
+    x[5] = torch.where(i % 1024 < 3, 5.0, 0.0).to(x.dtype)      # all in a few lanes' places
+    x[6] = torch.where(i % 8 == 1, (i // 8).float() * 1e-3, -9.0).to(x.dtype)
+    for k in (1, 7, 33, 64):
+        log_probs(x, 1, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [5, 700, 40000])
+def test_log_probs_of_rows_that_are_not_numbers(dtype, n):
+    x = torch.randn(9, n, device="cuda", generator=torch.Generator("cuda").manual_seed(n)).to(DT[dtype])
+    inf = math.inf
+    x[0, 3] = math.nan
+    x[1, 2] = inf
+    x[2] = -inf
+    x[3, ::2] = -inf
+    x[4] = -inf
+    x[4, 4] = 2.0
+    x[5, 1:3] = inf
+    x[6] = math.nan
+    x[7] = 0.0
+    x[7, 0] = -0.0                                             # equal to 0
+    x[8, 0], x[8, 1:] = 3e38, -3e38
+    logp, entropy, top, ids = log_probs(x, 2, min(5, n), extra=(0, 0, 0, 0, 4))
+    assert float(entropy[4]) == 0.0 and float(top[4, 0]) == 0.0 and bool((top[4, 1:] == -inf).all())
+    assert bool(torch.isnan(entropy[[0, 1, 2, 5, 6]]).all())
+
+
+def test_log_probs_asks_for_parts():
+    x = torch.randn(300, 777, device="cuda")
+    t = torch.randint(0, 777, (300, 1), dtype=torch.int32, device="cuda")
+    both = log_probs(x, 1, 6)
+    entropy, top, ids, logp = torch.empty(300, device="cuda"), torch.empty(300, 6, device="cuda"), torch.empty(300, 6, dtype=torch.int32, device="cuda"), torch.empty(300, 1, device="cuda")
+    B.a2sf_log_probs(x, entropy=entropy)
+    B.a2sf_log_probs(x, top=top)
+    B.a2sf_log_probs(x, top_tokens=ids)
+    B.a2sf_log_probs(x, tokens=t, logp=logp)
+    assert torch.equal(entropy, both[1]) and torch.equal(top, both[2]) and torch.equal(ids, both[3])
+    check_log_probs(x, t, logp, None, None, None)
+
+
+# ---- together, on streams and in graphs ---------------------------------------------------------------------------------------------
+
+def serve(b, x, heads, table, ws, out, o):
+    q, k, v = x.unflatten(1, (-1, b.d)).split([heads, b.kv, b.kv], 1)
+    B.a2sf_paged_append(q, k, v, b.cache, b.table, b.len, starts=b.starts, q_out=out, rotary=table)
+    B.a2sf_paged_attention(out, b.cache, b.table, b.len, o, starts=b.starts, window=200, sinks=2, workspace=ws)
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+@pytest.mark.parametrize("one_each", [True, False])
+def test_append_and_attention_in_a_graph(dtype, eight, one_each):
+    """Captured once, replayed with other lengths, pages and rows in the same memory: each replay is the eager result."""
+    lengths = [(700, 1), (0, 0), (50, 1)] if one_each else [(0, 90), (300, 40)]
+    b = Batch(30, lengths, 2, 128, 16, dtype, eight, one_each=one_each, spare=60).fill()
+    g = torch.Generator("cuda").manual_seed(1)
+    table = cos_sin(1000, 128)
+    ws = torch.empty(B.a2sf_paged_workspace_bytes(b.tokens, 8, 2, 128, len(lengths), b.table.shape[1] * 16) + 16, dtype=torch.uint8, device="cuda")
+    x = torch.randn(b.tokens, 12 * 128, device="cuda", generator=g).to(b.dt)
+    new = lambda: torch.zeros(b.tokens, 8, 128, dtype=b.dt, device="cuda")  # noqa: E731
+    out, o = new(), new()
+    b.table = b.table.clone()
+    serve(b, x, 8, table, ws, out, o)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        serve(b, x, 8, table, ws, out, o)
+    for turn in range(4):
+        x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+        if turn:
+            b.len[0] -= 7 * turn if one_each else 0
+            b.table.copy_(b.table.roll(1, 1) if turn == 2 else b.table)
+        cache = [t.clone() for t in b.cache.tensors()]
+        o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, o, *b.cache.tensors())]
+        for t, c in zip(b.cache.tensors(), cache):
+            t.copy_(c)
+        out2, o2 = new(), new()
+        serve(b, x, 8, table, ws, out2, o2)
+        bits = lambda t: t.contiguous().view(torch.uint8)  # noqa: E731
+        for a, c in zip(got, (out2, o2, *b.cache.tensors())):
+            assert torch.equal(bits(a), bits(c)), turn
+
+
+def test_two_streams_with_workspaces_of_their_own():
+    b = Batch(31, [(5000, 1), (3000, 1)], 2, 128, 64, "bf16", one_each=True).fill()
+    q = torch.randn(2, 8, 128, device="cuda").bfloat16()
+    n = B.a2sf_paged_workspace_bytes(2, 8, 2, 128, 2, b.table.shape[1] * 64)
+    want = torch.empty_like(q)
+    B.a2sf_paged_attention(q, b.cache, b.table, b.len, want, workspace=torch.empty(n, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    outs = [torch.empty_like(q) for _ in range(2)]
+    for _ in range(20):
+        for s, w, o in zip(streams, spaces, outs):
+            with torch.cuda.stream(s):
+                B.a2sf_paged_attention(q, b.cache, b.table, b.len, o, workspace=w)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+
+
+@pytest.mark.parametrize("dtype,eight", KINDS)
+def test_a_prompt_then_tokens_is_the_whole_at_once(dtype, eight):
+    """Chunks and single tokens give what one call gives, up to the order of sums (both are checked against the oracle)."""
+    whole = Batch(32, [(0, 150)], 2, 128, 16, dtype, eight)
+    x, (q, k, v) = new_rows(whole, 4)
+    table = cos_sin(200, 128)
+    full = torch.empty(150, 4, 128, dtype=whole.dt, device="cuda")
+    B.a2sf_paged_append(q, k, v, whole.cache, whole.table, whole.len, starts=whole.starts, q_out=full, rotary=table)
+    kept = [t.clone() for t in whole.cache.tensors()]
+    whole.rubbish()
+    at = 0
+    for n in (100, 1, 30, 1, 18):
+        s = slice(at, at + n)
+        out = torch.empty(n, 4, 128, dtype=whole.dt, device="cuda")
+        lens = torch.tensor([at + n], dtype=torch.int32, device="cuda")
+        starts = None if n == 1 else torch.tensor([0, n], dtype=torch.int32, device="cuda")
+        B.a2sf_paged_append(q[s], k[s], v[s], whole.cache, whole.table, lens, starts=starts, q_out=out, rotary=table)
+        assert torch.equal(out, full[s])
+        o = torch.empty_like(out)
+        B.a2sf_paged_attention(out, whole.cache, whole.table, lens, o, starts=starts)
+        part = whole
+        part.lengths, part.tokens, part.starts, part.first = [(at, n)], n, starts, [0]
+        check_attention(part, out, o, 1 << 30, 0, one_product=True)
+        at += n
+    page, place = whole.slots()
+    for t, w in zip(whole.cache.tensors(), kept):
+        t, w = (y.view(torch.uint8) if y.dtype == EIGHT else y for y in (t, w))
+        assert torch.equal(t[page, :, place], w[page, :, place])
