@@ -178,6 +178,7 @@ class _NoExtension:
         return -1
 
     decode_step = prefill = prefill_chunk = rms_norm = quantize = matmul_scaled = rotary = sample = _leave
+    paged_append = paged_attention = log_probs = _leave
 
 
 def _load_extension():
@@ -192,7 +193,7 @@ def _load_extension():
         warnings.warn(f"{os.path.join(_HERE, '_call.so')} is missing or does not load ({e}): steps, prompts and chunks take 2 us more host "
                       "time each; build it with `python -m paper_2407_20485_amd.build`", RuntimeWarning, stacklevel=3)
         return _NoExtension
-    extension.init(Cache, torch.float32, torch.bfloat16, _raw_stream if _get_device else None, _get_device)
+    extension.init(Cache, torch.float32, torch.bfloat16, _raw_stream if _get_device else None, _get_device, Pages)
     return extension
 
 
@@ -274,7 +275,7 @@ class Cache:
 
 class Pages:
     """Device buffers of a paged KV cache: k, v [pages, kv_heads, page_size, d], and for 8 bits (torch.float8_e4m3fn) the bytes of
-    their scales [pages, kv_heads, page_size]."""
+    their scales [pages, kv_heads, page_size]; with the matching C struct, made once, so the tensors stay the ones they are."""
 
     def __init__(self, pages: int, page_size: int, kv_heads: int, d: int, dtype: torch.dtype, device="cuda"):
         shape, eight = (pages, kv_heads, page_size, d), dtype == torch.float8_e4m3fn
@@ -308,6 +309,7 @@ class Pages:
         three = ctypes.c_int64 * 3
         self.struct = PagesStruct(k.data_ptr(), v.data_ptr(), _ptr(k_scales), _ptr(v_scales), three(*k.stride()[:3]), three(*scale_stride),
                                   self.pages, self.page_size, self.kv_heads, self.d, _PAGE_CODES[k.dtype])
+        self.address = ctypes.addressof(self.struct)
 
     def tensors(self):
         return tuple(t for t in (self.k, self.v, self.k_scales, self.v_scales) if t is not None)
@@ -682,6 +684,10 @@ def _sequences(table, lens, starts, like):
 def a2sf_paged_append(q, k, v, cache, table, lens, starts=None, q_out=None, rotary=None, interleaved=False, stream=None):
     """q [tokens, heads, d] (with q_out; both may be None), k, v [tokens, kv_heads, d] into the pages of `cache` (Pages); table, lens and
     starts as in a2sf_sequences; rotary: the table [rows, rotary_dims] of a2sf_rotary_table, None: nothing is turned."""
+    at = _entry("a2sf_paged_append")
+    status = _call.paged_append(at, q, k, v, cache, table, lens, starts, q_out, rotary, interleaved, stream)
+    if status >= 0:
+        return _check(status)
     _need(k.dim() == 3 and k.shape[2] == cache.d)
     _need((q is None) == (q_out is None), A2SF_EINVAL)
     _reach(cache.k, k)
@@ -702,6 +708,10 @@ def a2sf_paged_append(q, k, v, cache, table, lens, starts=None, q_out=None, rota
 
 def a2sf_paged_attention(q, cache, table, lens, o, starts=None, window=None, sinks=0, workspace=None, workspace_bytes=None, stream=None):
     """window: tokens that a token sees, itself among them (None: all)."""
+    at = _entry("a2sf_paged_attention")
+    status = _call.paged_attention(at, q, cache, table, lens, o, starts, window, sinks, workspace, workspace_bytes, stream)
+    if status >= 0:
+        return _check(status)
     _need(q.dim() == 3 and q.shape[2] == cache.d)
     _reach(cache.k, q)
     tokens, heads = q.shape[:2]
@@ -736,6 +746,10 @@ def _rows_of(x, rows, dtype, like):
 def a2sf_log_probs(logits, tokens=None, logp=None, entropy=None, top=None, top_tokens=None, stream=None):
     """tokens [rows, given] int32 with logp [rows, given], entropy [rows], top [rows, alternatives] and top_tokens int32: all but the
     logits may be None."""
+    at = _entry("a2sf_log_probs")
+    status = _call.log_probs(at, logits, tokens, logp, entropy, top, top_tokens, stream)
+    if status >= 0:
+        return _check(status)
     _need(logits.dim() == 2)
     rows, n = logits.shape
     _int32(rows, n)

@@ -18,7 +18,8 @@ CALL = os.path.join(HERE, "_call.so")
 CEILINGS = os.path.join(HERE, "ceilings")
 SOURCES = ["a2sf_api.hip", "decode.hip", "select_compact.hip", "prefill_f32.hip", "prefill_bf16.hip",
            "similarity.hip", "chunk.hip", "layer_api.hip", "rows.hip", "matmul.hip", "rotary.hip", "sample.hip",
-           "pages_api.hip", "paged_append.hip", "paged_attention.hip", "logprobs.hip"]
+           "pages_api.hip", "paged_append.hip", "paged_attention.hip",
+           "paged_tiles.hip", "logprobs.hip"]
 OBJECTS = os.path.join(HERE, "_build")
 # -packed-fp32-ops is switched off: packed fp32 forms have produced wrong results on the
 # target machines; the host pass does not know the feature and says so (harmless).

@@ -3,11 +3,13 @@
 //  paged_rows   up to 16 query rows (the heads that share a K/V head, of one token or of neighbouring ones) against a range of their
 //               tokens, straight from memory into registers: the form for single tokens, whose every byte of the cache is
 //               used once.  The range may be a share of what the rows see;
-//  paged_join   adds up the shares.
+//  paged_tiles  (paged_tiles.hip) 128 query rows against tiles of 64 tokens through LDS: bf16 prompts and chunks;
+//  paged_join   adds up the shares of either.
 #include <float.h>
 
 #include <algorithm>
 
+#include "paged_tiles.h"
 #include "pages_dev.h"
 #include "rows_dev.h"
 
@@ -24,92 +26,6 @@ __device__ __forceinline__ f32x4_t mfma16(const uint4& a, const uint4& b, const 
 __device__ __forceinline__ f32x4_t mfma16(float a, float b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
-constexpr float kNan = __builtin_nanf("");
-
-// N neighbouring elements at an element's alignment
-template <int N>
-__device__ __forceinline__ void load_n(const bf16_t* p, uint32_t* r) {
-#pragma unroll
-  for (int i = 0; i < N / 2; i += 4) {
-    const u32x4_t v = *(const u32x4_at2_t*)(p + 2 * i);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) r[i + j] = v[j];
-  }
-}
-typedef uint32_t u32_at2_t __attribute__((aligned(2)));
-template <int N>
-__device__ __forceinline__ void store_n(bf16_t* p, const float* f) {
-  if constexpr (N == 8) {
-    store_unit(p, f);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) ((u32_at2_t*)p)[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
-  }
-}
-template <int N>
-__device__ __forceinline__ void store_n(float* p, const float* f) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) p[i] = f[i];
-}
-
-// Rows of a sequence's new tokens under one K/V head are counted token by token, the heads of a token next to each other; a block
-// has ROWS of them.
-struct RowBlock {
-  int seq, first_row;  // of the sequence's
-  bool any;            // there is such a block
-};
-// Block b of the call: blocks of one sequence after the other.  The whole wave comes here with the same b.
-__device__ __forceinline__ RowBlock row_block(const PagedCache& c, int group, int rows, int b) {
-  RowBlock r = {0, 0, false};
-  if (!c.starts) {
-    const int per = (group + rows - 1) / rows;
-    r.seq = b / per;
-    r.first_row = (b - r.seq * per) * rows;
-    r.any = r.seq < c.sequences;
-    return r;
-  }
-  const int lane = threadIdx.x & 63;
-  long long before = 0;
-  for (int s = 0; s < c.sequences; s += 64) {
-    long long n = 0;
-    if (s + lane < c.sequences) {
-      const long long count = (long long)c.starts[s + lane + 1] - c.starts[s + lane];
-      n = (max(0ll, min(count, (long long)c.tokens)) * group + rows - 1) / rows;
-    }
-    long long upto = n;
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) {
-      const long long other = __shfl_up(upto, step);
-      if (lane >= step) upto += other;
-    }
-    const unsigned long long behind = __ballot(before + upto > b);
-    if (behind) {
-      const int at = __builtin_ctzll(behind);
-      r.seq = s + at;
-      const long long prior = before + __shfl(upto - n, at);
-      r.first_row = (int)(b - prior) * rows;
-      r.any = true;
-      return r;
-    }
-    before += __shfl(upto, 63);
-  }
-  return r;
-}
-// What the rows of a block see between them, and how it is shared out
-struct Share {
-  Visible see;
-  int size, parts;  // tokens of a share, shares that have any
-};
-__device__ __forceinline__ Share share_of(const PagedArgs& a, const NewTokens& t, int first_row, int rows, int unit) {
-  Share s;
-  const int last_row = (int)min((long long)first_row + rows, (long long)t.count * a.group) - 1;
-  s.see = visible(t.past + first_row / a.group, t.past + last_row / a.group, a.window, a.sinks);
-  const int units = (s.see.count + unit - 1) / unit;
-  s.size = (units + a.splits - 1) / a.splits * unit;
-  s.parts = (s.see.count + s.size - 1) / s.size;
-  return s;
-}
-
 // ---- up to 16 rows, straight from memory ------------------------------------------------------------------------------------------
 // S^T = K Q^T with the tokens as rows of the result: lane (g, q) = (l / 16, l % 16) gets the logits of query row q with tokens 4g .. 4g + 3
 // of 16, which is how the second product, O^T = V^T P^T, takes its P^T -- if its k runs over the tokens in that order, which is free to
@@ -133,7 +49,8 @@ struct RowForm {
   static constexpr int E = 4 * H;                         // tokens of V per lane
 };
 
-template <typename T, bool EIGHT, int D>
+// SEVERAL: a block may hold the rows of several tokens, which do not all see the same
+template <typename T, bool EIGHT, int D, bool SEVERAL>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedArgs a) {
   typedef RowForm<T, EIGHT, D> F;
   constexpr int H = F::H, NK = F::NK, VD = F::VD, VW = F::VW, E = F::E, TT = F::TOKENS;
@@ -172,7 +89,6 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedArgs
   const Visible see = share.see;
   const int v0 = split * share.size, v1 = min(see.count, v0 + share.size);
   const int pos = t.past + i_row;
-  const bool one_token = (first_row + kRows - 1) / a.group == first_row / a.group || t.count == 1;
 
   // Q: dimensions in the order of K's loads
   uint4 qb[F::F32 ? 1 : D / 32];
@@ -266,43 +182,21 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedArgs
 
   // A tile with tokens that some rows see and others do not: a probability of 0 keeps no infinity or NaN of V out of a row.  Such values
   // are taken out, and the rows that see one of them get NaN for its dimension: those for which a product of marks is above 0.
-  const auto separate = [&](uint32_t hidden, auto& vb, auto& vf) {
-    const auto odd16 = [](uint32_t x) { return (x & 0x7F80u) == 0x7F80u; };
+  const auto separate = [&](uint32_t hidden, auto& vf) {
     const auto odd32 = [](float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; };
-    bool odd = false;
+    uint32_t odd = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int i = 0; i < VD; ++i) {
-        if constexpr (F::F32) odd |= odd32(vf[e][i]);
-        else odd |= odd16(vb[e][i / 2] >> (i % 2 * 16));
-      }
-    if (!__any(odd)) return;
+      for (int i = 0; i < VD; ++i) odd |= (__float_as_uint(vf[e][i]) & 0x7F800000u) + 0x00800000u;
+    if (!__any(odd >> 31)) return;
 #pragma unroll
     for (int i = 0; i < VD; ++i) {
       f32x4_t marks = {0.f, 0.f, 0.f, 0.f};
-      if constexpr (F::F32) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          marks = mfma16(odd32(vf[e][i]) ? 1.f : 0.f, hidden >> e & 1 ? 0.f : 1.f, marks);
-          if (odd32(vf[e][i])) vf[e][i] = 0.f;
-        }
-      } else {
-        uint32_t w[4], seen[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          w[j] = seen[j] = 0;
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int e = 2 * j + b;
-            if (odd16(vb[e][i / 2] >> (i % 2 * 16))) {
-              w[j] |= 0x3F80u << 16 * b;
-              vb[e][i / 2] &= i % 2 ? 0xFFFFu : 0xFFFF0000u;
-            }
-            if (!(hidden >> e & 1)) seen[j] |= 0x3F80u << 16 * b;
-          }
-        }
-        marks = mfma16(make_uint4(w[0], w[1], w[2], w[3]), make_uint4(seen[0], seen[1], seen[2], seen[3]), marks);
+      for (int e = 0; e < E; ++e) {
+        marks = mfma16(odd32(vf[e][i]) ? 1.f : 0.f, hidden >> e & 1 ? 0.f : 1.f, marks);
+        if (odd32(vf[e][i])) vf[e][i] = 0.f;
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r)
@@ -395,7 +289,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedArgs
           clear(e);
         }
     }
-    if (!one_token) {
+    if constexpr (SEVERAL) {
+      static_assert(F::F32, "several tokens of bf16 take the tile form");
       uint32_t hidden = 0;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -405,7 +300,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedArgs
           hidden |= 1u << e;
         }
       }
-      if (__any(hidden)) separate(hidden, vb, vf);
+      if (__any(hidden)) separate(hidden, vf);
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) top = fmaxf(top, y[e]);
@@ -521,7 +416,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void paged_rows_kernel(PagedArgs
 // A wave takes a row: a share's maximum and sum to a lane, then the shares' vectors one after the other.
 constexpr int kMostSplits = 64;
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int rows, int unit) {
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int unit) {  // unit: that of paged_rows' shares; 0: paged_tiles made them
   constexpr int N = D / 64;
   const PagedCache& c = a.c;
   const int lane = threadIdx.x & 63;
@@ -538,17 +433,17 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int rows, 
   for (int i = 0; i < N; ++i) f[i] = t.bad ? kNan : 0.f;
   if (!t.bad && t.past >= 0) {
     const int row = (token - t.first) * a.group + head % a.group;
-    const Share s = share_of(a, t, row / rows * rows, rows, unit);
+    const int parts = unit ? share_of(a, t, row / kRows * kRows, kRows, unit).parts : tile_plan(a, t, row / kTileRows * kTileRows).parts;
     const float* part = a.part + at * a.splits * D + lane * N;
     float m = -FLT_MAX, l = 0.f;
-    if (lane < s.parts) {
+    if (lane < parts) {
       m = a.part_ml[2 * (at * a.splits + lane)];
       l = a.part_ml[2 * (at * a.splits + lane) + 1];
     }
     const float k = fast_exp2(m - wave_max(m));
     const float inv = 1.f / wave_sum(k * l);
 #pragma unroll 8
-    for (int p = 0; p < s.parts; ++p) {
+    for (int p = 0; p < parts; ++p) {
       const float w = wave_broadcast(k, p);
 #pragma unroll
       for (int i = 0; i < N; ++i) f[i] += w * part[(long long)p * D + i];
@@ -560,32 +455,37 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int rows, 
   for (int i = 0; i < N; ++i) store_one(out + i, f[i]);
 }
 
+// Blocks of `rows` rows, or a few more than there are
 int row_blocks(int tokens, int group, int sequences, bool one_each, int rows) {
   return one_each ? sequences * ((group + rows - 1) / rows) : (int)((long long)tokens * group / rows) + sequences;
 }
 // Shares for `groups` workgroups whose rows see at most `most` tokens
-constexpr int kWantedGroups = 2048;
-int splits_for(long long groups, long long most, int unit) {
-  const long long want = (kWantedGroups + groups - 1) / groups, units = (most + unit - 1) / unit;
+constexpr int kWantedGroups = 2048, kWantedTileGroups = 1024;
+int splits_for(long long groups, long long most, int unit, int wanted) {
+  const long long want = (wanted + groups - 1) / groups, units = (most + unit - 1) / unit;
   return (int)std::max(1ll, std::min({want, units, (long long)kMostSplits}));
 }
+constexpr int kFewestTiles = 4;  // of a share
 size_t part_bytes(long long rows, int splits, int d) { return splits > 1 ? (size_t)rows * splits * (d + 2) * 4 : 0; }
 
 template <typename T, bool EIGHT, int D>
 bool attend(PagedArgs a, void* workspace, size_t bytes, hipStream_t st) {
   typedef RowForm<T, EIGHT, D> F;
   const long long rows = (long long)a.c.tokens * a.heads;
-  a.blocks = row_blocks(a.c.tokens, a.group, a.c.sequences, !a.c.starts, kRows);
+  const bool tiles = a.c.starts && !F::F32;
+  a.blocks = row_blocks(a.c.tokens, a.group, a.c.sequences, !a.c.starts, tiles ? kTileRows : kRows);
   const long long groups = (long long)a.blocks * a.c.kv_heads;
-  const long long most = std::min((long long)a.c.table_pages << a.c.shift, (long long)a.window + a.sinks + (a.c.starts ? kRows : 0));
-  a.splits = splits_for(groups, most, F::UNIT);
+  const long long most = std::min((long long)a.c.table_pages << a.c.shift, (long long)a.window + a.sinks + (tiles ? kTileRows : a.c.starts ? kRows : 0));
+  a.splits = tiles ? splits_for(groups, most, kFewestTiles * kTileTokens, kWantedTileGroups) : splits_for(groups, most, F::UNIT, kWantedGroups);
   while (a.splits > 1 && part_bytes(rows, a.splits, D) > bytes) --a.splits;
-  a.part_ml = (float*)workspace;
-  a.part = a.part_ml + 2 * rows * a.splits;
+  a.part = (float*)workspace;
+  a.part_ml = a.part + rows * a.splits * D;
   const unsigned long long grid = (unsigned long long)groups * a.splits, join = (unsigned long long)(rows + 3) / 4;
   if (!grid_fits(grid, 64 * kRowWaves) || !grid_fits(join, 256)) return false;
-  paged_rows_kernel<T, EIGHT, D><<<(uint32_t)grid, 64 * kRowWaves, 0, st>>>(a);
-  if (a.splits > 1) paged_join_kernel<T, D><<<(uint32_t)join, 256, 0, st>>>(a, kRows, F::UNIT);
+  if (tiles) launch_paged_tiles(a, (uint32_t)grid, st);
+  else if (!a.c.starts) paged_rows_kernel<T, EIGHT, D, false><<<(uint32_t)grid, 64 * kRowWaves, 0, st>>>(a);
+  else if constexpr (F::F32) paged_rows_kernel<T, EIGHT, D, true><<<(uint32_t)grid, 64 * kRowWaves, 0, st>>>(a);
+  if (a.splits > 1) paged_join_kernel<T, D><<<(uint32_t)join, 256, 0, st>>>(a, tiles ? 0 : F::UNIT);
   return true;
 }
 
@@ -600,12 +500,13 @@ bool attend(const PagedArgs& a, void* workspace, size_t bytes, hipStream_t st) {
 
 size_t paged_workspace(int tokens, int heads, int kv_heads, int d, int sequences, long long table_tokens) {
   const long long rows = (long long)tokens * heads;
-  size_t most = 0;
-  for (const bool one_each : {true, false}) {
-    if (one_each && tokens != sequences) continue;
-    const long long groups = (long long)row_blocks(tokens, heads / kv_heads, sequences, one_each, kRows) * kv_heads;
-    most = std::max(most, part_bytes(rows, splits_for(groups, table_tokens, 16 * kRowWaves), d));
-  }
+  const auto bytes = [&](bool one_each, int block, int unit, int wanted) {
+    const long long groups = (long long)row_blocks(tokens, heads / kv_heads, sequences, one_each, block) * kv_heads;
+    return part_bytes(rows, splits_for(groups, table_tokens, unit, wanted), d);
+  };
+  // (of the forms for single tokens that of fp32 has the smaller shares)
+  size_t most = std::max(bytes(false, kRows, 16 * kRowWaves, kWantedGroups), bytes(false, kTileRows, kFewestTiles * kTileTokens, kWantedTileGroups));
+  if (tokens == sequences) most = std::max(most, bytes(true, kRows, 16 * kRowWaves, kWantedGroups));
   return most;
 }
 

@@ -1,0 +1,33 @@
+// How the tile form of attention over pages shares out its work (paged_tiles.hip; paged_join of paged_attention.hip follows it).
+#pragma once
+#include "pages_dev.h"
+
+namespace a2sf {
+
+constexpr int kTileRows = 128;   // query rows of a workgroup
+constexpr int kTileTokens = 64;
+
+// The tiles of a block of rows: those of the first `sinks` tokens, if they lie apart, then those from token `from` (a multiple of eight, so
+// that eight rows are in one page) to the block's newest token.
+struct TilePlan {
+  int sinks, sink_tiles, from, tiles;
+  int per, parts;  // tiles of a share, shares that have any
+};
+__device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, const NewTokens& t, int first_row) {
+  const int last_row = (int)min((long long)first_row + kTileRows, (long long)t.count * a.group) - 1;
+  const int p0 = t.past + first_row / a.group, p1 = t.past + last_row / a.group;
+  TilePlan p;
+  const Visible see = visible(p0, p1, a.window, a.sinks);
+  p.sinks = see.sinks;
+  p.from = see.from & ~7;
+  p.sink_tiles = (p.sinks + kTileTokens - 1) / kTileTokens;
+  if (p.sinks >= p.from) p.from = p.sink_tiles = 0;
+  p.tiles = p.sink_tiles + (p1 - p.from) / kTileTokens + 1;
+  p.per = (p.tiles + a.splits - 1) / a.splits;
+  p.parts = (p.tiles + p.per - 1) / p.per;
+  return p;
+}
+
+void launch_paged_tiles(const PagedArgs& a, uint32_t grid, hipStream_t st);
+
+}  // namespace a2sf

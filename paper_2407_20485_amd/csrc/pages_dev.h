@@ -3,6 +3,7 @@
 #pragma once
 #include "a2sf_dev.h"
 #include "a2sf_internal.h"
+#include "rows_dev.h"
 
 namespace a2sf {
 
@@ -60,5 +61,82 @@ __device__ __forceinline__ int page_of(const PagedCache& c, const int32_t* row, 
 
 // The value that a scale's byte stands for (255 stands for no number, as its values' bytes do too)
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
+
+constexpr float kNan = __builtin_nanf("");
+
+// N neighbouring elements at an element's alignment
+typedef uint32_t u32_at2_t __attribute__((aligned(2)));
+template <int N>
+__device__ __forceinline__ void store_n(bf16_t* p, const float* f) {
+  if constexpr (N == 8) {
+    store_unit(p, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) ((u32_at2_t*)p)[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+  }
+}
+template <int N>
+__device__ __forceinline__ void store_n(float* p, const float* f) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) p[i] = f[i];
+}
+
+// Rows of a sequence's new tokens under one K/V head are counted token by token, the heads of a token next to each other; a block
+// has ROWS of them.
+struct RowBlock {
+  int seq, first_row;  // of the sequence's
+  bool any;            // there is such a block
+};
+// Block b of the call: blocks of one sequence after the other.  The whole wave comes here with the same b.
+__device__ __forceinline__ RowBlock row_block(const PagedCache& c, int group, int rows, int b) {
+  RowBlock r = {0, 0, false};
+  if (!c.starts) {
+    const int per = (group + rows - 1) / rows;
+    r.seq = b / per;
+    r.first_row = (b - r.seq * per) * rows;
+    r.any = r.seq < c.sequences;
+    return r;
+  }
+  const int lane = threadIdx.x & 63;
+  long long before = 0;
+  for (int s = 0; s < c.sequences; s += 64) {
+    long long n = 0;
+    if (s + lane < c.sequences) {
+      const long long count = (long long)c.starts[s + lane + 1] - c.starts[s + lane];
+      n = (max(0ll, min(count, (long long)c.tokens)) * group + rows - 1) / rows;
+    }
+    long long upto = n;
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) {
+      const long long other = __shfl_up(upto, step);
+      if (lane >= step) upto += other;
+    }
+    const unsigned long long behind = __ballot(before + upto > b);
+    if (behind) {
+      const int at = __builtin_ctzll(behind);
+      r.seq = s + at;
+      const long long prior = before + __shfl(upto - n, at);
+      r.first_row = (int)(b - prior) * rows;
+      r.any = true;
+      return r;
+    }
+    before += __shfl(upto, 63);
+  }
+  return r;
+}
+// What the rows of a block see between them, and how it is shared out
+struct Share {
+  Visible see;
+  int size, parts;  // tokens of a share, shares that have any
+};
+__device__ __forceinline__ Share share_of(const PagedArgs& a, const NewTokens& t, int first_row, int rows, int unit) {
+  Share s;
+  const int last_row = (int)min((long long)first_row + rows, (long long)t.count * a.group) - 1;
+  s.see = visible(t.past + first_row / a.group, t.past + last_row / a.group, a.window, a.sinks);
+  const int units = (s.see.count + unit - 1) / unit;
+  s.size = (units + a.splits - 1) / a.splits * unit;
+  s.parts = (s.see.count + s.size - 1) / s.size;
+  return s;
+}
 
 }  // namespace a2sf

@@ -8,6 +8,7 @@
 // returns -1 before anything is done, and binding.py goes through ctypes, whose conversions and errors then apply.
 #include <Python.h>
 
+#include <algorithm>
 #include <exception>
 
 #include <torch/csrc/autograd/python_variable.h>
@@ -17,8 +18,8 @@
 
 namespace {
 
-PyObject *g_cache_type, *g_f32, *g_bf16, *g_raw_stream, *g_get_device;  // set once, by init
-PyObject *n_k, *n_v, *n_scores, *n_pos, *n_len, *n_G, *n_capacity, *n_d, *n_dtype;
+PyObject *g_cache_type, *g_f32, *g_bf16, *g_raw_stream, *g_get_device, *g_pages_type;  // set once, by init
+PyObject *n_k, *n_v, *n_scores, *n_pos, *n_len, *n_G, *n_capacity, *n_d, *n_dtype, *n_address;
 
 // Each reader: true if `x` is of the plain kind.
 bool tensor(PyObject* x, const at::Tensor** t) {
@@ -378,11 +379,130 @@ PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (binding.Cache, torch.float32, torch.bfloat16, function device -> current raw stream or None, function -> current device)
+// ---- keys and values in pages: [tokens, heads, d] tensors and binding.Pages itself ----
+bool heads_like(PyObject* x, const at::Tensor& like, int64_t heads, a2sf_heads* s) {
+  const at::Tensor* t;
+  if (!tensor(x, &t) || t->dim() != 3 || t->size(0) != like.size(0) || t->size(2) != like.size(2) || (heads && t->size(1) != heads) ||
+      t->stride(2) != 1 || t->scalar_type() != like.scalar_type() || t->device() != like.device() || t->size(1) > INT32_MAX)
+    return false;
+  *s = {t->data_ptr(), {t->stride(0), t->stride(1)}};
+  return true;
+}
+// the tensor that gives a call its tokens, heads and type, and the pages, on its device and of its d
+bool first_heads(PyObject* x, PyObject* cache, const at::Tensor** t, int32_t* dtype, const a2sf_pages** pages) {
+  if (!tensor(x, t) || (*t)->dim() != 3 || !type_of(**t, dtype) || (*t)->size(0) > INT32_MAX || (*t)->size(1) > INT32_MAX) return false;
+  if ((PyObject*)Py_TYPE(cache) != g_pages_type) return false;
+  const bool there = attribute(cache, n_address, [&](PyObject* a) {
+    *pages = PyLong_CheckExact(a) ? (const a2sf_pages*)PyLong_AsVoidPtr(a) : nullptr;
+    return *pages != nullptr;
+  });
+  return there && (*t)->size(2) == (*pages)->d && attribute(cache, n_k, [&](PyObject* a) {
+           const at::Tensor* k;
+           return tensor(a, &k) && k->device() == (*t)->device();
+         });
+}
+bool sequences(PyObject* table, PyObject* lens, PyObject* starts, const at::Tensor& like, a2sf_sequences* s) {
+  const at::Tensor* t;
+  const void *len, *start;
+  if (!tensor(table, &t) || t->scalar_type() != at::kInt || t->dim() != 2 || (t->size(1) != 1 && t->stride(1) != 1) ||
+      t->device() != like.device() || t->size(0) > INT32_MAX || t->size(1) > INT32_MAX || lens == Py_None ||
+      !column(lens, like, t->size(0), at::kInt, &len) || !column(starts, like, t->size(0) + 1, at::kInt, &start))
+    return false;
+  *s = {(const int32_t*)t->data_ptr(), (const int32_t*)len, (const int32_t*)start, t->stride(0), (int32_t)t->size(0), (int32_t)t->size(1)};
+  return true;
+}
+
+// (entry point, q, k, v, cache, table, lens, starts, q_out, rotary, interleaved, stream)
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!expects(n, 12)) return nullptr;
+  return guarded([&] {
+    void *st, *fn = PyLong_AsVoidPtr(a[0]);
+    const at::Tensor *k, *q, *rotary = nullptr;
+    const a2sf_pages* pages;
+    a2sf_heads hq, hk, hv, ho;
+    a2sf_sequences s;
+    int32_t dtype;
+    if (!(fn && first_heads(a[2], a[4], &k, &dtype, &pages) && heads_like(a[2], *k, pages->kv_heads, &hk) &&
+          heads_like(a[3], *k, pages->kv_heads, &hv) && sequences(a[5], a[6], a[7], *k, &s) && PyBool_Check(a[10]) &&
+          stream(a[11], a[2], &st)))
+      return -1;
+    const bool with_q = a[1] != Py_None;
+    if (with_q != (a[8] != Py_None)) return -1;
+    if (with_q && !(heads_like(a[1], *k, 0, &hq) && tensor(a[1], &q) && heads_like(a[8], *k, q->size(1), &ho))) return -1;
+    if (a[9] != Py_None && !(tensor(a[9], &rotary) && rotary->dim() == 2 && rotary->is_contiguous() && rotary->scalar_type() == at::kFloat &&
+                             rotary->device() == k->device() && rotary->size(0) <= INT32_MAX && rotary->size(1) <= INT32_MAX))
+      return -1;
+    return without_gil([&]() -> int {
+      return ((decltype(&a2sf_paged_append))fn)(with_q ? &hq : nullptr, &hk, &hv, (int32_t)k->size(0), with_q ? (int32_t)q->size(1) : 0,
+                                                dtype, &s, pages, rotary ? (const float*)rotary->data_ptr() : nullptr,
+                                                rotary ? (int32_t)rotary->size(0) : 0, rotary ? (int32_t)rotary->size(1) : 0,
+                                                a[10] == Py_True, with_q ? &ho : nullptr, st);
+    });
+  });
+}
+
+// (entry point, q, cache, table, lens, o, starts, window, sinks, workspace, workspace_bytes, stream)
+PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!expects(n, 12)) return nullptr;
+  return guarded([&] {
+    void *ws, *st, *fn = PyLong_AsVoidPtr(a[0]);
+    const at::Tensor *q, *room;
+    const a2sf_pages* pages;
+    a2sf_heads hq, ho;
+    a2sf_sequences s;
+    int32_t dtype, window = A2SF_NO_WINDOW, sinks;
+    size_t bytes;
+    if (!(fn && first_heads(a[1], a[2], &q, &dtype, &pages) && heads_like(a[1], *q, 0, &hq) && heads_like(a[5], *q, q->size(1), &ho) &&
+          sequences(a[3], a[4], a[6], *q, &s) && (a[7] == Py_None || number(a[7], &window)) && number(a[8], &sinks) &&
+          workspace(a[9], a[10], &ws, &bytes) && (!tensor(a[9], &room) || room->device() == q->device()) && stream(a[11], a[1], &st)))
+      return -1;
+    return without_gil([&]() -> int {
+      return ((decltype(&a2sf_paged_attention))fn)(&hq, (int32_t)q->size(0), (int32_t)q->size(1), dtype, &s, pages, window, sinks, &ho, ws,
+                                                   bytes, st);
+    });
+  });
+}
+
+// (entry point, logits, tokens, logp, entropy, top, top_tokens, stream)
+PyObject* log_probs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!expects(n, 8)) return nullptr;
+  return guarded([&] {
+    void *st, *fn = PyLong_AsVoidPtr(a[0]);
+    const at::Tensor* x;
+    a2sf_rows logits = {}, s[4];
+    const a2sf_rows* to[4];
+    const void* entropy;
+    int32_t dtype;
+    if (!(fn && first(a[1], &x, &dtype) && matrix(*x, x->size(0), x->size(1)) && column(a[4], *x, x->size(0), at::kFloat, &entropy) &&
+          stream(a[7], a[1], &st)))
+      return -1;
+    logits = {x->data_ptr(), x->stride(0)};
+    PyObject* const given[4] = {a[2], a[3], a[5], a[6]};
+    int64_t columns[4] = {0, 0, 0, 0};
+    for (int i = 0; i < 4; ++i) {
+      const at::Tensor* t;
+      to[i] = nullptr;
+      if (given[i] == Py_None) continue;
+      if (!tensor(given[i], &t) || t->dim() != 2 || !matrix(*t, x->size(0), t->size(1)) || t->size(1) > INT32_MAX ||
+          t->scalar_type() != (i == 0 || i == 3 ? at::kInt : at::kFloat) || t->device() != x->device())
+        return -1;
+      s[i] = {t->data_ptr(), t->stride(0)};
+      columns[i] = t->size(1);
+      to[i] = s + i;
+    }
+    if (columns[0] != columns[1] || (to[2] && to[3] && columns[2] != columns[3])) return -1;
+    return without_gil([&]() -> int {
+      return ((decltype(&a2sf_log_probs))fn)(&logits, (int32_t)x->size(0), (int32_t)x->size(1), dtype, to[0], (int32_t)columns[0], to[1],
+                                             (float*)entropy, to[2], to[3], (int32_t)std::max(columns[2], columns[3]), st);
+    });
+  });
+}
+
+// (binding.Cache, torch.float32, torch.bfloat16, function device -> current raw stream or None, function -> current device, binding.Pages)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!expects(n, 5)) return nullptr;
-  PyObject** const to[] = {&g_cache_type, &g_f32, &g_bf16, &g_raw_stream, &g_get_device};
-  for (int i = 0; i < 5; ++i) {
+  if (!expects(n, 6)) return nullptr;
+  PyObject** const to[] = {&g_cache_type, &g_f32, &g_bf16, &g_raw_stream, &g_get_device, &g_pages_type};
+  for (int i = 0; i < 6; ++i) {
     Py_XDECREF(*to[i]);
     *to[i] = a[i] == Py_None ? nullptr : a[i];
     Py_XINCREF(*to[i]);
@@ -399,6 +519,9 @@ PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)())init, METH_FASTCALL, 
                          {"matmul_scaled", (PyCFunction)(void (*)())matmul_scaled, METH_FASTCALL, nullptr},
                          {"rotary", (PyCFunction)(void (*)())rotary, METH_FASTCALL, nullptr},
                          {"sample", (PyCFunction)(void (*)())sample, METH_FASTCALL, nullptr},
+                         {"paged_append", (PyCFunction)(void (*)())paged_append, METH_FASTCALL, nullptr},
+                         {"paged_attention", (PyCFunction)(void (*)())paged_attention, METH_FASTCALL, nullptr},
+                         {"log_probs", (PyCFunction)(void (*)())log_probs, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -407,9 +530,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, null
 #define A2SF_STR_(x) #x
 #define A2SF_STR(x) A2SF_STR_(x)
 PyMODINIT_FUNC PyInit__call() {
-  PyObject** const names[] = {&n_k, &n_v, &n_scores, &n_pos, &n_len, &n_G, &n_capacity, &n_d, &n_dtype};
-  const char* const text[] = {"k", "v", "scores", "pos", "len", "G", "capacity", "d", "dtype"};
-  for (int i = 0; i < 9; ++i)
+  PyObject** const names[] = {&n_k, &n_v, &n_scores, &n_pos, &n_len, &n_G, &n_capacity, &n_d, &n_dtype, &n_address};
+  const char* const text[] = {"k", "v", "scores", "pos", "len", "G", "capacity", "d", "dtype", "address"};
+  for (int i = 0; i < 10; ++i)
     if (!*names[i] && !(*names[i] = PyUnicode_InternFromString(text[i]))) return nullptr;
   PyObject* m = PyModule_Create(&module);
   // (binding.py does without the extension where these are not the ones that run)

@@ -707,3 +707,53 @@ def test_a_prompt_then_tokens_is_the_whole_at_once(dtype, eight):
     for t, w in zip(whole.cache.tensors(), kept):
         t, w = (y.view(torch.uint8) if y.dtype == EIGHT else y for y in (t, w))
         assert torch.equal(t[page, :, place], w[page, :, place])
+
+
+@pytest.mark.parametrize("one_each", [True, False])
+def test_calls_through_ctypes(one_each, monkeypatch):
+    """The extension and ctypes make the same calls."""
+    lengths = [(70, 1), (300, 1)] if one_each else [(0, 30), (60, 50)]
+    b = Batch(33, lengths, 2, 128, 16, "bf16", True, one_each=one_each).fill()
+    x, (q, k, v) = new_rows(b, 4)
+    table = cos_sin(400, 128)
+    logits = torch.randn(7, 500, device="cuda").bfloat16()
+    tokens = torch.randint(0, 500, (7, 2), dtype=torch.int32, device="cuda")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    kept = [t.clone() for t in b.cache.tensors()]
+    got = []
+    for call in (B._call, B._NoExtension):
+        monkeypatch.setattr(B, "_call", call)
+        for t, c in zip(b.cache.tensors(), kept):
+            t.copy_(c)
+        out, o = (torch.zeros(b.tokens, 4, 128, dtype=b.dt, device="cuda") for _ in range(2))
+        logp, entropy, top = torch.zeros(7, 2, device="cuda"), torch.zeros(7, device="cuda"), torch.zeros(7, 3, device="cuda")
+        ids = torch.zeros(7, 3, dtype=torch.int32, device="cuda")
+        B.a2sf_paged_append(q, k, v, b.cache, b.table, b.len, starts=b.starts, q_out=out, rotary=table, interleaved=True)
+        B.a2sf_paged_attention(out, b.cache, b.table, b.len, o, starts=b.starts, window=40, sinks=3, workspace=ws)
+        B.a2sf_log_probs(logits, tokens, logp, entropy, top, ids)
+        got.append([t.clone().contiguous().view(torch.uint8) for t in (out, o, logp, entropy, top, ids, *b.cache.tensors())])
+    assert all(torch.equal(a, c) for a, c in zip(*got))
+
+
+@pytest.mark.parametrize("page", [1, 4, 8])
+@pytest.mark.parametrize("dtype,eight", [("bf16", False), ("bf16", True)])
+def test_prompts_in_small_pages(page, dtype, eight):
+    """Pages that end inside the rows that one load takes."""
+    b = Batch(34, [(0, 100), (77, 140), (1000, 3)], 2, 64, page, dtype, eight).fill()
+    attend(b, 6, one_product=True)
+    attend(b, 6, 50, 5, one_product=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("one_each", [True, False])
+def test_scales_of_any_size(dtype, one_each):
+    """Scale bytes from the smallest to where bf16 ends: values of 8 bits times powers of two."""
+    b = Batch(35, [(40, 1)] if one_each else [(3, 38)], 1, 128, 16, dtype, True, one_each=one_each).fill()
+    page, place = b.slots()
+    b.ks[page, :, place] = 120
+    for byte in (10, 60, 127, 200, 235):
+        b.vs[page, :, place] = byte
+        attend(b, 4, one_product=True)
+    b.vs[page, :, place] = torch.randint(100, 150, (len(page), 1), dtype=torch.uint8, device="cuda")
+    b.ks[page, :, place] = torch.randint(110, 124, (len(page), 1), dtype=torch.uint8, device="cuda")
+    attend(b, 4, one_product=True)

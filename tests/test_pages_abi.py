@@ -184,3 +184,21 @@ def test_binding_takes_sizes_and_types_from_the_tensors(no_gpu):
               dict(tokens=torch.zeros(3, 2, dtype=torch.int32), logp=torch.zeros(3, 1))):
         with refused():
             B.a2sf_log_probs(x, stream=0, **a)
+
+
+def test_extension_leaves_unusual_arguments_to_ctypes():
+    bf = torch.bfloat16
+    k = torch.zeros(4, 2, 16, 128, dtype=bf)
+    cache = B.Pages.of(k, k.clone())
+    q = torch.zeros(3, 4, 128, dtype=bf)
+    table, lens = torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    at = B._entry("a2sf_paged_attention")
+    good = dict(q=q, cache=cache, table=table, lens=lens, o=q.clone(), starts=None, window=None, sinks=0, workspace=None, nbytes=None,
+                stream=None)
+    assert B._call.paged_attention(at, *good.values()) == -1                                    # not on a GPU
+    for change in (dict(q=5), dict(cache=cache.struct), dict(window=2.0), dict(sinks=None), dict(stream=0), dict(table=None), dict(lens=None)):
+        assert B._call.paged_attention(at, *{**good, **change}.values()) == -1
+    with pytest.raises(TypeError):
+        B._call.paged_attention(at, q)
+    assert B._call.paged_append(B._entry("a2sf_paged_append"), q, k, k, cache, table, lens, None, None, None, False, None) == -1
+    assert B._call.log_probs(B._entry("a2sf_log_probs"), torch.zeros(3, 9), None, None, torch.zeros(3), None, None, None) == -1
