@@ -585,8 +585,9 @@ def test_log_probs_of_rows_with_ties(dtype, n):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n", [5, 700, 40000])
 def test_log_probs_of_rows_that_are_not_numbers(dtype, n):
-    x = torch.randn(9, n, device="cuda", generator=torch.Generator("cuda").manual_seed(n)).to(DT[dtype])
+    x = torch.randn(10, n, device="cuda", generator=torch.Generator("cuda").manual_seed(n)).to(DT[dtype])
     inf = math.inf
+    x[9, : n // 2] = math.nan                                  # whole groups of lanes
     x[0, 3] = math.nan
     x[1, 2] = inf
     x[2] = -inf
@@ -601,6 +602,19 @@ def test_log_probs_of_rows_that_are_not_numbers(dtype, n):
     logp, entropy, top, ids = log_probs(x, 2, min(5, n), extra=(0, 0, 0, 0, 4))
     assert float(entropy[4]) == 0.0 and float(top[4, 0]) == 0.0 and bool((top[4, 1:] == -inf).all())
     assert bool(torch.isnan(entropy[[0, 1, 2, 5, 6]]).all())
+
+
+@pytest.mark.parametrize("dtype,rows,n,k", [("bf16", 700, 9001, 20), ("f32", 600, 8200, 32), ("bf16", 520, 12000, 33), ("f32", 3, 300001, 64)])
+def test_log_probs_of_many_rows(dtype, rows, n, k):
+    x = torch.randn(rows, n, device="cuda", generator=torch.Generator("cuda").manual_seed(k)).to(DT[dtype])
+    x[1] = x[1].sort().values                                   # a row that rises: its list overflows
+    tokens = torch.randint(0, n, (rows, 1), dtype=torch.int32, device="cuda")
+    logp, entropy, top = torch.empty(rows, 1, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, k, device="cuda")
+    ids = torch.empty(rows, k, dtype=torch.int32, device="cuda")
+    B.a2sf_log_probs(x, tokens, logp, entropy, top, ids)
+    few = [0, 1, 2] + ([rows // 2, rows - 1] if rows > 3 else [])
+    check_log_probs(x[few], tokens[few], logp[few], entropy[few], top[few], ids[few])
+    assert torch.equal(ids, torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :k].int())
 
 
 def test_log_probs_asks_for_parts():
