@@ -255,8 +255,9 @@ struct PagedArgs {
   int heads, group, window, sinks;
   float scale_log2e;
   // set by the launcher
-  float *part, *part_ml;  // [rows][splits][d], [rows][splits][2]: a row is a (token, head)
-  int splits, blocks;
+  float *part, *part_ml;  // sums of parts of rows, their maxima and weights: [rows][splits] (a row is a (token, head)) or [even][2][part_rows]
+  int splits, blocks, blocks_per;  // blocks of rows: of the call, of a sequence (one token each)
+  int even, part_rows;             // workgroups that share the tokens evenly (one token each), or 0
 };
 size_t paged_workspace(int tokens, int heads, int kv_heads, int d, int sequences, long long table_tokens);
 bool launch_paged_attention(PagedArgs a, int dtype, void* workspace, size_t workspace_bytes, hipStream_t st);

@@ -17,9 +17,9 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, const NewToken
   const int last_row = (int)min((long long)first_row + kTileRows, (long long)t.count * a.group) - 1;
   const int p0 = t.past + first_row / a.group, p1 = t.past + last_row / a.group;
   TilePlan p;
-  const Visible see = visible(p0, p1, a.window, a.sinks);
-  p.sinks = see.sinks;
-  p.from = see.from & ~7;
+  const int from = first_in_window(p0, a.window);
+  p.sinks = min(a.sinks, from);
+  p.from = from & ~7;
   p.sink_tiles = (p.sinks + kTileTokens - 1) / kTileTokens;
   if (p.sinks >= p.from) p.from = p.sink_tiles = 0;
   p.tiles = p.sink_tiles + (p1 - p.from) / kTileTokens + 1;

@@ -39,15 +39,24 @@ __device__ __forceinline__ int sequence_of(const PagedCache& c, int t) {
   return before - 1;
 }
 
-// Tokens that positions p0 .. p1 of a sequence see between them: 0 .. sinks - 1 and from .. p1.  They are numbered one after the other.
+// Tokens that positions p0 .. p1 of a sequence see between them: the first `sinks` and those from a position on.  They are numbered one
+// after the other, sixteen that start at a multiple of sixteen together, so that such a group is in one page if pages have so many; the
+// few that nobody sees are in the numbers below `edge`.
 struct Visible {
-  int sinks, from, count;
+  int sinks, from, count, edge;  // sinks, from: multiples of sixteen
   __device__ __forceinline__ int token(int i) const { return i < sinks ? i : i - sinks + from; }
 };
+__device__ __forceinline__ int first_in_window(int p0, int window) { return p0 < window ? 0 : p0 - window + 1; }
 __device__ __forceinline__ Visible visible(int p0, int p1, int window, int sinks) {
   Visible v;
-  v.from = p0 < window ? 0 : p0 - window + 1;
-  v.sinks = min(sinks, v.from);
+  const int from = first_in_window(p0, window);
+  v.from = from & ~15;
+  v.sinks = (min(sinks, from) + 15) & ~15;
+  v.edge = from > 0 ? v.sinks + 16 : 0;
+  if (v.sinks >= v.from) {  // nothing between them
+    v.from = v.sinks = 0;
+    v.edge = from;
+  }
   v.count = v.sinks + p1 - v.from + 1;
   return v;
 }
