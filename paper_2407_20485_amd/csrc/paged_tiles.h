@@ -28,6 +28,28 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, const NewToken
   return p;
 }
 
+// The block of a rank: the sequences by their lengths, longer ones first, and in a sequence the blocks from its end, whose rows see most (up
+// to 64 sequences, one to a lane; the whole wave comes here).  What is begun last is then short.  (Blocks by what they see across the
+// sequences would end more evenly, but share no tiles in the caches: 4 prompts of up to 2048 tokens x us, y.)
+__device__ __forceinline__ RowBlock ranked_block(const PagedArgs& a, int rank) {
+  const int lane = threadIdx.x & 63;
+  int blocks = 0, len = -1;
+  if (lane < a.c.sequences) {
+    const NewTokens t = new_tokens(a.c, lane);
+    blocks = (int)(((long long)t.count * a.group + kTileRows - 1) / kTileRows);
+    len = t.bad ? 0 : t.past + t.count;
+  }
+  int before = 0;
+  for (int s = 0; s < a.c.sequences; ++s) {
+    const int other = __builtin_amdgcn_readlane(len, s);
+    if (other > len || (other == len && s < lane)) before += __builtin_amdgcn_readlane(blocks, s);
+  }
+  const unsigned long long here = __ballot(before <= rank && rank < before + blocks);
+  if (!here) return {0, 0, false};
+  const int seq = __builtin_ctzll(here);
+  return {seq, (__builtin_amdgcn_readlane(blocks, seq) - 1 - (rank - __builtin_amdgcn_readlane(before, seq))) * kTileRows, true};
+}
+
 void launch_paged_tiles(const PagedArgs& a, uint32_t grid, hipStream_t st);
 
 }  // namespace a2sf

@@ -8,6 +8,7 @@
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_tiles.h"
 #include "pages_dev.h"
@@ -43,10 +44,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
   lds_char* const lds = (lds_char*)smem;
   lds_char* const vst = lds + 2 * kTB;
 
-  // K/V heads fastest, so that with a multiple of eight of them a head's blocks are on one die; the last blocks, whose rows see most, first
+  // K/V heads fastest, so that with a multiple of eight of them a head's blocks are on one die; blocks whose rows see most first
   const int kv = blockIdx.x % c.kv_heads;
   const int split = blockIdx.x / c.kv_heads % a.splits;
-  const RowBlock rb = row_block(c, a.group, kTileRows, a.blocks - 1 - (int)(blockIdx.x / c.kv_heads / a.splits));
+  const int rank = (int)(blockIdx.x / c.kv_heads / a.splits);
+  const RowBlock rb = c.sequences <= 64 ? ranked_block(a, rank) : row_block(c, a.group, kTileRows, a.blocks - 1 - rank);
   if (!rb.any) return;
   const int seq = __builtin_amdgcn_readfirstlane(rb.seq), first_row = __builtin_amdgcn_readfirstlane(rb.first_row);
   const NewTokens t = new_tokens(c, seq);
@@ -123,15 +125,19 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
   const auto fetch = [&](int i, int pages, lds_char* kt, lds_char* vt) {  // bf16
     const int base = base_of(i);
     const int sound = (uint32_t)pages < (uint32_t)c.pages ? pages : 0;
+    if (grouped) {
 #pragma unroll
-    for (int u = 0; u < NL; ++u) {
-      const uint32_t to = (u * 4 + wave) * 1024;
-      if (grouped) {
+      for (int u = 0; u < NL; ++u) {
+        const uint32_t to = (u * 4 + wave) * 1024;
         const int r = (u * 4 + wave) * RPL;
         const long long at = (long long)__builtin_amdgcn_readlane(sound, r) * c.stride[0] + (long long)((base + r) & mask_in_page) * c.stride[2];
         dma16(kbase + at, in_group + kchunk * 16, (uint32_t)(size_t)kt + to);
         dma16(vbase + at, in_group + vchunk * 16, (uint32_t)(size_t)vt + to);
-      } else {
+      }
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < NL; ++u) {
+        const uint32_t to = (u * 4 + wave) * 1024;
         const int r = u * 4 * RPL + lrow;
         const long long at = (long long)__shfl(sound, r) * c.stride[0] + (long long)((base + r) & mask_in_page) * c.stride[2];
         dma16_at(kbase + at + kchunk * 16, (uint32_t)(size_t)kt + to);
@@ -159,18 +165,16 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
 #pragma unroll
     for (int u = 0; u < NE; ++u) {
       const int r = (u * kThreads + tid) / (D / 16), col = tid % (D / 16);
+      // (a power of two: values in bf16 are exact, from its subnormal numbers to where its range ends)
       const auto unpack = [&](const uint4& x, uint32_t byte, uint4& lo, uint4& hi) {
         const float scale = scale_value(byte);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        uint32_t b[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x2_t e = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false), f = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
-          b[2 * j] = pack_bf16(e[0] * scale, e[1] * scale);
-          b[2 * j + 1] = pack_bf16(f[0] * scale, f[1] * scale);
-        }
-        lo = make_uint4(b[0], b[1], b[2], b[3]);
-        hi = make_uint4(b[4], b[5], b[6], b[7]);
+        const auto two = [&](uint32_t w, auto half) {
+          return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, scale, decltype(half)::value));
+        };
+        constexpr std::false_type lower{};
+        constexpr std::true_type upper{};
+        lo = make_uint4(two(x.x, lower), two(x.x, upper), two(x.y, lower), two(x.y, upper));
+        hi = make_uint4(two(x.z, lower), two(x.z, upper), two(x.w, lower), two(x.w, upper));
       };
       uint4 lo, hi;
       unpack(kraw[u], both[u] & 255u, lo, hi);
@@ -236,7 +240,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
   // A tile with tokens that some rows see and others do not: a probability of 0 keeps no infinity or NaN of V out of a row.  Such values are
   // taken out of the tile, and the rows that see one of them get NaN for its dimension: those for which a product of marks is above 0.
   // The whole workgroup comes here.
-  const auto separate = [&](bool need, uint32_t hidden, lds_char* vt) {
+  const auto separate = [&](bool need, auto hidden, lds_char* vt) {
     lds_char* const mine = vt + tid * (kTB / kThreads);
     uint32_t odd = 0;
 #pragma unroll
@@ -258,7 +262,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
           uint32_t seen[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            seen[j] = (hidden >> (8 * kt + 2 * j) & 1 ? 0u : 0x3F80u) | (hidden >> (8 * kt + 2 * j + 1) & 1 ? 0u : 0x3F800000u);
+            seen[j] = (hidden(kt / 2, 8 * (kt % 2) + 2 * j) ? 0u : 0x3F80u) | (hidden(kt / 2, 8 * (kt % 2) + 2 * j + 1) ? 0u : 0x3F800000u);
           marks = mfma_bf16(make_uint4(odd_marks(x.x), odd_marks(x.y), odd_marks(y.x), odd_marks(y.y)),
                             make_uint4(seen[0], seen[1], seen[2], seen[3]), marks);
         }
@@ -281,29 +285,36 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
     const bool sink_tile = i < plan.sink_tiles;
     const bool need = any_rows && (sink_tile || (base <= w1 && (w0 - (base + kTile - 1) < a.window || base < a.sinks)));
     const bool uneven = sink_tile ? base + kTile > plan.sinks : base + kTile - 1 > p0 || p1 - base >= a.window;
+    const int limit = sink_tile ? plan.sinks - 1 : pos;
+    // whether this lane's row does not see element e of key block kb (no branches: the comparisons of all 32 stand side by side)
+    const auto hidden = [&](int kb, int e) -> bool {
+      const int token = base + kb * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
+      return (token > limit) | ((pos - token >= a.window) & (token >= a.sinks));
+    };
     f32x16 s[2];
-    uint32_t hidden = 0;
     if (need) {
       logits(kt, s);
-      if (uneven) {
-        const int limit = sink_tile ? plan.sinks - 1 : pos;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int token = base + kb * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
-            if (token > limit || (pos - token >= a.window && token >= a.sinks)) {
-              s[kb][e] = -INFINITY;
-              hidden |= 1u << (kb * 16 + e);
-            }
-          }
-      }
       if (bad) {  // a page that is none of the cache's
+        const uint32_t of_lane[2] = {(uint32_t)bad >> (4 * h), (uint32_t)(bad >> 32) >> (4 * h)};
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (!(hidden >> (kb * 16 + e) & 1) && (bad >> (kb * 32 + 8 * (e >> 2) + 4 * h + (e & 3)) & 1)) s[kb][e] = kNan;
+            s[kb][e] = of_lane[kb] & (1u << (8 * (e >> 2) + (e & 3))) ? kNan : s[kb][e];
+      }
+      if (uneven) {
+        if (sink_tile || p1 - base < a.window) {  // no row's window ends here
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              s[kb][e] = base + kb * 32 + 8 * (e >> 2) + 4 * h + (e & 3) > limit ? -INFINITY : s[kb][e];
+        } else {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[kb][e] = hidden(kb, e) ? -INFINITY : s[kb][e];
+        }
       }
     }
     if (uneven) separate(need, hidden, vt);

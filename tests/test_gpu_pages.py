@@ -769,5 +769,9 @@ def test_scales_of_any_size(dtype, one_each):
         b.vs[page, :, place] = byte
         attend(b, 4, one_product=True)
     b.vs[page, :, place] = torch.randint(100, 150, (len(page), 1), dtype=torch.uint8, device="cuda")
+    b.v.view(torch.uint8)[page[:5], :, place[:5]] = 0           # rows of zeros have the smallest scale
+    b.vs[page[:5], :, place[:5]] = 0
+    b.k.view(torch.uint8)[page[5:9], :, place[5:9]] = 0
     b.ks[page, :, place] = torch.randint(110, 124, (len(page), 1), dtype=torch.uint8, device="cuda")
+    b.ks[page[5:9], :, place[5:9]] = 0
     attend(b, 4, one_product=True)
