@@ -7,8 +7,8 @@ namespace a2sf {
 namespace {
 
 // Eight neighbouring elements of a head to a lane, so 16 (d = 128) or 8 lanes to a head, a few heads of one token each.  An element is
-// turned with its partner, which with pairs of halves another lane holds as its own: it is read twice, the second time from the
-// caches.  All lanes of a head are in one wave, which has read all it needs before it writes, so q may be turned in place.
+// turned with its partner, which with pairs of halves another lane holds as its own: where a whole head of 128 turns, it comes from there
+// by a lane rotation, else it is read twice, the second time from the caches.  All lanes of a head are in one wave, which has read all it needs before it writes, so q may be turned in place.
 constexpr int kMostHeads = 4;
 
 template <typename T, bool EIGHT, int D, bool NEIGHBOURS>
@@ -43,19 +43,45 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   float co[kUnit], si[kUnit];
 #pragma unroll
   for (int j = 0; j < kUnit; ++j) { co[j] = 1.f; si[j] = 0.f; }
+  // (a lane's partners are eight neighbours too, and so are its cosines, or four with pairs of neighbours)
+  const bool whole = (NEIGHBOURS ? a.rot : half) % kUnit == 0;
   if (live && turns) {
     const float* row = a.table + (long long)(known ? pos : 0) * a.rot;
+    if (whole) {
+      float c8[kUnit], s8[kUnit];
+      const int first = NEIGHBOURS ? e0 / 2 : e0 < half ? e0 : e0 - half;
+      if (NEIGHBOURS) {
+        const u32x4_t cv = *(const u32x4_at4_t*)(row + first), sv = *(const u32x4_at4_t*)(row + half + first);
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) {
-      const int e = e0 + j;
-      if (e >= a.rot) break;
-      const int pair = NEIGHBOURS ? e / 2 : e < half ? e : e - half;
-      const bool second = NEIGHBOURS ? (e & 1) != 0 : e >= half;
-      co[j] = known ? row[pair] : __uint_as_float(0x7FC00000u);
-      si[j] = second ? row[half + pair] : -row[half + pair];
+        for (int j = 0; j < kUnit; ++j) {
+          c8[j] = __uint_as_float(cv[j / 2]);
+          s8[j] = j % 2 ? __uint_as_float(sv[j / 2]) : -__uint_as_float(sv[j / 2]);
+        }
+      } else {
+        load_unit(row + first, c8);
+        load_unit(row + half + first, s8);
+        if (e0 < half)
+#pragma unroll
+          for (int j = 0; j < kUnit; ++j) s8[j] = -s8[j];
+      }
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) {
+        co[j] = known ? c8[j] : __uint_as_float(0x7FC00000u);
+        si[j] = s8[j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) {
+        const int e = e0 + j;
+        if (e >= a.rot) break;
+        const int pair = NEIGHBOURS ? e / 2 : e < half ? e : e - half;
+        const bool second = NEIGHBOURS ? (e & 1) != 0 : e >= half;
+        co[j] = known ? row[pair] : __uint_as_float(0x7FC00000u);
+        si[j] = second ? row[half + pair] : -row[half + pair];
+      }
     }
   }
-  const bool whole = NEIGHBOURS || half % kUnit == 0;  // a lane's partners are eight neighbours too
+  const bool swaps = !NEIGHBOURS && D == 128 && a.rot == D;  // the partners are in the lane eight further on in a row of 16
   float f[kMostHeads][kUnit];
 #pragma unroll
   for (int i = 0; i < kMostHeads; ++i) {
@@ -66,7 +92,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
                  : kind == 1 ? (const T*)a.k + (long long)token * a.k_stride[0] + (h - a.heads) * a.k_stride[1]
                              : (const T*)a.v + (long long)token * a.v_stride[0] + (h - a.heads - c.kv_heads) * a.v_stride[1];
     load_unit(x + e0, f[i]);
-    if (kind == 2 || !turns) continue;
+    if (kind == 2 || !turns || swaps) continue;
     float other[kUnit];
     if (NEIGHBOURS) {
 #pragma unroll
@@ -83,6 +109,19 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
 #pragma unroll
     for (int j = 0; j < kUnit; ++j)
       if (e0 + j < a.rot) f[i][j] = f[i][j] * co[j] + other[j] * si[j];
+  }
+  if (swaps) {
+#pragma unroll
+    for (int i = 0; i < kMostHeads; ++i) {
+      const int h = group * a.per_lane + i;
+      if (i >= a.per_lane) break;
+      const bool turned = h < a.heads + c.kv_heads;
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) {
+        const float other = dpp_move<0x128>(f[i][j]);  // (the lanes of a head are all here or none)
+        f[i][j] = turned ? f[i][j] * co[j] + other * si[j] : f[i][j];
+      }
+    }
   }
   wait_vm<0>();  // (all of the wave's reads)
   __builtin_amdgcn_wave_barrier();
