@@ -1,6 +1,6 @@
 """MI355X-native A2SF hot path: masked attention fused with forgotten-score bookkeeping and
 budgeted KV-cache eviction (arxiv 2407.20485), and the operators of a decoder layer around it (norm, 8-bit products,
-rotary positions, sampling).  All compute runs in liba2sf.so (HIP, gfx950)
+rotary positions, sampling), and a cache in pages that evicts nothing.  All compute runs in liba2sf.so (HIP, gfx950)
 behind the C ABI of include/a2sf.h; `binding` marshals arguments, `synth` draws workloads."""
 from .binding import (A2SF_BF16, A2SF_EVICT_FAST, A2SF_EVICT_STABLE, A2SF_F32, A2SF_MAX_CAPACITY,
                       A2SFError, Cache, a2sf_compact, a2sf_decode_step, a2sf_prefill, a2sf_select,

@@ -26,10 +26,12 @@ __device__ __forceinline__ f32x4_t mfma16(const uint4& a, const uint4& b, const 
 __device__ __forceinline__ f32x4_t mfma16(float a, float b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
+
 // ---- even shares ---------------------------------------------------------------------------------------------------------------------
 // The tokens that the sequences' rows see, in units, all pieces (a sequence's rows under one K/V head) one after the other, dealt out to the
-// workgroups evenly (4 sequences of 16000 .. 65536 tokens 133 us, 170 with each sequence cut into as many shares): a workgroup takes `per` units in a row, whatever pieces they are of.  What it has of a piece that is not whole goes to one of
-// two places of its own: the second if the piece goes on behind it, else the first.
+// workgroups evenly (4 sequences of 16000 .. 65536 tokens 133 us, 170 with each sequence cut into as many shares): a workgroup takes `per`
+// units in a row, whatever pieces they are of.  What it has of a piece that is not whole goes to one of two places of its own: the second if
+// the piece goes on behind it, else the first.
 __device__ __forceinline__ int units_of(const PagedArgs& a, int seq, int unit) {  // of a piece of the sequence
   const NewTokens t = new_tokens(a.c, seq);
   if (t.bad || t.past < 0) return 1;  // (there is something to write)
@@ -77,6 +79,7 @@ __device__ __forceinline__ EvenPlace even_place(const PagedArgs& a, int unit, in
       return {s + l, piece, at - start - piece * each, min(all.per, all.total - at)};
     }
     before += __builtin_amdgcn_readlane(upto, 63);
+    if (s + 64 >= a.c.sequences) return {0, 0, 0, 0};  // (only if lengths change under the call)
   }
 }
 
@@ -518,7 +521,9 @@ __global__ __launch_bounds__(64 * kRowWaves, D == 64 ? 3 : 2) void paged_rows_ke
       const NewTokens t = new_tokens(c, seq);
       Visible see = {0, 0, 0, 0};
       if (!t.bad && t.past >= 0) see = visible(t.past, t.past, a.window, a.sinks);
-      const int units = max(1, (see.count + F::UNIT - 1) / F::UNIT), u1 = units - u0 < left ? units : u0 + left;
+      const int units = max(1, (see.count + F::UNIT - 1) / F::UNIT);
+      if (u0 >= units) return;  // (only if lengths change under the call)
+      const int u1 = units - u0 < left ? units : u0 + left;
       const int part = u0 == 0 && u1 == units ? -1 : 2 * (int)blockIdx.x + (u1 < units);
       attend(seq, t, piece % c.kv_heads, piece / c.kv_heads * kRows, see, u0 * F::UNIT, min(see.count, u1 * F::UNIT), part);
       left -= u1 - u0;
@@ -527,7 +532,7 @@ __global__ __launch_bounds__(64 * kRowWaves, D == 64 ? 3 : 2) void paged_rows_ke
       u0 = 0;
       if (++piece == pieces) {
         piece = 0;
-        ++seq;
+        if (++seq >= c.sequences) return;  // (the same)
       }
     }
   }
@@ -631,8 +636,8 @@ size_t part_bytes(long long rows, int splits, int d) { return splits > 1 ? (size
 constexpr int kEvenGroups(int d) { return d == 64 ? 768 : 512; }  // as many as are on the chip at once
 constexpr int kPiecesEnough = 2048;
 int even_groups(long long pieces, long long most, int unit, int d) {
-  const long long units = (most + unit - 1) / unit;
-  return pieces >= kPiecesEnough || units < 2 ? 0 : (int)std::min((long long)kEvenGroups(d), pieces * units);
+  const long long units = (most + unit - 1) / unit;  // (all together are counted in 32 bits)
+  return pieces >= kPiecesEnough || units < 2 || pieces * units > 0x3FFFFFFF ? 0 : (int)std::min((long long)kEvenGroups(d), pieces * units);
 }
 size_t even_bytes(int groups, int group, int d) { return (size_t)groups * 2 * std::min(group, kRows) * (d + 2) * 4; }
 

@@ -29,8 +29,8 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, const NewToken
 }
 
 // The block of a rank: the sequences by their lengths, longer ones first, and in a sequence the blocks from its end, whose rows see most (up
-// to 64 sequences, one to a lane; the whole wave comes here).  What is begun last is then short.  (Blocks by what they see across the
-// sequences would end more evenly, but share no tiles in the caches: 4 prompts of up to 2048 tokens x us, y.)
+// to 64 sequences, one to a lane; the whole wave comes here).  What is begun last is then short, and blocks that
+// run together share their tiles in the caches.
 __device__ __forceinline__ RowBlock ranked_block(const PagedArgs& a, int rank) {
   const int lane = threadIdx.x & 63;
   int blocks = 0, len = -1;

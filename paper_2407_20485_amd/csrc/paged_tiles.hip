@@ -18,7 +18,6 @@
 namespace a2sf {
 namespace {
 
-typedef const __attribute__((address_space(3))) char* lds_in;
 typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
 __device__ __forceinline__ void lds_write16(lds_char* p, const uint4& v) { *reinterpret_cast<lds_u32x4*>(p) = u32x4_t{v.x, v.y, v.z, v.w}; }
 

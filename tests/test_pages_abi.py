@@ -103,7 +103,7 @@ def test_workspace_of_attention():
     assert f(4, 32, 8, 128, 4, 0) == 0 and f(1 << 40, 32, 8, 128, 4, 4096) == 0
     assert f(1, 32, 8, 128, 1, 16) == 0                                             # nothing to split
     one = f(1, 32, 8, 128, 1, 4096)
-    assert 0 < one <= 64 * 32 * 130 * 4 and one % 4 == 0
+    assert 0 < one <= 512 * 2 * 4 * 130 * 4 and one % 4 == 0                        # two places of a group's heads per workgroup
     assert f(4096, 32, 8, 128, 4096, 4096) == 0                                     # workgroups enough
 
 
