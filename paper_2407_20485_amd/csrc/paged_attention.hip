@@ -580,23 +580,25 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int unit) 
   for (int p0 = 0; p0 < parts; p0 += 64) {
     const int here = min(64, parts - p0);
     const f32x2_t ml = *(const f32x2_t*)(a.part_ml + 2 * place(p0 + min(lane, here - 1)));
+    f32x4_t v[4];
+    const auto ask = [&](int p) {  // (before the weights are known)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = *(const f32x4_t*)(a.part + place(p0 + min(p + i * NG, here - 1)) * D + 4 * x);
+    };
+    ask(side);
     const float mine = lane < here ? ml[0] : -FLT_MAX;
     const float m_new = fmaxf(m, wave_max(mine)), shrink = fast_exp2(m - m_new), k = lane < here ? fast_exp2(mine - m_new) : 0.f;
     m = m_new;
     l = l * shrink + wave_sum(lane < here ? k * ml[1] : 0.f);
     f *= shrink;
-    for (int p = side; p < here; p += 4 * NG) {
-      f32x4_t v[4];
-      float w[4];
+    for (int p = 0; p < here; p += 4 * NG) {  // (the whole wave: a weight comes from the lane that has it)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int q = p + i * NG;
-        v[i] = *(const f32x4_t*)(a.part + place(p0 + min(q, here - 1)) * D + 4 * x);
-        w[i] = __shfl(k, q & 63);
-        if (q >= here) v[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        const int q = p + side + i * NG;
+        const float w = __shfl(k, q & 63);
+        if (q < here) f += w * v[i];
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f += w[i] * v[i];
+      if (p + 4 * NG < here) ask(p + 4 * NG + side);
     }
   }
   if constexpr (WAVES == 1) {

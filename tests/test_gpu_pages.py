@@ -186,6 +186,18 @@ def test_single_tokens_of_a_long_sequence(dtype, eight, workspace):
     assert torch.equal(o, again)
 
 
+@pytest.mark.parametrize("parts", [2, 3, 7, 8, 9, 16, 31, 32, 33, 34, 40, 41, 63, 64, 65, 66, 97, 129])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_any_number_of_shares(dtype, d, parts):
+    """One sequence under one K/V head in so many shares: every one of them is added up."""
+    unit = 128 if dtype == "bf16" else 64
+    b = Batch(40, [(parts * unit - unit // 2, 1)], 1, d, 64, dtype, one_each=True).fill(scale=0.3)
+    attend(b, 2, scale=0.3)                      # logits of a tenth: each share has its part in the result
+    b = Batch(41, [(parts * unit - 40, 5)], 1, d, 64, dtype).fill(scale=0.3)
+    attend(b, 2, scale=0.3, one_product=True)
+
+
 @pytest.mark.parametrize("dtype,eight", KINDS)
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 5), (2, 1), (33, 0), (64, 4), (100, 70), (128, 1), (400, 2), (5000, 4)])
 def test_single_tokens_under_a_window(dtype, eight, window, sinks):
