@@ -327,7 +327,7 @@ a2sf_status a2sf_decode_plan(int32_t G, int32_t capacity, int32_t d, int32_t* ns
  *  - Where an input and an output are the same rows, every element is read before it is written.  Other overlaps are
  *    not allowed.
  *  - A launch takes less than 2^32 lanes, and what needs more is refused with A2SF_ESHAPE: a row of a2sf_rms_norm takes 64 to 1024 by its
- *    length, a row of a2sf_sample 1024, 128 columns of a2sf_quantize 16, 128 x 128 weights 256, 64 bytes of a token's heads in a2sf_rotary 1.
+ *    length, a row of a2sf_sample or a2sf_log_probs 1024, 128 columns of a2sf_quantize 16, 128 x 128 weights 256, 64 bytes of a token's heads in a2sf_rotary 1.
  *  - Sums, norms and products are formed in 32 bits or more whatever the type (a2sf_matmul_scaled: where the caller does not leave that
  *    to the 8-bit matrix instruction); results are rounded once. */
 typedef struct {
@@ -448,7 +448,7 @@ a2sf_status a2sf_sample(const a2sf_rows* logits, const a2sf_rows* noise, int32_t
  * A cache that keeps every token (or, under a window, the newest and a few first ones) of sequences of different lengths that come and
  * go: the baseline without eviction, and the local one.  Keys and values lie in pages of page_size tokens; a table says which
  * page holds a sequence's tokens 0 .. page_size - 1, page_size .. 2 page_size - 1, and so on.  The conventions of the operators around
- * the attention hold. */
+ * the attention hold.  At most 2^24 - 1 sequences and 2^28 - 1 tokens a call. */
 typedef struct {
   void* k;                    /* page p, head h, token t of the page: d elements from p * stride[0] + h * stride[1] + t * stride[2] on */
   void* v;                    /* laid out as k */
@@ -460,7 +460,7 @@ typedef struct {
   int32_t page_size;          /* tokens, a power of two, at most 65536 */
   int32_t kv_heads;
   int32_t d;                  /* 64 or 128 */
-  int32_t dtype;              /* that of the call's tensors, or A2SF_E4M3 */
+  int32_t dtype;              /* that of the call's tensors, or A2SF_E4M3 (read as bf16 by bf16 calls of several tokens: scale bytes of 10 to 246) */
 } a2sf_pages;
 
 /* Which sequences a call is about, and which of its tokens are theirs. */
@@ -480,8 +480,8 @@ typedef struct {
 } a2sf_heads;
 
 /* A sequence is bad if its length is negative or more than table_pages * page_size, or if it has a negative number of new tokens or more
- * of them than tokens.  Starts do not fall and lie in 0 .. the call's tokens; where two of them do, their sequence is bad, and rows of others
- * may be left alone.  Tokens of the call that no sequence has are left alone: nothing is written for them. */
+ * of them than tokens.  Starts do not fall and lie in 0 .. the call's tokens; where two of them fall, their sequence is bad, and rows of others may
+ * be left alone.  Tokens of the call that no sequence has are left alone: nothing is written for them. */
 
 /* New tokens: their keys and values go to their sequences' pages, k and q turned by their positions (a token's place in its sequence) on
  * the way, as a2sf_rotary turns them.
@@ -507,7 +507,7 @@ a2sf_status a2sf_paged_append(const a2sf_heads* q, const a2sf_heads* k, const a2
  *              0 for a place without a sequence.  An infinity or NaN in a row of v reaches the tokens that see it alone, as one or the other.
  *   workspace  may be NULL; with a2sf_paged_workspace_bytes() bytes calls of few rows split their tokens over more of the chip, with less into
  *              fewer parts.  The same sizes with the same workspace give the same bits.
- * Only pages with a token that some token of the call sees are looked up in the table and read. */
+ * What the table names for tokens that none of the call's sees does not matter, nor what lies there. */
 #define A2SF_NO_WINDOW 0x7FFFFFFF
 a2sf_status a2sf_paged_attention(const a2sf_heads* q, int32_t tokens, int32_t heads, int32_t dtype, const a2sf_sequences* sequences,
                                  const a2sf_pages* cache, int32_t window, int32_t sinks, const a2sf_heads* o, void* workspace,
