@@ -59,12 +59,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
     head = kv * a.group + row % a.group;
     return r < rows && token >= 0 && token < c.tokens;
   };
-  if (t.bad || t.past < 0) {
+  if (t.bad) {
     if (a.splits == 1)
       for (int e = tid; e < rows * D; e += kThreads) {
         int token, head;
-        if (place(e / D, token, head))
-          store_one((bf16_t*)a.o + token * a.o_stride[0] + head * a.o_stride[1] + e % D, t.bad ? kNan : 0.f);
+        if (place(e / D, token, head)) store_one((bf16_t*)a.o + token * a.o_stride[0] + head * a.o_stride[1] + e % D, kNan);
       }
     return;
   }
@@ -148,10 +147,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
   uint32_t both[EIGHT ? NE : 1];
   const auto request = [&](int i, int pages) {  // 8 bits
     const int base = base_of(i);
+    int thread = tid;
+    asm volatile("" : "+v"(thread));  // (what is formed of it is not kept over the loop: 8192 tokens 755 us, 679 so)
     const int sound = (uint32_t)pages < (uint32_t)c.pages ? pages : 0;
 #pragma unroll
     for (int u = 0; u < NE; ++u) {
-      const int r = (u * kThreads + tid) / (D / 16), col = tid % (D / 16);
+      const int r = (u * kThreads + thread) / (D / 16), col = thread % (D / 16);
       const long long page = __shfl(sound, r), in_page = (base + r) & mask_in_page;
       const long long at = page * c.stride[0] + in_page * c.stride[2] + col * 16;
       const long long s = page * c.scale_stride[0] + kv * c.scale_stride[1] + in_page * c.scale_stride[2];
@@ -161,9 +162,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
     }
   };
   const auto deliver = [&](lds_char* kt, lds_char* vt) {
+    int thread = tid;
+    asm volatile("" : "+v"(thread));  // (the same)
 #pragma unroll
     for (int u = 0; u < NE; ++u) {
-      const int r = (u * kThreads + tid) / (D / 16), col = tid % (D / 16);
+      const int r = (u * kThreads + thread) / (D / 16), col = thread % (D / 16);
       // (a power of two: values in bf16 are exact, from its subnormal numbers to where its range ends)
       const auto unpack = [&](const uint4& x, uint32_t byte, uint4& lo, uint4& hi) {
         const float scale = scale_value(byte);

@@ -96,16 +96,9 @@ struct RowBlock {
   int seq, first_row;  // of the sequence's
   bool any;            // there is such a block
 };
-// Block b of the call: blocks of one sequence after the other.  The whole wave comes here with the same b.
+// Block b of a call with starts: blocks of one sequence after the other.  The whole wave comes here with the same b.
 __device__ __forceinline__ RowBlock row_block(const PagedCache& c, int group, int rows, int b) {
   RowBlock r = {0, 0, false};
-  if (!c.starts) {
-    const int per = (group + rows - 1) / rows;
-    r.seq = b / per;
-    r.first_row = (b - r.seq * per) * rows;
-    r.any = r.seq < c.sequences;
-    return r;
-  }
   const int lane = threadIdx.x & 63;
   long long before = 0;
   for (int s = 0; s < c.sequences; s += 64) {
