@@ -90,7 +90,7 @@ __device__ __forceinline__ EvenPlace even_place(const PagedArgs& a, int unit, in
 // of V being read by 16 lanes side by side; a pair of tokens' values of one dimension is one byte permutation.
 // So neither P nor V goes through LDS.  Q and K take their dimensions in the order in which K's 16 bytes per lane come.
 // bf16: P goes into the product as two bf16 numbers, its value and what that leaves out (2^-17 of it stays out): the matrix pipe has room.
-// Bound by memory: 4 x 65536 tokens of 8 K/V heads 119 us = 6.1 TB/s, 200 x 1004 of 40 heads 646 = 6.4; in 8 bits 5.2.  A wave has one tile's
+// Bound by memory: 4 x 65536 tokens of 8 K/V heads 119 us = 6.1 TB/s, 200 x 1004 of 40 heads 660 = 6.2; in 8 bits 5.3.  A wave has one tile's
 // K and V in registers and asks for the next K when it has used this one's (two tiles at a time take 256 registers and spill: 200 x 1004
 // 745 us without streaming loads and 951 with them).
 constexpr int kRows = 16;
