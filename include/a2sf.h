@@ -329,7 +329,7 @@ a2sf_status a2sf_decode_plan(int32_t G, int32_t capacity, int32_t d, int32_t* ns
  *  - A launch takes less than 2^32 lanes, and what needs more is refused with A2SF_ESHAPE: a row of a2sf_rms_norm takes 64 to 1024 by its
  *    length, a row of a2sf_sample or a2sf_log_probs 1024, 128 columns of a2sf_quantize 16, 128 x 128 weights 256, 64 bytes of a token's heads in a2sf_rotary 1.
  *  - Sums, norms and products are formed in 32 bits or more whatever the type (a2sf_matmul_scaled: where the caller does not leave that
- *    to the 8-bit matrix instruction); results are rounded once. */
+ *    to the 8-bit matrix instruction; a2sf_paged_attention: the probabilities of bf16 calls, as stated there); results are rounded once. */
 typedef struct {
   void* data;
   int64_t stride; /* elements from row to row */
@@ -384,7 +384,7 @@ a2sf_status a2sf_quantize_weight(const a2sf_rows* w, int32_t n, int32_t k, int32
  *              that have too few tiles for the whole chip split their sums over k; with less, if their own parts fit.  The same sizes with
  *              the same choices give the same bits.
  * Bytes of the rows past k are not used.  k <= 2^20, rows of a and b and rows of scales at most 2^23 bytes apart. */
-#define A2SF_WIDE_SUMS 0x100 /* or'ed to c_dtype */
+#define A2SF_WIDE_SUMS 0x100 /* or'ed to c_dtype, and to the dtype of a2sf_paged_attention */
 size_t a2sf_matmul_workspace_bytes(int32_t m, int32_t n, int32_t k);
 a2sf_status a2sf_matmul_scaled(const a2sf_rows8* a, const a2sf_rows8* b, int32_t m, int32_t n, int32_t k,
                                const a2sf_rows* c, int32_t c_dtype, void* workspace, size_t workspace_bytes,
@@ -501,6 +501,9 @@ a2sf_status a2sf_paged_append(const a2sf_heads* q, const a2sf_heads* k, const a2
 /* Attention of each sequence's newest tokens (already appended) over its pages: o_i = sum_j softmax_j(q_i . k_j / sqrt(d)) v_j over the
  * tokens j that token i sees: j <= i, and j > i - window or j < sinks (the window counts the token itself).
  *   q          [tokens, heads, d] dtype, heads a multiple of cache->kv_heads: query head h reads K/V head h / (heads / kv_heads).
+ *   dtype      A2SF_F32 or A2SF_BF16.  Logits, maxima and sums are in 32 bits.  What a probability p is multiplied with v as: of fp32 calls 32
+ *              bits; of bf16 calls without starts two bf16 numbers, within 2^-17 p; of bf16 calls with starts one, within 2^-8 p (so o is
+ *              within 2^-8 sum p |v| before it is rounded to bf16), or with A2SF_BF16 | A2SF_WIDE_SUMS two (1.1 to 1.3 times the time).
  *   window     >= 1; A2SF_NO_WINDOW: every earlier token.
  *   sinks      >= 0: first tokens that stay visible.
  *   o          out [tokens, heads, d] dtype.  NaN for a bad sequence, and for a token that sees one whose page is none of the cache's;

@@ -706,10 +706,12 @@ def a2sf_paged_append(q, k, v, cache, table, lens, starts=None, q_out=None, rota
                                    _stream_of(k, stream)))
 
 
-def a2sf_paged_attention(q, cache, table, lens, o, starts=None, window=None, sinks=0, workspace=None, workspace_bytes=None, stream=None):
-    """window: tokens that a token sees, itself among them (None: all)."""
+def a2sf_paged_attention(q, cache, table, lens, o, starts=None, window=None, sinks=0, workspace=None, workspace_bytes=None, stream=None,
+                         wide_sums=False):
+    """window: tokens that a token sees, itself among them (None: all).  wide_sums: bfloat16 calls with starts hold probabilities to 2^-17 as
+    those without do (A2SF_WIDE_SUMS)."""
     at = _entry("a2sf_paged_attention")
-    status = _call.paged_attention(at, q, cache, table, lens, o, starts, window, sinks, workspace, workspace_bytes, stream)
+    status = _call.paged_attention(at, q, cache, table, lens, o, starts, window, sinks, workspace, workspace_bytes, stream, wide_sums)
     if status >= 0:
         return _check(status)
     _need(q.dim() == 3 and q.shape[2] == cache.d)
@@ -721,9 +723,9 @@ def a2sf_paged_attention(q, cache, table, lens, o, starts=None, window=None, sin
         workspace_bytes = workspace.nbytes if workspace is not None else 0
     if isinstance(workspace, torch.Tensor):
         _reach(workspace, q)
-    _check(lib().a2sf_paged_attention(_heads(q, q), tokens, heads, dtype_code(q.dtype), _sequences(table, lens, starts, q),
-                                      ctypes.byref(cache.struct), window, sinks, _heads(o, q, heads), _ptr(workspace), workspace_bytes,
-                                      _stream_of(q, stream)))
+    _check(lib().a2sf_paged_attention(_heads(q, q), tokens, heads, dtype_code(q.dtype) | (A2SF_WIDE_SUMS if wide_sums else 0),
+                                      _sequences(table, lens, starts, q), ctypes.byref(cache.struct), window, sinks, _heads(o, q, heads),
+                                      _ptr(workspace), workspace_bytes, _stream_of(q, stream)))
 
 
 def a2sf_paged_workspace_bytes(tokens, heads, kv_heads, d, sequences, table_tokens) -> int:

@@ -253,6 +253,7 @@ struct PagedArgs {
   void* o;
   long long q_stride[2], o_stride[2];
   int heads, group, window, sinks;
+  bool wide;  // probabilities as two bf16 numbers in the tile form too
   float scale_log2e;
   // set by the launcher
   float *part, *part_ml;  // sums of parts of rows, their maxima and weights: [rows][splits] (a row is a (token, head)) or [even][2][part_rows]

@@ -3,8 +3,10 @@
 // matrix instruction, a lane holding one query row and 16 of 32 tokens, an online softmax whose maximum moves only when it has to.
 //
 // A block's rows are the heads of a K/V head's group, token by token, so a tile of K and V serves all heads of the group at once.
-// Probabilities go into the second product as bf16 numbers (2^-9 of each on the average, at random; a second number each would cost a half
-// more of the matrix pipe, which bounds this kernel); their sum is of the unrounded ones.
+// Probabilities go into the second product as bf16 numbers, each within 2^-8 of itself, or with WIDE as two, its value and what that
+// leaves out (2^-17 of it stays out); their sum is of the unrounded ones.  The caller chooses: the second number is a half more matrix
+// instructions and three vector instructions a pair (4 prompts of up to 2048 tokens, 32 heads: 110 us without, 134 with it; 16384 tokens under a window of 2048
+// 587 and 736, without a window 2104 and 2774; 8192 tokens over pages of 8 bits 627 and 781; a chunk of 512 with 15 single tokens 92 and 102).
 #include <float.h>
 
 #include <algorithm>
@@ -31,7 +33,7 @@ __device__ __forceinline__ uint32_t without_odd(uint32_t w) {
 }
 
 // D: head dimension; EIGHT: pages of 8 bits, whose rows are unpacked to bf16 (with their scales) on their way into LDS.
-template <int D, bool EIGHT>
+template <int D, bool EIGHT, bool WIDE>
 __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
   constexpr int KK = D / 16, DB = D / 32, ROW = D * 2, kTB = kTile * ROW;
   constexpr int RPL = 512 / D, NL = kTile / (4 * RPL);     // rows of a direct load, loads of a wave
@@ -216,7 +218,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
       if (i + kPrefetch < NF) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
   };
-  const auto add_values = [&](const lds_char* vt, const uint32_t (&pf)[16]) {  // O += V^T P
+  constexpr int kNumbers = WIDE ? 2 : 1;  // of a probability
+  const auto add_values = [&](const lds_char* vt, const uint32_t (&pf)[kNumbers][16]) {  // O += V^T P
     constexpr int NF = DB * 4;  // fragment i = (kb, tt, db), db fastest
     uint2 lo[NF], hi[NF];
     const auto vread = [&](int i, uint2& x, uint2& y) {
@@ -230,12 +233,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
     for (int i = 0; i < NF; ++i) {
       if (i + kPrefetch < NF) vread(i + kPrefetch, lo[i + kPrefetch], hi[i + kPrefetch]);
       const int w = 4 * (i / DB);
-      oacc[i % DB] = mfma_bf16(make_uint4(lo[i].x, lo[i].y, hi[i].x, hi[i].y), make_uint4(pf[w], pf[w + 1], pf[w + 2], pf[w + 3]), oacc[i % DB]);
+#pragma unroll
+      for (int p = 0; p < kNumbers; ++p)
+        oacc[i % DB] = mfma_bf16(make_uint4(lo[i].x, lo[i].y, hi[i].x, hi[i].y), make_uint4(pf[p][w], pf[p][w + 1], pf[p][w + 2], pf[p][w + 3]),
+                                 oacc[i % DB]);
     }
     __builtin_amdgcn_sched_group_barrier(0x100, 2 * kPrefetch, 0);
 #pragma unroll
     for (int i = 0; i < NF; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kNumbers, 0);
       if (i + kPrefetch < NF) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
   };
@@ -336,7 +342,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
         for (int e = 0; e < 16; ++e) oacc[db][e] *= shrink;
       m = m_new;
     }
-    uint32_t pf[16];
+    uint32_t pf[kNumbers][16];
     float rs = 0.f;
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
@@ -344,7 +350,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
       const float e1 = fast_exp2(fmaf(s[j >> 3][(2 * j + 1) & 15], a.scale_log2e, -m));
       rs += e0;
       rs += e1;
-      pf[j] = pack_bf16(e0, e1);
+      const uint32_t both = pack_bf16(e0, e1);
+      pf[0][j] = both;
+      if constexpr (WIDE) pf[1][j] = pack_bf16(e0 - __uint_as_float(both << 16), e1 - __uint_as_float(both & 0xFFFF0000u));
     }
     lsum += rs;
     add_values(vt, pf);
@@ -429,15 +437,21 @@ __global__ __launch_bounds__(kThreads, 2) void paged_tiles_kernel(PagedArgs a) {
 
 }  // namespace
 
-void launch_paged_tiles(const PagedArgs& a, uint32_t grid, hipStream_t st) {
+template <bool WIDE>
+void tiles(const PagedArgs& a, uint32_t grid, hipStream_t st) {
   const bool eight = a.c.dtype == A2SF_E4M3;
   if (a.c.d == 128) {
-    if (eight) paged_tiles_kernel<128, true><<<grid, kThreads, 0, st>>>(a);
-    else paged_tiles_kernel<128, false><<<grid, kThreads, 0, st>>>(a);
+    if (eight) paged_tiles_kernel<128, true, WIDE><<<grid, kThreads, 0, st>>>(a);
+    else paged_tiles_kernel<128, false, WIDE><<<grid, kThreads, 0, st>>>(a);
   } else {
-    if (eight) paged_tiles_kernel<64, true><<<grid, kThreads, 0, st>>>(a);
-    else paged_tiles_kernel<64, false><<<grid, kThreads, 0, st>>>(a);
+    if (eight) paged_tiles_kernel<64, true, WIDE><<<grid, kThreads, 0, st>>>(a);
+    else paged_tiles_kernel<64, false, WIDE><<<grid, kThreads, 0, st>>>(a);
   }
+}
+
+void launch_paged_tiles(const PagedArgs& a, uint32_t grid, hipStream_t st) {
+  if (a.wide) tiles<true>(a, grid, st);
+  else tiles<false>(a, grid, st);
 }
 
 }  // namespace a2sf

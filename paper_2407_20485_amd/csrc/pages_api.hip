@@ -139,6 +139,8 @@ a2sf_status a2sf_paged_append(const a2sf_heads* q, const a2sf_heads* k, const a2
 a2sf_status a2sf_paged_attention(const a2sf_heads* q, int32_t tokens, int32_t heads, int32_t dtype, const a2sf_sequences* sequences,
                                  const a2sf_pages* cache, int32_t window, int32_t sinks, const a2sf_heads* o, void* workspace,
                                  size_t workspace_bytes, void* hip_stream) {
+  const bool wide = (dtype & A2SF_WIDE_SUMS) != 0;
+  dtype &= ~A2SF_WIDE_SUMS;
   A2SF_TRY(check_pages(cache, dtype));
   A2SF_TRY(check_sequences(sequences, tokens, cache));
   A2SF_TRY(check_heads(q, tokens, heads, cache->d, dtype));
@@ -159,6 +161,7 @@ a2sf_status a2sf_paged_attention(const a2sf_heads* q, int32_t tokens, int32_t he
   a.group = heads / cache->kv_heads;
   a.window = window;
   a.sinks = sinks;
+  a.wide = wide;
   a.scale_log2e = 1.44269504088896340736f / sqrtf((float)cache->d);
   return launched([&] { return launch_paged_attention(a, dtype, workspace, workspace ? workspace_bytes : 0, (hipStream_t)hip_stream); });
 }

@@ -441,9 +441,9 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (entry point, q, cache, table, lens, o, starts, window, sinks, workspace, workspace_bytes, stream)
+// (entry point, q, cache, table, lens, o, starts, window, sinks, workspace, workspace_bytes, stream[, wide_sums])
 PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!expects(n, 12)) return nullptr;
+  if (n != 13 && !expects(n, 12)) return nullptr;
   return guarded([&] {
     void *ws, *st, *fn = PyLong_AsVoidPtr(a[0]);
     const at::Tensor *q, *room;
@@ -454,8 +454,10 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     size_t bytes;
     if (!(fn && first_heads(a[1], a[2], &q, &dtype, &pages) && heads_like(a[1], *q, 0, &hq) && heads_like(a[5], *q, q->size(1), &ho) &&
           sequences(a[3], a[4], a[6], *q, &s) && (a[7] == Py_None || number(a[7], &window)) && number(a[8], &sinks) &&
-          workspace(a[9], a[10], &ws, &bytes) && (!tensor(a[9], &room) || room->device() == q->device()) && stream(a[11], a[1], &st)))
+          workspace(a[9], a[10], &ws, &bytes) && (!tensor(a[9], &room) || room->device() == q->device()) && stream(a[11], a[1], &st) &&
+          (n == 12 || PyBool_Check(a[12]))))
       return -1;
+    if (n == 13 && a[12] == Py_True) dtype |= A2SF_WIDE_SUMS;
     return without_gil([&]() -> int {
       return ((decltype(&a2sf_paged_attention))fn)(&hq, (int32_t)q->size(0), (int32_t)q->size(1), dtype, &s, pages, window, sinks, &ho, ws,
                                                    bytes, st);

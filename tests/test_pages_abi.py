@@ -97,6 +97,15 @@ def test_attention_refusals():
     assert attend(tokens=0x7FFFFFF, h=32 * 8, seqs=sequences(starts=FAKE)) == B.A2SF_ESHAPE
 
 
+def test_choice_of_probabilities_is_checked_with_the_type():
+    wide = B.A2SF_WIDE_SUMS
+    assert attend(dtype=7 | wide) == B.A2SF_EDTYPE and attend(dtype=B.A2SF_E4M3 | wide) == B.A2SF_EDTYPE
+    assert attend(dtype=B.A2SF_BF16 | 0x200) == B.A2SF_EDTYPE
+    assert append(dtype=B.A2SF_BF16 | wide) == B.A2SF_EDTYPE                        # nothing to choose
+    for dtype in (B.A2SF_BF16, B.A2SF_F32):
+        assert attend(dtype=dtype | wide, cache=pages(dtype=dtype), window=0) == B.A2SF_EINVAL
+
+
 def test_workspace_of_attention():
     f = B.a2sf_paged_workspace_bytes
     assert f(0, 32, 8, 128, 4, 4096) == 0 and f(4, 33, 8, 128, 4, 4096) == 0 and f(4, 32, 8, 96, 4, 4096) == 0
