@@ -509,7 +509,8 @@ a2sf_status a2sf_paged_append(const a2sf_heads* q, const a2sf_heads* k, const a2
  *   o          out [tokens, heads, d] dtype.  NaN for a bad sequence, and for a token that sees one whose page is none of the cache's;
  *              0 for a place without a sequence.  An infinity or NaN in a row of v reaches the tokens that see it alone, as one or the other.
  *   workspace  may be NULL; with a2sf_paged_workspace_bytes() bytes calls of few rows split their tokens over more of the chip, with less into
- *              fewer parts.  The same sizes with the same workspace give the same bits.
+ *              fewer parts, and single tokens of up to 512 sequences, some of which may be much longer than others (by the size of the table), share
+ *              it evenly.  The same sizes with the same workspace give the same bits.
  * What the table names for tokens that none of the call's sees does not matter, nor what lies there. */
 #define A2SF_NO_WINDOW 0x7FFFFFFF
 a2sf_status a2sf_paged_attention(const a2sf_heads* q, int32_t tokens, int32_t heads, int32_t dtype, const a2sf_sequences* sequences,

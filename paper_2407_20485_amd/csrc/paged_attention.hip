@@ -633,13 +633,20 @@ int splits_for(long long groups, long long most, int unit, int wanted) {
 }
 constexpr int kFewestTiles = 4;  // of a share
 size_t part_bytes(long long rows, int splits, int d) { return splits > 1 ? (size_t)rows * splits * (d + 2) * 4 : 0; }
-// One token of each: workgroups that share the tokens evenly, 0 where there are pieces enough to go round as they are, or no piece has more
-// than a unit
+// One token of each: workgroups that share the tokens evenly, or 0 where a piece goes to each workgroup: if no piece has more than a unit, or if
+// there are two pieces and more for each workgroup on the chip and none can be so long that it runs on alone, or the lengths are too many to be
+// scanned by all.  us, a piece to each / even shares, 128 and 256 sequences on 8 K/V heads of d = 128 in tables for 8192 tokens (4 and 8 a piece
+// of the call): one of 8192 beside others of 300 tokens 132 / 47 and 143 / 81, all of 300 32 / 37 and 60 / 71, of 75 to 300 up to 1000 66 / 75 and 122 / 139; in tables for
+// 65536: one such beside 500 937 / 94 and 954 / 144.  1024 sequences of 300 on one head 32 / 53.
 constexpr int kEvenGroups(int d) { return d == 64 ? 768 : 512; }  // as many as are on the chip at once
-constexpr int kPiecesEnough = 2048;
-int even_groups(long long pieces, long long most, int unit, int d) {
-  const long long units = (most + unit - 1) / unit;  // (all together are counted in 32 bits)
-  return pieces >= kPiecesEnough || units < 2 || pieces * units > 0x3FFFFFFF ? 0 : (int)std::min((long long)kEvenGroups(d), pieces * units);
+constexpr int kLongPiece = 4;          // tokens for each piece of the call
+constexpr int kScannedLengths = 512;
+constexpr long long kMostUnits = 0x3FFFFFFF;  // (counted in 32 bits)
+int even_groups(long long pieces, long long most, int unit, int d, int sequences) {
+  const long long units = (most + unit - 1) / unit;
+  if (units < 2 || pieces * units > kMostUnits) return 0;
+  if (pieces >= 2 * kEvenGroups(d) && (most < kLongPiece * pieces || sequences > kScannedLengths)) return 0;
+  return (int)std::min((long long)kEvenGroups(d), pieces * units);
 }
 size_t even_bytes(int groups, int group, int d) { return (size_t)groups * 2 * std::min(group, kRows) * (d + 2) * 4; }
 
@@ -658,8 +665,9 @@ bool attend(PagedArgs a, void* workspace, size_t bytes, hipStream_t st) {
   a.part = (float*)workspace;
   unsigned long long grid = (unsigned long long)groups;
   if (!a.c.starts) {
-    a.even = (int)std::min((unsigned long long)even_groups(groups, most, F::UNIT, D), (unsigned long long)(bytes / even_bytes(1, a.group, D)));
-    if (a.even <= groups / 2) a.even = 0;  // too little room to be of use
+    const int wanted = even_groups(groups, most, F::UNIT, D, a.c.sequences);
+    a.even = (int)std::min((unsigned long long)wanted, (unsigned long long)(bytes / even_bytes(1, a.group, D)));
+    if (a.even <= std::min(groups, (long long)wanted) / 2) a.even = 0;  // too little room to be of use
     if (a.even) grid = a.even;
     a.part_ml = a.part + 2ll * a.even * a.part_rows * D;
   } else {
@@ -701,7 +709,9 @@ size_t paged_workspace(int tokens, int heads, int kv_heads, int d, int sequences
   size_t most = std::max(bytes(false, kRows, 16 * kRowWaves, kWantedGroups), bytes(false, kTileRows, kFewestTiles * kTileTokens, kWantedTileGroups));
   if (tokens == sequences) {
     const long long pieces = (long long)row_blocks(tokens, heads / kv_heads, sequences, true, kRows) * kv_heads;
-    most = std::max(most, even_bytes(even_groups(pieces, table_tokens, 16 * kRowWaves, d), heads / kv_heads, d));
+    const int unit = 16 * kRowWaves;
+    const long long counted = std::min(table_tokens, kMostUnits / pieces * unit);  // (a call under a window may have few enough)
+    most = std::max(most, even_bytes(even_groups(pieces, counted, unit, d, sequences), heads / kv_heads, d));
   }
   return most;
 }

@@ -50,3 +50,43 @@ def test_wide_sums_through_ctypes(monkeypatch):
     monkeypatch.setattr(B, "_call", B._NoExtension)
     got.append(run(b, q, wide_sums=True))
     assert torch.equal(*got)
+
+
+# ---- single tokens of many sequences ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("sequences,kv,group,d,dtype,eight,longest",
+                         [(130, 8, 1, 128, "bf16", False, 4200), (200, 8, 1, 64, "bf16", False, 6500), (129, 8, 2, 128, "bf16", True, 4200),
+                          (130, 8, 1, 128, "f32", False, 4200), (512, 2, 3, 128, "bf16", False, 4100), (140, 16, 1, 64, "f32", True, 9000)])
+def test_many_pieces_of_unequal_lengths(sequences, kv, group, d, dtype, eight, longest):
+    """More than 1024 and 2048 pieces (d = 64: 1536), one of them a hundred times as long as the others: dealt out evenly, through the
+    workspace that was asked for; the same bits again, and without a workspace the same values."""
+    g = np.random.default_rng(sequences)
+    past = g.integers(10, 2 * longest // 100, sequences)
+    lengths = [(int(p), 1) if i % 17 else (0, 0) for i, p in enumerate(past)]
+    lengths[sequences // 3] = (longest - 1, 1)
+    b = Batch(54, lengths, kv, d, 64, dtype, eight, one_each=True).fill()
+    q, _ = strided(b.tokens, kv * group, d, b.dt, g, 2.0)
+    ws = space(b, kv * group)
+    assert ws.numel() > 0
+    o = run(b, q, workspace=ws)
+    assert not bool((ws == 0xFF).all())
+    check_attention(b, q, o, 1 << 30, 0)
+    assert torch.equal(o, run(b, q, workspace=ws))
+    plain = run(b, q)
+    check_attention(b, q, plain, 1 << 30, 0)
+    assert bool((o[[i for i in range(sequences) if i % 17 == 0 and i != sequences // 3]] == 0).all())
+
+
+def test_many_pieces_with_too_little_room():
+    """Room for fewer workgroups than half of those that would share: a piece to each, the workspace is left alone."""
+    lengths = [(20 + i % 50, 1) for i in range(130)]
+    lengths[7] = (4300, 1)
+    b = Batch(55, lengths, 8, 128, 64, "bf16", one_each=True).fill()
+    q, _ = strided(b.tokens, 8, 128, b.dt, np.random.default_rng([55, 1]), 2.0)
+    ws = space(b, 8)
+    of_one = 2 * (128 + 2) * 4                                   # of a workgroup: two places for a row
+    few, most = ws[: 200 * of_one], ws[: 400 * of_one]          # 512 share where there is room
+    check_attention(b, q, run(b, q, workspace=few), 1 << 30, 0)
+    assert bool((ws == 0xFF).all())
+    check_attention(b, q, run(b, q, workspace=most), 1 << 30, 0)
+    assert not bool((most == 0xFF).all()) and bool((ws[most.numel():] == 0xFF).all())

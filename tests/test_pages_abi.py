@@ -116,6 +116,18 @@ def test_workspace_of_attention():
     assert f(4096, 32, 8, 128, 4096, 4096) == 0                                     # workgroups enough
 
 
+def test_workspace_of_many_pieces():
+    """Two pieces and more for each workgroup: of use only where the table has room for long ones, and then whatever the window."""
+    f = B.a2sf_paged_workspace_bytes
+    shares = lambda d, g: (768 if d == 64 else 512) * 2 * g * (d + 2) * 4  # noqa: E731
+    for sequences, kv, d, longest in ((255, 8, 128, 8160), (400, 8, 128, 12800), (300, 8, 64, 9600), (512, 16, 128, 32768)):
+        assert f(sequences, 2 * kv, kv, d, sequences, longest) == shares(d, 2)
+        assert f(sequences, 2 * kv, kv, d, sequences, longest - 1) == 0
+    assert f(127, 16, 8, 128, 127, 300) >= shares(128, 2)                           # fewer: each is cut
+    assert f(513, 16, 8, 128, 513, 1 << 20) == 0                                    # too many lengths to look at
+    assert f(512, 4, 4, 128, 512, (1 << 31) - 512) == shares(128, 1)                # a window may leave few enough of them
+
+
 def test_log_probs_refusals():
     r = lambda data=FAKE, stride=256: ref(B.Rows(data, stride))  # noqa: E731
 
