@@ -631,7 +631,6 @@ int splits_for(long long groups, long long most, int unit, int wanted) {
   const long long want = (wanted + groups - 1) / groups, units = (most + unit - 1) / unit;
   return (int)std::max(1ll, std::min({want, units, (long long)kMostSplits}));
 }
-constexpr int kFewestTiles = 4;  // of a share
 size_t part_bytes(long long rows, int splits, int d) { return splits > 1 ? (size_t)rows * splits * (d + 2) * 4 : 0; }
 // One token of each: workgroups that share the tokens evenly, or 0 where a piece goes to each workgroup: if no piece has more than a unit, or if
 // there are two pieces and more for each workgroup on the chip and none can be so long that it runs on alone, or the lengths are too many to be

@@ -6,6 +6,9 @@ namespace a2sf {
 
 constexpr int kTileRows = 128;   // query rows of a workgroup
 constexpr int kTileTokens = 64;
+// Tiles of a share, unless the block has fewer (us with 1 / 2 / 4 / 8 of them, 32 heads on 8: 512 tokens in a table for 65536 34 / 29 / 28 / 31,
+// 64 behind 1000 25 / 21 / 22 / 27, four of those 29 / 23 / 24 / 27, 16 x 4 behind 500 22 / 21 / 25 / 28, 512 behind 8192 105 with any)
+constexpr int kFewestTiles = 2;
 
 // The tiles of a block of rows: those of the first `sinks` tokens, if they lie apart, then those from token `from` (a multiple of eight, so
 // that eight rows are in one page) to the block's newest token.
@@ -23,7 +26,7 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, const NewToken
   p.sink_tiles = (p.sinks + kTileTokens - 1) / kTileTokens;
   if (p.sinks >= p.from) p.from = p.sink_tiles = 0;
   p.tiles = p.sink_tiles + (p1 - p.from) / kTileTokens + 1;
-  p.per = (p.tiles + a.splits - 1) / a.splits;
+  p.per = max(kFewestTiles, (p.tiles + a.splits - 1) / a.splits);  // (the table may have room for many more than there are)
   p.parts = (p.tiles + p.per - 1) / p.per;
   return p;
 }

@@ -90,3 +90,36 @@ def test_many_pieces_with_too_little_room():
     assert bool((ws == 0xFF).all())
     check_attention(b, q, run(b, q, workspace=most), 1 << 30, 0)
     assert not bool((most == 0xFF).all()) and bool((ws[most.numel():] == 0xFF).all())
+
+
+# ---- shares of prompts and chunks ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("past,new", [(448, 64), (0, 64), (200, 100), (900, 17)])
+def test_shares_in_a_table_with_room_for_more(past, new, eight):
+    """A share has at least two tiles of 64 tokens also where the table has room for a thousand: no row has more parts than that gives."""
+    b = Batch(56, [(past, new)], 1, 128, 64, "bf16", eight).fill()
+    wide = torch.full((1, 1024), -1, dtype=torch.int32, device="cuda")
+    wide[:, : b.table.shape[1]] = b.table
+    b.table = wide
+    q, _ = strided(b.tokens, 4, 128, b.dt, np.random.default_rng([56, 1]), 2.0)
+    ws = space(b, 4)
+    check_attention(b, q, run(b, q, workspace=ws), 1 << 30, 0, one_product=True)
+    written = int((ws.view(torch.int32) != -1).sum())
+    tiles = -(-(past + new) // 64)
+    assert written <= b.tokens * 4 * -(-tiles // 2) * (128 + 2)
+
+
+@pytest.mark.parametrize("dtype,eight,wide", [("bf16", False, False), ("bf16", True, True), ("f32", False, False)])
+@pytest.mark.parametrize("share", [0.02, 0.1, 0.4, 0.7])
+def test_chunks_with_less_workspace(dtype, eight, wide, share):
+    """Less room than the shares of a chunk would take: fewer of them, and nothing behind the room is written."""
+    b = Batch(57, [(1900, 40), (700, 1), (0, 90)], 2, 64, 32, dtype, eight).fill()
+    q, _ = strided(b.tokens, 6, 64, b.dt, np.random.default_rng([57, 1]), 2.0)
+    ws = space(b, 6)
+    some = ws[: int(ws.numel() * share) // 16 * 16]
+    for window, sinks in ((None, 0), (300, 5)):
+        check_attention(b, q, run(b, q, window, sinks, some, wide), window or 1 << 30, sinks, one_product=not wide and dtype == "bf16")
+    assert bool((ws[some.numel():] == 0xFF).all())
+    if share > 0.5:
+        assert not bool((some == 0xFF).all())
