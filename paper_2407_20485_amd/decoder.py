@@ -89,6 +89,8 @@ class Decoder:
     def start_paged(self, sequences, capacity, page_size=64, window=None, sinks=0, eight=False):
         """Empty pages for `sequences` sequences of up to `capacity` tokens each, which nothing is evicted from; a window: a token sees the
         newest `window` ones and the first `sinks`.  eight: keys and values in 8 bits."""
+        if capacity > self.table.shape[0]:
+            raise ValueError(f"sequences of {capacity} tokens: the decoder was made for {self.table.shape[0]} positions")
         c, per = self.config, -(-capacity // page_size)
         kind = torch.float8_e4m3fn if eight else torch.bfloat16
         self.pages = [B.Pages(sequences * per, page_size, c.kv_heads, c.d, kind) for _ in self.layers]
