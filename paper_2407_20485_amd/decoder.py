@@ -180,8 +180,8 @@ class Decoder:
         starts = [0]
         for n in counts:
             starts.append(starts[-1] + n)
-        self.lengths = [have + n for have, n in zip(self.lengths, counts)]
-        lens = torch.tensor(self.lengths, dtype=torch.int32).cuda()
+        lengths = [have + n for have, n in zip(self.lengths, counts)]
+        lens = torch.tensor(lengths, dtype=torch.int32).cuda()
         at = None if single else torch.tensor(starts, dtype=torch.int32).cuda()
         torch.index_select(self.embedding, 0, torch.cat(texts), out=m["stream"])
 
@@ -193,6 +193,7 @@ class Decoder:
             return m["rows"].view(rows, c.width)
 
         self._layers(m, attend)
+        self.lengths = lengths  # (a call that fails before this has added no token: the next one writes the same rows)
         delta, stream = m["delta"], m["stream"]
         if not every and not single:
             last = torch.tensor([max(s - 1, 0) for s in starts[1:]]).cuda()
