@@ -1,9 +1,11 @@
-"""The small decoder over pages: what it refuses and what it keeps when a call fails."""
+"""The small decoder over pages: what it refuses, what it keeps when a call fails, and logits under a window."""
+import math
+
 import pytest
 import torch
 
 from paper_2407_20485_amd import decoder as D
-from test_gpu_decoder import SMALL
+from test_gpu_decoder import SMALL, values
 from test_gpu_decoder_pages import texts
 
 pytestmark = pytest.mark.gpu
@@ -37,3 +39,65 @@ def test_a_call_that_fails_adds_no_tokens():
         model.feed([x[:3].float() for x in t])
     assert model.lengths == [10, 7]
     assert torch.equal(model.feed([x[:3] for x in t]), again)
+
+
+# ---- windows ----------------------------------------------------------------------------------------------------------------------------
+
+def plain(model, tokens, window, sinks):
+    """Logits of every position of one text in 64 bits: a token sees the newest `window` ones and the first `sinks`."""
+    c, n = model.config, len(tokens)
+    h = model.embedding[tokens].double()
+    norm = lambda x, w: x / torch.sqrt(x.square().mean(-1, keepdim=True) + c.eps) * w.double()  # noqa: E731
+    r = c.rotary_dims // 2
+    cos, sin = model.table[:n, None, :r].double(), model.table[:n, None, r:].double()
+    turn = lambda x: torch.cat([x[..., :r] * cos - x[..., r: 2 * r] * sin, x[..., r: 2 * r] * cos + x[..., :r] * sin, x[..., 2 * r:]], -1)  # noqa: E731
+    i, j = torch.arange(n, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
+    hidden = ~((j <= i) & ((i - j < window) | (j < sinks)))
+    for layer in model.layers:
+        x = norm(h, layer["norm1"]) @ values(layer["qkv"]).t()
+        q, k, v = x.view(n, -1, c.d).split([c.heads, c.kv_heads, c.kv_heads], 1)
+        q, k = turn(q), turn(k)
+        k, v = (y.repeat_interleave(c.heads // c.kv_heads, 1) for y in (k, v))
+        p = torch.matmul(q.transpose(0, 1).contiguous(), k.permute(1, 2, 0).contiguous()) / math.sqrt(c.d)
+        p = torch.softmax(p.masked_fill(hidden, -math.inf), -1)
+        o = torch.matmul(p, v.transpose(0, 1).contiguous()).transpose(0, 1).reshape(n, c.width)
+        h = h + o @ values(layer["out"]).t()
+        g, u = (norm(h, layer["norm2"]) @ values(layer["gate_up"]).t()).split(c.inner, -1)
+        h = h + (g * torch.sigmoid(g) * u) @ values(layer["down"]).t()
+    return norm(h, model.norm) @ values(model.head).t()
+
+
+@pytest.mark.parametrize("config", SMALL)
+@pytest.mark.parametrize("window,sinks", [(6, 0), (6, 3), (17, 4)])
+@pytest.mark.parametrize("page", [8, 16])
+def test_logits_under_a_window(config, window, sinks, page):
+    """Texts longer than the window, as prompts, chunks and single tokens: the plain model's logits under the same window, within the
+    bound of 8-bit activations, and not those without it or with the other numbers of first tokens."""
+    model = D.Decoder(config, positions=64)
+    t = texts(config, (50, 33))
+    model.start_paged(2, 52, page, window=window, sinks=sinks)
+    at, got = [0, 0], []
+    for counts in ((30, 12), (9, 1), (1, 19), (1, 1), (9, 0)):
+        logits = model.feed([x[a: a + n] for x, a, n in zip(t, at, counts)])
+        at = [a + n for a, n in zip(at, counts)]
+        got += [(i, at[i] - 1, logits[i].double().clone()) for i in range(2) if counts[i]]
+    off = lambda g, w: float((g - w).norm() / w.norm())  # noqa: E731
+    want = [plain(model, x, window, sinks) for x in t]
+    other = [[plain(model, x, *o) for x in t] for o in ((64, 0), (window, 0 if sinks else 3), (window + 3, sinks))]
+    # an activation in 8 bits is off by 3 % in the mean square; four such products per layer, each diluted by the residual stream
+    for i, last, g in got:
+        assert off(g, want[i][last]) < 0.1, (i, last)
+    worst = lambda w: max(off(g, w[i][last]) for i, last, g in got)  # noqa: E731
+    assert all(worst(o) > worst(want) for o in other)
+
+
+def test_a_window_that_holds_the_text_changes_nothing():
+    model = D.Decoder(SMALL[0], positions=64)
+    t = texts(SMALL[0], (40, 21))
+    got = []
+    for window, sinks in ((None, 0), (40, 0), (41, 4), (39, 0)):
+        model.start_paged(2, 40, 16, window=window, sinks=sinks)
+        got.append(model.feed(t, every=True).clone())
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+    assert not torch.equal(got[0][39], got[3][39])              # the only token that the window does not reach back for
+    assert torch.equal(got[0][:39], got[3][:39]) and torch.equal(got[0][40:], got[3][40:])
