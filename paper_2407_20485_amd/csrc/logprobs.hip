@@ -9,8 +9,8 @@
 // to a list (somewhat more than k tokens for each time that the lanes take as many) whose tokens are ranked against each other.  A list
 // that overflows (rows that rise, or of few values) is given up and the k found one by one.
 //
-// 2000 x 50272 in bf16 (201 MB): 43 us = 4.7 TB/s without alternatives, where the vector units are as busy as the memory (100 million
-// exponentials), 60 with 20 of them; 1000 rows in fp32 36 us = 5.6 TB/s and 44.
+// 2000 x 50272 in bf16 (201 MB): 42 us = 4.8 TB/s without alternatives, where the vector units are as busy as the memory (100 million
+// exponentials), 52 with 20 of them; 1000 rows in fp32 36 us = 5.6 TB/s and 44.
 #include <float.h>
 
 #include "a2sf_internal.h"
@@ -24,7 +24,8 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kGroups = 256, kListed = 1024;
 constexpr float kFar = -200.f;  // exp(kFar) is 0 in fp32
 
-// exp(y) for y <= 0
+// exp(y) for y <= 0.  The rounding of the product puts |y| units of rounding into it, which the sums hide: 512 rows of 32000 logits of standard deviation
+// 2 are off by 2.2e-7 (root mean square), as with what the rounding cuts off put back (2.5e-7; 12 % more time) and as fp32's own exp (2.2e-7).
 __device__ __forceinline__ float exp_of(float y) { return __builtin_amdgcn_exp2f(y * kLog2e); }
 
 struct Sums {
@@ -274,7 +275,9 @@ template <typename T>
 bool launch(const LogProbsArgs& a, hipStream_t st) {
   if (!grid_fits((unsigned long long)a.rows, 1024)) return false;
   // Half as many lanes to a row where there are more rows than the chip holds at once with 1024 to each: a row's barriers then wait beside
-  // others' work (2000 x 50272 bf16, 20 alternatives: 60 us, 70 with 1024; with 64, whose list grows longer, 79 and 73; 256 rows 15.0 and 12.4).
+  // others' work (us with 512 / 1024 lanes, 50272 logits in bf16: 2000 rows with 20 alternatives 52 / 61, with 33 57 / 63, with 64, whose list grows
+  // longer, 73 / 69; 513 rows 20 / 23, 300 rows 17.6 / 16.8).  Short rows take 256 (2000 rows of 8192 14.0, 17.5 with 512; 100 rows of 4096 in fp32 5.6, 6.8 with 1024,
+  // of 16384 9.8 and 6.3).
   if (a.n <= 8192) log_probs_kernel<T, 256><<<(uint32_t)a.rows, 256, 0, st>>>(a);
   else if (a.rows > 512 && a.alternatives <= 32) log_probs_kernel<T, 512><<<(uint32_t)a.rows, 512, 0, st>>>(a);
   else log_probs_kernel<T, 1024><<<(uint32_t)a.rows, 1024, 0, st>>>(a);

@@ -625,12 +625,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a, int unit) 
 int row_blocks(int tokens, int group, int sequences, bool one_each, int rows) {
   return one_each ? sequences * ((group + rows - 1) / rows) : (int)((long long)tokens * group / rows) + sequences;
 }
-// Several tokens of a sequence: shares for `groups` workgroups whose rows see at most `most` tokens
-constexpr int kWantedGroups = 2048, kWantedTileGroups = 1024;
-int splits_for(long long groups, long long most, int unit, int wanted) {
-  const long long want = (wanted + groups - 1) / groups, units = (most + unit - 1) / unit;
+// Several tokens of a sequence: shares of at least `unit` tokens for `groups` workgroups whose rows see at most `most`.  Two workgroups to a compute
+// unit are on the chip at once, and as many are wanted (us with 256 / 512 / 1024 / 2048 of them, 32 heads on 8: 512 tokens behind 8192 113 / 92 / 108 / 108,
+// 64 behind 8192 33 / 31 / 41 / 39, the same over pages of 8 bits 145 / 101 / 119 / 119; in fp32 64 behind 4096 94 / 82 / 94 / 118, 256 behind 2000 133 / 133 / 151 / 170).
+constexpr int kWantedGroups = 512;
+int splits_for(long long groups, long long most, long long unit) {
+  const long long want = (kWantedGroups + groups - 1) / groups, units = most / unit;
   return (int)std::max(1ll, std::min({want, units, (long long)kMostSplits}));
 }
+// The tile form: a share costs each row of the call some writing and reading, so the more rows, the more tokens it has to have (us with shares of
+// 128 / 512 / 1024 / 2048 tokens or more, and whole rows, 32 heads on 8: 16 tokens behind 4096 in 4 sequences, 2048 rows, 29 / 31 / 33 / 43, 93; 256 behind 4096, 8192
+// rows, 40 / 40 / 44 / 47, 96; 512 alone, 16384 rows, 26 / 18 / 18 / 18, 18, behind 4096 60 / 60 / 60 / 66, 102; 4 x 256 behind 512, 32768 rows, 46 / 46 / 24 / 24, 24, behind
+// 1024 54 / 54 / 54 / 35, 35).
+constexpr int kRowsPerToken = 16;
+long long tokens_of_share(long long rows) { return std::max((long long)kFewestTiles * kTileTokens, rows / kRowsPerToken); }
 size_t part_bytes(long long rows, int splits, int d) { return splits > 1 ? (size_t)rows * splits * (d + 2) * 4 : 0; }
 // One token of each: workgroups that share the tokens evenly, or 0 where a piece goes to each workgroup: if no piece has more than a unit, or if
 // there are two pieces and more for each workgroup on the chip and none can be so long that it runs on alone, or the lengths are too many to be
@@ -670,12 +678,13 @@ bool attend(PagedArgs a, void* workspace, size_t bytes, hipStream_t st) {
     if (a.even) grid = a.even;
     a.part_ml = a.part + 2ll * a.even * a.part_rows * D;
   } else {
-    a.splits = tiles ? splits_for(groups, most, kFewestTiles * kTileTokens, kWantedTileGroups) : splits_for(groups, most, F::UNIT, kWantedGroups);
+    a.splits = splits_for(groups, most, tiles ? tokens_of_share(rows) : F::UNIT);
     while (a.splits > 1 && part_bytes(rows, a.splits, D) > bytes) --a.splits;
     a.part_ml = a.part + rows * a.splits * D;
     grid *= a.splits;
   }
-  const bool few = rows <= 2048;  // four waves to a row
+  // four waves to a row (one token of 8000, 32 rows, 15.0 us, 17.9 with one; a chunk of 16, 512 rows, 19.9 and 20.8; 64 tokens of 8000, 2048 rows, 216 and 212)
+  const bool few = rows <= 512;
   const unsigned long long join = few ? (unsigned long long)rows : (unsigned long long)(rows + 3) / 4;
   if (!grid_fits(grid, 64 * kRowWaves) || !grid_fits(join, 256)) return false;
   if (tiles) launch_paged_tiles(a, (uint32_t)grid, st);
@@ -700,12 +709,12 @@ bool attend(const PagedArgs& a, void* workspace, size_t bytes, hipStream_t st) {
 
 size_t paged_workspace(int tokens, int heads, int kv_heads, int d, int sequences, long long table_tokens) {
   const long long rows = (long long)tokens * heads;
-  const auto bytes = [&](bool one_each, int block, int unit, int wanted) {
-    const long long groups = (long long)row_blocks(tokens, heads / kv_heads, sequences, one_each, block) * kv_heads;
-    return part_bytes(rows, splits_for(groups, table_tokens, unit, wanted), d);
+  const auto bytes = [&](int block, long long unit) {
+    const long long groups = (long long)row_blocks(tokens, heads / kv_heads, sequences, false, block) * kv_heads;
+    return part_bytes(rows, splits_for(groups, table_tokens, unit), d);
   };
   // (of the forms for single tokens that of fp32 has the smaller shares)
-  size_t most = std::max(bytes(false, kRows, 16 * kRowWaves, kWantedGroups), bytes(false, kTileRows, kFewestTiles * kTileTokens, kWantedTileGroups));
+  size_t most = std::max(bytes(kRows, 16 * kRowWaves), bytes(kTileRows, tokens_of_share(rows)));
   if (tokens == sequences) {
     const long long pieces = (long long)row_blocks(tokens, heads / kv_heads, sequences, true, kRows) * kv_heads;
     const int unit = 16 * kRowWaves;

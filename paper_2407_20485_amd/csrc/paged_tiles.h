@@ -26,7 +26,8 @@ __device__ __forceinline__ TilePlan tile_plan(const PagedArgs& a, const NewToken
   p.sink_tiles = (p.sinks + kTileTokens - 1) / kTileTokens;
   if (p.sinks >= p.from) p.from = p.sink_tiles = 0;
   p.tiles = p.sink_tiles + (p1 - p.from) / kTileTokens + 1;
-  p.per = max(kFewestTiles, (p.tiles + a.splits - 1) / a.splits);  // (the table may have room for many more than there are)
+  const int shares = max(1, min(a.splits, p.tiles / kFewestTiles));  // (the table may have room for many more tiles than there are)
+  p.per = (p.tiles + shares - 1) / shares;
   p.parts = (p.tiles + p.per - 1) / p.per;
   return p;
 }
