@@ -1,11 +1,11 @@
 """Forms of attention over pages that are chosen by the caller or by a call's sizes: probabilities as two numbers, shares of single tokens
-where there are many pieces, a workspace that is too small.  Tolerances as in test_gpu_pages.py."""
+where there are many pieces, a workspace that is too small; and calls as a serving loop makes them.  Tolerances as in test_gpu_pages.py."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2407_20485_amd import binding as B
-from test_gpu_pages import RAGGED, Batch, check_attention, strided
+from test_gpu_pages import DT, RAGGED, Batch, check_attention, check_log_probs, strided
 
 pytestmark = pytest.mark.gpu
 
@@ -123,3 +123,69 @@ def test_chunks_with_less_workspace(dtype, eight, wide, share):
     assert bool((ws[some.numel():] == 0xFF).all())
     if share > 0.5:
         assert not bool((some == 0xFF).all())
+
+
+# ---- calls of a serving loop ----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,eight", [("bf16", False), ("bf16", True), ("f32", False)])
+def test_two_graphs_share_a_workspace(dtype, eight):
+    """A step and a chunk captured apart on the same workspace and replayed in turn, eager calls between them: the eager results each time."""
+    step = Batch(58, [(900, 1), (0, 0), (3000, 1)], 2, 128, 16, dtype, eight, one_each=True).fill()
+    chunk = Batch(59, [(1500, 30), (0, 70)], 2, 128, 16, dtype, eight).fill()
+    gen = torch.Generator("cuda").manual_seed(58)
+    calls = []
+    ws = torch.empty(max(space(step, 8).numel(), space(chunk, 8).numel()), dtype=torch.uint8, device="cuda")
+    for b in (step, chunk):
+        q = torch.randn(b.tokens, 8, 128, device="cuda", generator=gen).to(b.dt)
+        o = torch.empty_like(q)
+        go = lambda b=b, q=q, o=o: B.a2sf_paged_attention(q, b.cache, b.table, b.len, o, starts=b.starts, window=2000, sinks=3,  # noqa: E731
+                                                          workspace=ws)
+        go()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            go()
+        calls.append((b, q, o, graph))
+    for turn in range(4):
+        for b, q, o, _ in calls:
+            q.copy_(torch.randn(q.shape, device="cuda", generator=gen))
+            o.zero_()
+        for i in ((0, 1), (1, 0), (0, 0, 1), (1,))[turn]:
+            calls[i][3].replay()
+        torch.cuda.synchronize()
+        for i, (b, q, o, _) in enumerate(calls):
+            if (turn, i) != (3, 0):
+                assert torch.equal(o, run(b, q, 2000, 3, ws)), (turn, i)
+
+
+@pytest.mark.parametrize("dtype,eight", [("bf16", False), ("f32", True)])
+def test_append_leaves_tokens_behind_the_last_sequence(dtype, eight):
+    """A padded batch: rows that no sequence has write nothing, before the first start and behind the last."""
+    b = Batch(60, [(5, 9), (0, 4), (30, 0), (17, 12)], 2, 64, 8, dtype, eight)
+    heads, total = 3, 40
+    x = torch.randn(total, (heads + 4) * 64, device="cuda", generator=torch.Generator("cuda").manual_seed(60)).to(b.dt)
+    q, k, v = x.unflatten(1, (-1, 64)).split([heads, 2, 2], 1)
+    table = torch.empty(64, 64, device="cuda")
+    B.a2sf_rotary_table(table)
+    first = 6
+    want = torch.empty(25, heads, 64, dtype=b.dt, device="cuda")
+    B.a2sf_paged_append(q[first: first + 25], k[first: first + 25], v[first: first + 25], b.cache, b.table, b.len, starts=b.starts, q_out=want,
+                        rotary=table)
+    bits = lambda t: t.clone().view(torch.uint8)  # noqa: E731
+    kept = [bits(t) for t in b.cache.tensors()]
+    b.rubbish()
+    out = torch.full((total, heads, 64), 5.0, dtype=b.dt, device="cuda")
+    B.a2sf_paged_append(q, k, v, b.cache, b.table, b.len, starts=b.starts + first, q_out=out, rotary=table)
+    assert torch.equal(out[first: first + 25], want) and bool((out[:first] == 5).all()) and bool((out[first + 25:] == 5).all())
+    assert all(torch.equal(bits(t), w) for t, w in zip(b.cache.tensors(), kept))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,given", [(70, 257), (9000, 1030), (9000, 1024), (300, 2000)])
+def test_log_probs_of_more_tokens_than_lanes(dtype, n, given):
+    """The same tokens again and again, some that are none, more of them than a row has lanes."""
+    x = torch.randn(3, n, device="cuda", generator=torch.Generator("cuda").manual_seed(n)).to(DT[dtype])
+    tokens = torch.randint(-1, n + 1, (3, given), dtype=torch.int32, device="cuda", generator=torch.Generator("cuda").manual_seed(given))
+    logp = torch.full((3, given), 7.0, device="cuda")
+    B.a2sf_log_probs(x, tokens, logp)
+    check_log_probs(x, tokens, logp, None, None, None)
