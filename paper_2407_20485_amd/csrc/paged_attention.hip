@@ -90,8 +90,9 @@ __device__ __forceinline__ EvenPlace even_place(const PagedArgs& a, int unit, in
 // of V being read by 16 lanes side by side; a pair of tokens' values of one dimension is one byte permutation.
 // So neither P nor V goes through LDS.  Q and K take their dimensions in the order in which K's 16 bytes per lane come.
 // bf16: P goes into the product as two bf16 numbers, its value and what that leaves out (2^-17 of it stays out): the matrix pipe has room.
-// Bound by memory: 4 x 65536 tokens of 8 K/V heads 119 us = 6.1 TB/s, 200 x 1004 of 40 heads 660 = 6.2; in 8 bits 5.3.  A wave has one tile's
-// K and V in registers and asks for the next K when it has used this one's (two tiles at a time take 256 registers and spill: 200 x 1004
+// Bound by memory: 4 x up to 65536 tokens of 8 K/V heads 118 us = 6.1 TB/s, 200 x 1004 of 40 heads 657 = 6.3; 48 x up to 8192 in 8 bits 98 = 5.4,
+// in fp32 8 x up to 32768 265 = 5.7.  A wave has one tile's K and V
+// in registers and asks for the next K when it has used this one's (two tiles at a time take 256 registers and spill: 200 x 1004
 // 745 us without streaming loads and 951 with them).
 constexpr int kRows = 16;
 constexpr int kRowWaves = 4;
@@ -627,7 +628,7 @@ int row_blocks(int tokens, int group, int sequences, bool one_each, int rows) {
 }
 // Several tokens of a sequence: shares of at least `unit` tokens for `groups` workgroups whose rows see at most `most`.  Two workgroups to a compute
 // unit are on the chip at once, and as many are wanted (us with 256 / 512 / 1024 / 2048 of them, 32 heads on 8: 512 tokens behind 8192 113 / 92 / 108 / 108,
-// 64 behind 8192 33 / 31 / 41 / 39, the same over pages of 8 bits 145 / 101 / 119 / 119; in fp32 64 behind 4096 94 / 82 / 94 / 118, 256 behind 2000 133 / 133 / 151 / 170).
+// over pages of 8 bits 145 / 101 / 119 / 119, 64 behind 8192 33 / 31 / 41 / 39; in fp32 64 behind 4096 94 / 82 / 94 / 118, 256 behind 2000 133 / 133 / 151 / 170).
 constexpr int kWantedGroups = 512;
 int splits_for(long long groups, long long most, long long unit) {
   const long long want = (kWantedGroups + groups - 1) / groups, units = most / unit;
@@ -642,8 +643,8 @@ long long tokens_of_share(long long rows) { return std::max((long long)kFewestTi
 size_t part_bytes(long long rows, int splits, int d) { return splits > 1 ? (size_t)rows * splits * (d + 2) * 4 : 0; }
 // One token of each: workgroups that share the tokens evenly, or 0 where a piece goes to each workgroup: if no piece has more than a unit, or if
 // there are two pieces and more for each workgroup on the chip and none can be so long that it runs on alone, or the lengths are too many to be
-// scanned by all.  us, a piece to each / even shares, 128 and 256 sequences on 8 K/V heads of d = 128 in tables for 8192 tokens (4 and 8 a piece
-// of the call): one of 8192 beside others of 300 tokens 132 / 47 and 143 / 81, all of 300 32 / 37 and 60 / 71, of 75 to 300 up to 1000 66 / 75 and 122 / 139; in tables for
+// scanned by all.  us, a piece to each / even shares, 128 and 256 sequences on 8 K/V heads of d = 128 in tables for 8192 tokens (8 and 4 for a
+// piece): one of 8192 beside others of 300 tokens 132 / 47 and 143 / 81, all of 300 32 / 37 and 60 / 71, of 75 to 300 up to 1000 66 / 75 and 122 / 139; in tables for
 // 65536: one such beside 500 937 / 94 and 954 / 144.  1024 sequences of 300 on one head 32 / 53.
 constexpr int kEvenGroups(int d) { return d == 64 ? 768 : 512; }  // as many as are on the chip at once
 constexpr int kLongPiece = 4;          // tokens for each piece of the call

@@ -5,8 +5,9 @@
 // A block's rows are the heads of a K/V head's group, token by token, so a tile of K and V serves all heads of the group at once.
 // Probabilities go into the second product as bf16 numbers, each within 2^-8 of itself, or with WIDE as two, its value and what that
 // leaves out (2^-17 of it stays out); their sum is of the unrounded ones.  The caller chooses: the second number is a half more matrix
-// instructions and three vector instructions a pair (4 prompts of up to 2048 tokens, 32 heads: 110 us without, 134 with it; 16384 tokens under a window of 2048
-// 587 and 736, without a window 2104 and 2774; 8192 tokens over pages of 8 bits 627 and 781; a chunk of 512 with 15 single tokens 92 and 102).
+// instructions and three vector instructions a pair (4 prompts of up to 2048 tokens, 32 heads: 111 us without, 136 with it; 16384 tokens under a window of 2048
+// 591 and 757, without a window 2145 and 2827; 8192 tokens over pages of 8 bits 643 and 781, of d = 64 345 and 448; a chunk of 512 with 15 single
+// tokens 83 and 97).
 #include <float.h>
 
 #include <algorithm>
